@@ -175,6 +175,120 @@ int regenvc_out_project(const void* attn_out, const void* w_o, const void* b_o, 
                         int n_tokens, int n_heads, int head_dim, void* stream);
 
 /*
+ * Steps of the same transformer block around its attention and projections.  Conventions of this part: matrices are
+ * rows of elements with a row stride (in elements, 0 for "rows packed"; rows may be views of a wider tensor), element
+ * types are named per call, and a pointer needs the alignment of its elements only -- rows whose address, stride and
+ * width allow 16-byte accesses take them, others go element by element.  Vectors of parameters are fp32.  Arithmetic
+ * is fp32 with one rounding per result.  The calls allocate nothing, take scratch memory as arguments and are
+ * asynchronous on `stream`; all can be captured into a CUDA graph (after one call of the library on the device).
+ */
+typedef enum { REGENVC_BF16 = 0, REGENVC_F16 = 1, REGENVC_F32 = 2 } regenvc_type;
+typedef enum { REGENVC_NORM_NONE = 0, REGENVC_NORM_LAYER = 1, REGENVC_NORM_RMS = 2 } regenvc_norm;
+
+/*
+ * Norms before and after a block, fused with the block's gate and residual scale (backbone by reference, Sec. 3.2 /
+ * 3.4: every branch reads a normalised and modulated copy of the residual stream and is added back through a gate):
+ *     z  = N2(y) post_weight            (post_norm; N2 absent: z = y)
+ *     x' = residual_scale x + gate z    (y == NULL: x' = x, nothing is added or scaled)
+ *     h  = (N1(x') weight + bias) (1 + scale) + shift
+ * N is layer norm (v - mean) / sqrt(var + eps) or RMS norm v / sqrt(mean v^2 + eps) over `channels` (1 .. 8192).
+ * gate, scale, shift: fp32 rows of `channels`, one per tokens_per_mod consecutive tokens (all tokens, a frame, one
+ * token), mod_stride elements apart.  Any of gate, post_weight, weight, bias, scale, shift may be NULL (ones or zeros).
+ *   x, x_out : x_type;  y, h : io_type;  x_type is fp32 or equal to io_type
+ *   x_out    : x' rounded to x_type; may be x itself (in place, same stride), or NULL; NULL if y is NULL
+ *   h        : from x' before that rounding; NULL exactly if norm is REGENVC_NORM_NONE
+ * Other overlaps of a result with an operand are refused (REGENVC_ERR_ALIASING); NaN and infinity stay in their rows.
+ */
+typedef struct {
+    int n_tokens, channels, tokens_per_mod;
+    int x_type, io_type;        /* regenvc_type */
+    int norm, post_norm;        /* regenvc_norm */
+    float eps, post_eps;        /* >= 0 */
+    float residual_scale;
+    long long mod_stride;       /* >= channels, or 0: rows packed */
+    long long x_stride, y_stride, x_out_stride, h_stride;
+    long long dx_out_stride, dx_stride, dy_stride;   /* backward only */
+} regenvc_block_norm_desc;
+int regenvc_block_norm_forward(const regenvc_block_norm_desc* desc, const void* x, const void* y, const void* gate,
+                               const void* post_weight, const void* weight, const void* bias, const void* scale,
+                               const void* shift, void* x_out, void* h, void* stream);
+/*
+ * Its gradients, at the saved x' (x_out, x_type, x_out_stride; x itself where y is NULL): statistics are recomputed.
+ *   dh     : io_type, gradient of h (h_stride); NULL exactly if norm is REGENVC_NORM_NONE
+ *   dx_out : x_type, gradient that reaches x' by other ways (the residual stream), or NULL
+ *   dx, dy : gradients of x (x_type) and y (io_type); dx may be dx_out itself; each may be NULL
+ *   dgate, dscale, dshift : fp32 [rows of the modulation][channels], packed; dpost_weight, dweight, dbias : fp32
+ *            [channels]; NULL if not wanted; dgate, dpost_weight, dweight, dscale need the parameter they belong to, and
+ *            dweight, dbias, dscale, dshift need dh
+ *   workspace : regenvc_block_norm_workspace_bytes(n_tokens, channels) bytes, 16-byte aligned; calls that may overlap on
+ *            the GPU (and graphs that may be replayed at a time) need one each
+ * Sums over tokens run in fp32 in an order that depends on the shape only: two calls give the same bits.
+ */
+size_t regenvc_block_norm_workspace_bytes(int n_tokens, int channels);
+int regenvc_block_norm_backward(const regenvc_block_norm_desc* desc, const void* x_out, const void* y, const void* gate,
+                                const void* post_weight, const void* weight, const void* bias, const void* scale,
+                                const void* dh, const void* dx_out, void* dx, void* dy, void* dgate, void* dpost_weight,
+                                void* dweight, void* dbias, void* dscale, void* dshift, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary embedding by explicit positions on several axes, for queries and keys that are not a whole T x H x W grid in
+ * order (the attention entry points rotate those themselves): image or text tokens among the video's, cropped or
+ * resampled grids, frame times that are not whole numbers.  regenvc_cross_attn_forward() is attention on the result.
+ *   q, k : type, element (token n, head a, i) at n * token_stride + a * head_stride + i, i < head_dim (even, 2 .. 256);
+ *          k may be NULL (n_k_heads 0) and have fewer heads; results likewise; a result may be its operand (in place, same
+ *          strides), other overlaps are refused
+ *   positions : [n_axes][n_tokens] int32 or fp32 (pos_float), pos_stride elements between axes (0: n_tokens)
+ *   widths : elements of a head that turn with each axis, even, >= 2, their sum R <= head_dim; the rest is copied
+ *   halves : pair j is (j, j + R/2) instead of (2j, 2j + 1); pairs go to the axes in order
+ *   whole_ladder : frequency of pair j is theta^(-2j/R); else theta^(-2i/width) for the i-th pair of its axis
+ *   inverse : turn back (the gradient of the rotation)
+ * Angles are formed in 64 bits.  n_tokens >= 1.
+ */
+typedef struct {
+    int n_tokens, n_q_heads, n_k_heads, head_dim;
+    int type;                   /* regenvc_type */
+    int n_axes, widths[4];      /* 1 .. 4 axes */
+    float rope_theta;           /* > 0 */
+    int halves, whole_ladder, pos_float, inverse;   /* 0 or 1 */
+    long long pos_stride;
+    long long q_token_stride, q_head_stride, k_token_stride, k_head_stride;                 /* 0: packed */
+    long long q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+} regenvc_rope_axes_desc;
+int regenvc_rope_axes(const regenvc_rope_axes_desc* desc, const void* q, const void* k, const void* positions,
+                      void* q_out, void* k_out, void* stream);
+
+/*
+ * Microscaled 4-bit floating point (OCP MX: e2m1 elements, one e8m0 scale per 32 columns of a row): the projections
+ * with a quarter of the operand bytes and up to four times the tensor rate of bf16.
+ *
+ * Packed form of a [rows, cols] matrix (regenvc_mxfp4_bytes() bytes, 0 for invalid arguments; device, 256-byte aligned):
+ * cols_pad = cols rounded up to 128.
+ *   codes  : [rows][cols_pad / 2] bytes, element 2b of a row in the low, 2b + 1 in the high half of byte b; 0 behind cols
+ *   scales : at the next multiple of 512 bytes, value 2^(byte - 127), 255 = NaN; the byte of row r and block b (32
+ *            columns) at tile (r / 128) * (cols_pad / 128) + b / 4 of 512 bytes, in it (r % 32) * 16 + (r % 128) / 32 * 4
+ *            + b % 4; 0 behind the last row and block
+ * regenvc_mxfp4_quantize(): scale 2^(floor(log2 of the block's largest magnitude) - 2), at least 2^-127; elements to the
+ *   nearest code, ties to even, saturating at 6 scales.  A block that holds an infinity or NaN reads back as NaN.
+ *   src: type, row_stride elements between rows (0: cols).
+ * regenvc_mxfp4_dequantize(): the values that a packed matrix stands for, rounded to type.
+ * regenvc_mxfp4_project(): y = x w^T + bias on packed x [n_tokens, in_features] and w [out_features, in_features]; fp32
+ *   accumulation, y bf16 or fp16, packed rows, 16-byte aligned; bias fp32 [out_features] or NULL.  out_features must be a
+ *   multiple of 8 (REGENVC_ERR_UNSUPPORTED).  Waits inside are bounded as in the attention kernels.
+ * regenvc_mxfp4_linear(): the same from unpacked x, quantised in the call: as regenvc_mxfp4_quantize() into `scratch`
+ *   (regenvc_mxfp4_bytes(n_tokens, in_features) bytes, 256-byte aligned, its content unspecified afterwards) and
+ *   regenvc_mxfp4_project().
+ */
+size_t regenvc_mxfp4_bytes(int rows, int cols);
+int regenvc_mxfp4_quantize(const void* src, int type, int rows, int cols, long long row_stride, void* packed, void* stream);
+int regenvc_mxfp4_dequantize(const void* packed, void* dst, int type, int rows, int cols, long long row_stride,
+                             void* stream);
+int regenvc_mxfp4_project(const void* x_packed, const void* w_packed, const void* bias, void* y, int y_type,
+                          int n_tokens, int out_features, int in_features, void* stream);
+int regenvc_mxfp4_linear(const void* x, int x_type, long long x_stride, const void* w_packed, const void* bias, void* y,
+                         int y_type, int n_tokens, int out_features, int in_features, void* scratch, void* stream);
+
+/*
  * Block-wise attention for sequence-parallel use (Sec. 3.5: Ring attention streams key/value blocks around
  * the devices and combines the per-block results by the online-softmax rule; the result is unsharded
  * attention, only summed in another order).

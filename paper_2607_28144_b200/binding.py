@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_HERE, "libregenvc_attn.so")
 OK, ERR_NULL_POINTER, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_MISALIGNED, ERR_ALIASING, ERR_CUDA, ERR_TIMEOUT, \
     ERR_WORKSPACE, ERR_RANGE, ERR_STATIC_LIMIT, ERR_INTERNAL = range(12)
 STATIC_SCRATCH_BYTES = 16 << 20
+NORM_NONE, NORM_LAYER, NORM_RMS = range(3)
+TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 EXPORTS = [
     "regenvc_attn_forward", "regenvc_cross_attn_forward", "regenvc_attn_forward_host",
@@ -28,7 +30,30 @@ EXPORTS = [
     "regenvc_prepared_bytes", "regenvc_cross_kv_prepare", "regenvc_cross_attn_forward_prepared",
     "regenvc_attn_forward_prepared", "regenvc_qkv_rope_project", "regenvc_out_project", "regenvc_attn_merge",
     "regenvc_ulysses_scatter_heads", "regenvc_ulysses_gather_heads", "regenvc_debug_expire_wait",
+    "regenvc_block_norm_forward", "regenvc_block_norm_backward", "regenvc_block_norm_workspace_bytes",
+    "regenvc_rope_axes", "regenvc_mxfp4_bytes", "regenvc_mxfp4_quantize", "regenvc_mxfp4_dequantize",
+    "regenvc_mxfp4_project", "regenvc_mxfp4_linear",
 ]
+
+
+class BlockNormDesc(ctypes.Structure):
+    """``regenvc_block_norm_desc``."""
+    _fields_ = [(n, ctypes.c_int) for n in ("n_tokens", "channels", "tokens_per_mod", "x_type", "io_type", "norm",
+                                            "post_norm")] + \
+               [(n, ctypes.c_float) for n in ("eps", "post_eps", "residual_scale")] + \
+               [(n, ctypes.c_longlong) for n in ("mod_stride", "x_stride", "y_stride", "x_out_stride", "h_stride",
+                                                 "dx_out_stride", "dx_stride", "dy_stride")]
+
+
+class RopeAxesDesc(ctypes.Structure):
+    """``regenvc_rope_axes_desc``."""
+    _fields_ = [(n, ctypes.c_int) for n in ("n_tokens", "n_q_heads", "n_k_heads", "head_dim", "type", "n_axes")] + \
+               [("widths", ctypes.c_int * 4), ("rope_theta", ctypes.c_float)] + \
+               [(n, ctypes.c_int) for n in ("halves", "whole_ladder", "pos_float", "inverse")] + \
+               [(n, ctypes.c_longlong) for n in ("pos_stride", "q_token_stride", "q_head_stride", "k_token_stride",
+                                                 "k_head_stride", "q_out_token_stride", "q_out_head_stride",
+                                                 "k_out_token_stride", "k_out_head_stride")]
+
 
 _lib = None
 
@@ -80,6 +105,25 @@ def lib() -> ctypes.CDLL:
     L.regenvc_qkv_rope_project.restype = i32
     L.regenvc_out_project.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
     L.regenvc_out_project.restype = i32
+    i64 = ctypes.c_longlong
+    L.regenvc_block_norm_forward.argtypes = [ctypes.POINTER(BlockNormDesc)] + [vp] * 11
+    L.regenvc_block_norm_forward.restype = i32
+    L.regenvc_block_norm_workspace_bytes.argtypes = [i32, i32]
+    L.regenvc_block_norm_workspace_bytes.restype = sz
+    L.regenvc_block_norm_backward.argtypes = [ctypes.POINTER(BlockNormDesc)] + [vp] * 18 + [sz, vp]
+    L.regenvc_block_norm_backward.restype = i32
+    L.regenvc_rope_axes.argtypes = [ctypes.POINTER(RopeAxesDesc)] + [vp] * 6
+    L.regenvc_rope_axes.restype = i32
+    L.regenvc_mxfp4_bytes.argtypes = [i32, i32]
+    L.regenvc_mxfp4_bytes.restype = sz
+    L.regenvc_mxfp4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp]
+    L.regenvc_mxfp4_quantize.restype = i32
+    L.regenvc_mxfp4_dequantize.argtypes = [vp, vp, i32, i32, i32, i64, vp]
+    L.regenvc_mxfp4_dequantize.restype = i32
+    L.regenvc_mxfp4_project.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    L.regenvc_mxfp4_project.restype = i32
+    L.regenvc_mxfp4_linear.argtypes = [vp, i32, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp]
+    L.regenvc_mxfp4_linear.restype = i32
     L.regenvc_workspace_bytes.argtypes = [i32, i32, i32]
     L.regenvc_workspace_bytes.restype = sz
     L.regenvc_set_workspace.argtypes = [vp, sz]
@@ -256,6 +300,292 @@ def regenvc_out_project(attn_out, w_o, b_o, y=None, stream=None):
         raise TypeError("y must be a contiguous CUDA bf16 tensor [tokens, C]")
     _check(lib().regenvc_out_project(attn_out.data_ptr(), w_o.data_ptr(), None if b_o is None else b_o.data_ptr(),
                                      y.data_ptr(), n, h, d, _stream(stream)))
+    return y
+
+
+# ---------------------------------------------------------------------------- steps around the attention of a block
+def _addr(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _new(shape, dtype, device, stream):
+    """A result or scratch tensor that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _on_current_device(first, *others):
+    """All operands on the device the library launches on (the current one)."""
+    if not first.is_cuda:
+        raise TypeError("expected CUDA tensors")
+    dev = first.device
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"operands are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError("operands are on different devices")
+
+
+def _rows(t, name: str, dtype, shape):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise TypeError(f"{name} must be {dtype} {list(shape)} with neighbouring columns")
+    _row_stride(t, name)
+
+
+def _row_stride(t, name: str = "the tensor") -> int:
+    """Elements between rows as the library takes them (0: packed); rows that share memory are refused here, since an
+    expanded tensor's stride of 0 would read as "packed"."""
+    if t is None or t.shape[0] < 2:
+        return 0
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name} has rows that overlap (an expanded tensor?)")
+    return t.stride(0)
+
+
+def _vector(t, name: str, size: int):
+    if t is not None and (t.dtype != torch.float32 or t.numel() != size or not t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous fp32 tensor of {size} elements (or None)")
+
+
+def _modulation(n: int, c: int, tokens_per_mod, tensors):
+    """Checks the modulation tables and returns (tokens_per_mod, rows, row stride)."""
+    per = n if tokens_per_mod is None else int(tokens_per_mod)
+    if per < 1:
+        raise ValueError("tokens_per_mod must be at least 1")
+    rows = -(-n // per)
+    strides = set()
+    for t, name in tensors:
+        if t is not None:
+            _rows(t, name, torch.float32, (rows, c))
+            if rows > 1:
+                strides.add(t.stride(0))
+    if len(strides) > 1:
+        raise ValueError("gate, scale and shift must have the same distance between rows")
+    return per, rows, strides.pop() if strides else 0
+
+
+def regenvc_block_norm_forward(x, y=None, *, gate=None, post_norm: int = NORM_NONE, post_weight=None,
+                               post_eps: float = 1e-6, residual_scale: float = 1.0, norm: int = NORM_LAYER, weight=None,
+                               bias=None, eps: float = 1e-6, scale=None, shift=None, tokens_per_mod=None, h_dtype=None,
+                               x_out=None, h=None, stream=None):
+    """x' = residual_scale x + gate N2(y) and h = (N1(x') weight + bias) (1 + scale) + shift in one pass; returns
+    (x' or None where y is None, h or None where norm is NORM_NONE).  x [tokens, C]: bf16, fp16 or fp32; y and h: the
+    same type, or any of them where x is fp32 (h: ``h_dtype``, else y's, else x's).  gate, scale, shift: fp32 [rows, C],
+    one row per ``tokens_per_mod`` tokens (None: one for all); post_weight, weight, bias: fp32 [C].  x may be given as
+    ``x_out`` (in place)."""
+    if x.dim() != 2 or x.dtype not in TYPES:
+        raise TypeError("x must be [tokens, C] in bf16, fp16 or fp32")
+    _on_current_device(x, y, gate, post_weight, weight, bias, scale, shift, x_out, h)
+    n, c = x.shape
+    io = h.dtype if h is not None else h_dtype or (y.dtype if y is not None else x.dtype)
+    if io not in TYPES:
+        raise TypeError("h must be bf16, fp16 or fp32")
+    _rows(x, "x", x.dtype, (n, c))
+    if y is not None:
+        _rows(y, "y", io, (n, c))
+    for t, name in ((post_weight, "post_weight"), (weight, "weight"), (bias, "bias")):
+        _vector(t, name, c)
+    per, _, mod_stride = _modulation(n, c, tokens_per_mod, ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+    if y is None:
+        if x_out is not None:
+            raise ValueError("x_out needs y")
+    elif x_out is None:
+        x_out = _new((n, c), x.dtype, x.device, stream)
+    if norm == NORM_NONE:
+        if h is not None:
+            raise ValueError("h needs a norm")
+    elif h is None:
+        h = _new((n, c), io, x.device, stream)
+    if x_out is not None:
+        _rows(x_out, "x_out", x.dtype, (n, c))
+    if h is not None:
+        _rows(h, "h", io, (n, c))
+    d = BlockNormDesc(n, c, min(per, 2**31 - 1), TYPES[x.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
+                      mod_stride, _row_stride(x), _row_stride(y), _row_stride(x_out), _row_stride(h))
+    _check(lib().regenvc_block_norm_forward(ctypes.byref(d), x.data_ptr(), _addr(y), _addr(gate), _addr(post_weight),
+                                            _addr(weight), _addr(bias), _addr(scale), _addr(shift), _addr(x_out), _addr(h),
+                                            _stream(stream)))
+    return x_out, h
+
+
+def regenvc_block_norm_workspace_bytes(n_tokens: int, channels: int) -> int:
+    return int(lib().regenvc_block_norm_workspace_bytes(n_tokens, channels))
+
+
+def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, post_norm: int = NORM_NONE, post_weight=None,
+                                post_eps: float = 1e-6, residual_scale: float = 1.0, norm: int = NORM_LAYER, weight=None,
+                                bias=None, eps: float = 1e-6, scale=None, shift=None, tokens_per_mod=None, dx=None,
+                                workspace=None, stream=None):
+    """Gradients of regenvc_block_norm_forward at the saved ``x_out`` (its x where y was None): dh is the gradient of h
+    (None where norm is NORM_NONE), dx_out the one that reaches x_out by other ways (or None).  Returns a dict: dx, dy
+    (None without y), and dgate, dpost_weight, dweight, dbias, dscale, dshift, each None where its parameter is.  ``shift``
+    only says whether dshift is wanted.  ``dx`` may be dx_out (in place)."""
+    like = x_out if x_out is not None else dx_out
+    if like is None or like.dim() != 2 or like.dtype not in TYPES:
+        raise TypeError("x_out must be [tokens, C] in bf16, fp16 or fp32")
+    _on_current_device(like, x_out, dh, dx_out, y, gate, post_weight, weight, bias, scale, shift, dx, workspace)
+    n, c = like.shape
+    io = dh.dtype if dh is not None else (y.dtype if y is not None else like.dtype)
+    if io not in TYPES:
+        raise TypeError("dh must be bf16, fp16 or fp32")
+    for t, name, dtype in ((x_out, "x_out", like.dtype), (dh, "dh", io), (dx_out, "dx_out", like.dtype), (y, "y", io)):
+        if t is not None:
+            _rows(t, name, dtype, (n, c))
+    for t, name in ((post_weight, "post_weight"), (weight, "weight"), (bias, "bias")):
+        _vector(t, name, c)
+    per, rows, mod_stride = _modulation(n, c, tokens_per_mod, ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+    new = lambda shape, dtype: _new(shape, dtype, like.device, stream)  # noqa: E731
+    dx = new((n, c), like.dtype) if dx is None else dx
+    _rows(dx, "dx", like.dtype, (n, c))
+    f32 = torch.float32
+    g = {"dx": dx, "dy": None if y is None else new((n, c), io)}
+    for t, name in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")):
+        g[name] = None if t is None else new((rows, c), f32)
+    for t, name in ((post_weight, "dpost_weight"), (weight, "dweight"), (bias, "dbias")):
+        g[name] = None if t is None else new((c,), f32)
+    need = regenvc_block_norm_workspace_bytes(n, c)
+    if workspace is None:
+        workspace = new((need,), torch.uint8)
+    d = BlockNormDesc(n, c, min(per, 2**31 - 1), TYPES[like.dtype], TYPES[io], norm, post_norm, eps, post_eps,
+                      residual_scale, mod_stride, 0, _row_stride(y), _row_stride(x_out), _row_stride(dh),
+                      _row_stride(dx_out), _row_stride(dx), 0)
+    _check(lib().regenvc_block_norm_backward(
+        ctypes.byref(d), _addr(x_out), _addr(y), _addr(gate), _addr(post_weight), _addr(weight), _addr(bias), _addr(scale),
+        _addr(dh), _addr(dx_out), dx.data_ptr(), _addr(g["dy"]), _addr(g["dgate"]), _addr(g["dpost_weight"]),
+        _addr(g["dweight"]), _addr(g["dbias"]), _addr(g["dscale"]), _addr(g["dshift"]), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+    return g
+
+
+def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, halves: bool = False,
+                      whole_ladder: bool = False, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotates q [tokens, heads, head_dim] and k (fewer heads allowed, or None) by ``positions`` [axes, tokens] (int32 or
+    fp32), ``widths[a]`` elements of a head turning with axis a; returns (q_out, k_out).  Views with any token and head
+    strides are taken as they are; q / k given as q_out / k_out are rotated in place.  ``inverse`` turns back, which is the
+    gradient."""
+    if q.dim() != 3 or q.dtype not in TYPES:
+        raise TypeError("q must be [tokens, heads, head_dim] in bf16, fp16 or fp32")
+    _on_current_device(q, k, positions, q_out, k_out)
+    n, hq, d = q.shape
+    widths = [int(w) for w in widths]
+    if positions.dtype not in (torch.int32, torch.float32) or tuple(positions.shape) != (len(widths), n) or \
+            (n > 1 and positions.stride(1) != 1) or (len(widths) > 1 and positions.stride(0) < n):
+        raise TypeError(f"positions must be int32 or fp32 [{len(widths)}, {n}] with neighbouring tokens")
+    if k is not None and (k.dtype != q.dtype or k.dim() != 3 or k.shape[0] != n or k.shape[2] != d):
+        raise TypeError("k must be [tokens, heads, head_dim] of q's type")
+    if k is None and k_out is not None:
+        raise ValueError("k_out needs k")
+    if len(widths) > 4:
+        raise RegenvcError(ERR_BAD_SHAPE, status_string(ERR_BAD_SHAPE))
+    if q_out is None:
+        q_out = _new(q.shape, q.dtype, q.device, stream)
+    if k is not None and k_out is None:
+        k_out = _new(k.shape, k.dtype, k.device, stream)
+    hk = 0 if k is None else k.shape[1]
+    strides = []
+    for t, like, name in ((q, q, "q"), (k, k, "k"), (q_out, q, "q_out"), (k_out, k, "k_out")):
+        if t is None:
+            strides += [0, 0]
+            continue
+        if t.dtype != q.dtype or t.shape != like.shape or (d > 1 and t.stride(2) != 1):
+            raise TypeError(f"{name} must have its operand's type and shape and neighbouring elements of a head")
+        if (n > 1 and t.stride(0) < d) or (t.shape[1] > 1 and t.stride(1) < d):
+            raise ValueError(f"{name} has vectors that overlap (an expanded tensor?)")
+        # the stride of an axis with one entry is never used: name the packed one
+        head = t.stride(1) if t.shape[1] > 1 else d
+        strides += [t.stride(0) if n > 1 else max(t.shape[1] * head, d), head]
+    desc = RopeAxesDesc(n, hq, hk, d, TYPES[q.dtype], len(widths), (ctypes.c_int * 4)(*widths), float(rope_theta), int(halves),
+                        int(whole_ladder), int(positions.dtype == torch.float32), int(inverse),
+                        positions.stride(0) if len(widths) > 1 else 0, *strides)
+    _check(lib().regenvc_rope_axes(ctypes.byref(desc), q.data_ptr(), _addr(k), positions.data_ptr(), q_out.data_ptr(),
+                                   _addr(k_out), _stream(stream)))
+    return q_out, k_out
+
+
+def regenvc_mxfp4_bytes(rows: int, cols: int) -> int:
+    return int(lib().regenvc_mxfp4_bytes(rows, cols))
+
+
+def _mx_packed(t, name: str, rows: int, cols: int):
+    need = regenvc_mxfp4_bytes(rows, cols)
+    if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < need or need == 0:
+        raise TypeError(f"{name} must be a contiguous uint8 tensor of at least {need} bytes")
+
+
+def _mx_values(t, name: str):
+    if t.dim() != 2 or t.dtype not in TYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError(f"{name} must be [rows, cols] in bf16, fp16 or fp32 with neighbouring columns")
+
+
+def regenvc_mxfp4_quantize(src, packed=None, stream=None):
+    """Rows of bf16, fp16 or fp32 [rows, cols] to microscaled 4-bit form; returns the ``packed`` uint8 tensor."""
+    _mx_values(src, "src")
+    _on_current_device(src, packed)
+    rows, cols = src.shape
+    if packed is None:
+        packed = _new((regenvc_mxfp4_bytes(rows, cols),), torch.uint8, src.device, stream)
+    _mx_packed(packed, "packed", rows, cols)
+    _check(lib().regenvc_mxfp4_quantize(src.data_ptr(), TYPES[src.dtype], rows, cols, _row_stride(src), packed.data_ptr(),
+                                        _stream(stream)))
+    return packed
+
+
+def regenvc_mxfp4_dequantize(packed, rows: int, cols: int, dtype=torch.bfloat16, out=None, stream=None):
+    """The [rows, cols] values that a packed matrix stands for."""
+    _mx_packed(packed, "packed", rows, cols)
+    _on_current_device(packed, out)
+    if out is None:
+        out = _new((rows, cols), dtype, packed.device, stream)
+    _mx_values(out, "out")
+    if tuple(out.shape) != (rows, cols):
+        raise TypeError(f"out must be [{rows}, {cols}]")
+    _check(lib().regenvc_mxfp4_dequantize(packed.data_ptr(), out.data_ptr(), TYPES[out.dtype], rows, cols, _row_stride(out),
+                                          _stream(stream)))
+    return out
+
+
+def _mx_result(y, y_dtype, n: int, features: int, device, stream):
+    if y is None:
+        y = _new((n, features), y_dtype, device, stream)
+    if y.dtype not in (torch.bfloat16, torch.float16) or tuple(y.shape) != (n, features) or not y.is_contiguous():
+        raise TypeError(f"y must be a contiguous bf16 or fp16 tensor [{n}, {features}]")
+    return y
+
+
+def regenvc_mxfp4_project(x_packed, w_packed, n_tokens: int, out_features: int, in_features: int, bias=None, *,
+                          y_dtype=torch.bfloat16, y=None, stream=None):
+    """y [n_tokens, out_features] = x w^T + bias on packed 4-bit x [n_tokens, in_features] and w [out_features,
+    in_features]; bias fp32 [out_features] or None."""
+    _mx_packed(x_packed, "x_packed", n_tokens, in_features)
+    _mx_packed(w_packed, "w_packed", out_features, in_features)
+    _vector(bias, "bias", out_features)
+    _on_current_device(x_packed, w_packed, bias, y)
+    y = _mx_result(y, y_dtype, n_tokens, out_features, x_packed.device, stream)
+    _check(lib().regenvc_mxfp4_project(x_packed.data_ptr(), w_packed.data_ptr(), _addr(bias), y.data_ptr(), TYPES[y.dtype],
+                                       n_tokens, out_features, in_features, _stream(stream)))
+    return y
+
+
+def regenvc_mxfp4_linear(x, w_packed, out_features: int, bias=None, *, y_dtype=torch.bfloat16, y=None, scratch=None,
+                         stream=None):
+    """y [tokens, out_features] = Q(x) w^T + bias: x [tokens, in_features] (bf16, fp16 or fp32) is taken to 4 bits in the
+    call, w is packed (regenvc_mxfp4_quantize).  ``scratch``: uint8, regenvc_mxfp4_bytes(tokens, in_features)."""
+    _mx_values(x, "x")
+    n, cols = x.shape
+    _mx_packed(w_packed, "w_packed", out_features, cols)
+    _vector(bias, "bias", out_features)
+    _on_current_device(x, w_packed, bias, y, scratch)
+    y = _mx_result(y, y_dtype, n, out_features, x.device, stream)
+    if scratch is None:
+        scratch = _new((regenvc_mxfp4_bytes(n, cols),), torch.uint8, x.device, stream)
+    _mx_packed(scratch, "scratch", n, cols)
+    _check(lib().regenvc_mxfp4_linear(x.data_ptr(), TYPES[x.dtype], _row_stride(x), w_packed.data_ptr(), _addr(bias),
+                                      y.data_ptr(), TYPES[y.dtype], n, out_features, cols, scratch.data_ptr(),
+                                      _stream(stream)))
     return y
 
 

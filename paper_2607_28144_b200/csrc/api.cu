@@ -12,6 +12,7 @@
 
 #include "../../include/regenvc_attn.h"
 #include "common.cuh"
+#include "mxfp4.cuh"
 
 
 namespace {
@@ -129,6 +130,7 @@ int device_state(int* dev_out, DeviceState** st_out) {
             CUDA_TRY(configure_qkv_project_pair());
             CUDA_TRY(configure_out_project());
             CUDA_TRY(configure_attn_persistent());
+            CUDA_TRY(configure_mxfp4_project());
             CUDA_TRY(cudaMalloc(&st.status, sizeof(int)));
             CUDA_TRY(cudaMemset(st.status, 0, sizeof(int)));
         }
@@ -505,6 +507,28 @@ int check_self_args(int T, int H, int W, float theta, long long* n_out) {
 namespace regenvc {
 void count_launch() { launched(); }
 int record_cuda_failure(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+int op_device(int* sm_count, int** status) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    int dev = 0;
+    DeviceState* st = nullptr;
+    const int rc = device_state(&dev, &st);
+    if (rc != REGENVC_OK) return rc;
+    *sm_count = st->sm_count;
+    *status = st->status;
+    return REGENVC_OK;
+}
+int encode_map(CUtensorMap* m, CUtensorMapDataType type, void* base, uint64_t inner, uint64_t outer, uint64_t row_bytes,
+               uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swizzle) {
+    const cuuint64_t gdim[2] = {inner, outer};
+    const cuuint64_t gstride[1] = {row_bytes};
+    const cuuint32_t box[2] = {box_inner, box_outer};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = g_encode(m, type, 2, base, gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return REGENVC_OK;
+    tl_cuda_error = "cuTensorMapEncodeTiled failed with CUresult " + std::to_string((int)r);
+    return REGENVC_ERR_CUDA;
+}
 }  // namespace regenvc
 
 extern "C" {
