@@ -116,14 +116,14 @@ __device__ __forceinline__ BlockSum block_sum_init(float (*buf)[2][32]) {
 }
 
 // v -> normalised v (dead columns hold and keep 0); returns the reciprocal deviation.
-__device__ __forceinline__ float normalise(float* v, int kind, float eps, float inv_c, unsigned live, bool vec, BlockSum& sum) {
+__device__ __forceinline__ float normalise(float* v, int kind, float eps, float channels, unsigned live, bool vec, BlockSum& sum) {
     float s[1];
     if (kind == kNormLayer) {
         s[0] = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] += v[i];
         sum.run<1>(s);
-        const float mean = s[0] * inv_c;
+        const float mean = s[0] / channels;   // (a product with 1 / channels would leave a constant row a mean off by an ulp)
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (vec ? live != 0 : (live >> i & 1) != 0) ? v[i] - mean : 0.0f;
     }
@@ -131,7 +131,7 @@ __device__ __forceinline__ float normalise(float* v, int kind, float eps, float 
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[0] = fmaf(v[i], v[i], s[0]);
     sum.run<1>(s);
-    const float r = rsqrtf(fmaf(s[0], inv_c, eps));
+    const float r = rsqrtf(s[0] / channels + eps);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= r;
     return r;
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_forward_kernel(const BlockNor
     BlockSum sum = block_sum_init(buf);
     int c0, step;
     const unsigned live = live_columns(p.channels, VEC, &c0, &step);
-    const float inv_c = 1.0f / (float)p.channels;
+    const float channels = (float)p.channels;
     const int row0 = blockIdx.x * p.rows_per_cta;
     const int row1 = min(p.n_tokens, row0 + p.rows_per_cta);
     int mod = -1, mod_end = row0;   // modulation row held in registers, and its first token behind
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_forward_kernel(const BlockNor
             for (int i = 0; i < 8; ++i) g[i] *= t[i];
         }
         if (p.y) {
-            if (p.post_norm) normalise(z, p.post_norm, p.post_eps, inv_c, live, VEC, sum);
+            if (p.post_norm) normalise(z, p.post_norm, p.post_eps, channels, live, VEC, sum);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = fmaf(g[i], z[i], p.residual_scale * v[i]);
             if (p.x_out) Cols<TX, VEC>::store(p.x_out, row, p.x_out_stride, c0, step, live, v);
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_forward_kernel(const BlockNor
             for (int i = 0; i < 8; ++i) v[i] = (VEC ? live != 0 : (live >> i & 1) != 0) ? v[i] : 0.0f;
         }
         if (p.norm) {   // on x' before its rounding to the residual stream's type
-            normalise(v, p.norm, p.eps, inv_c, live, VEC, sum);
+            normalise(v, p.norm, p.eps, channels, live, VEC, sum);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], w[i], b[i]);
             Cols<TIO, VEC>::store(p.h, row, p.h_stride, c0, step, live, v);
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
     BlockSum sum = block_sum_init(buf);
     int c0, step;
     const unsigned live = live_columns(p.channels, VEC, &c0, &step);
-    const float inv_c = 1.0f / (float)p.channels;
+    const float channels = (float)p.channels;
     const int row0 = blockIdx.x * p.rows_per_cta;
     const int row1 = min(p.n_tokens, row0 + p.rows_per_cta);
     const int first_mod = row0 / p.tokens_per_mod;
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
                 float t[2] = {0.0f, 0.0f};
                 rx.widen(xh, live);
                 rdh.widen(d, live);
-                const float r = normalise(xh, p.norm, p.eps, inv_c, live, VEC, sum);
+                const float r = normalise(xh, p.norm, p.eps, channels, live, VEC, sum);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     s0[i] += d[i];
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
                     t[1] = fmaf(d[i], xh[i], t[1]);
                 }
                 sum.run<2>(t);
-                const float m0 = p.norm == kNormLayer ? t[0] * inv_c : 0.0f, m1 = t[1] * inv_c;
+                const float m0 = p.norm == kNormLayer ? t[0] / channels : 0.0f, m1 = t[1] / channels;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] = r * (d[i] - fmaf(xh[i], m1, m0));
             } else {
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
                 float yh[8];
                 ry.widen(yh, live);
                 float r = 1.0f;
-                if (p.post_norm) r = normalise(yh, p.post_norm, p.post_eps, inv_c, live, VEC, sum);
+                if (p.post_norm) r = normalise(yh, p.post_norm, p.post_eps, channels, live, VEC, sum);
                 float t[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
                 }
                 if (p.post_norm) {
                     sum.run<2>(t);
-                    const float m0 = p.post_norm == kNormLayer ? t[0] * inv_c : 0.0f, m1 = t[1] * inv_c;
+                    const float m0 = p.post_norm == kNormLayer ? t[0] / channels : 0.0f, m1 = t[1] / channels;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) d[i] = r * (d[i] - fmaf(yh[i], m1, m0));
                 }

@@ -252,6 +252,7 @@ int regenvc_block_norm_backward(const regenvc_block_norm_desc* desc, const void*
     rc = norm_memory(&a, ins, in_size, 9, outs, out_size, 9, in_place);
     if (rc != REGENVC_OK) return rc;
     p.x = x_out;
+    p.x_stride = p.x_out_stride;   // the kernel's x is the saved x'
     p.y = y;
     p.gate = reinterpret_cast<const float*>(gate);
     p.post_weight = reinterpret_cast<const float*>(post_weight);
