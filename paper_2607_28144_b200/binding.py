@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -32,7 +33,7 @@ EXPORTS = [
     "regenvc_ulysses_scatter_heads", "regenvc_ulysses_gather_heads", "regenvc_debug_expire_wait",
     "regenvc_block_norm_forward", "regenvc_block_norm_backward", "regenvc_block_norm_workspace_bytes",
     "regenvc_rope_axes", "regenvc_mxfp4_bytes", "regenvc_mxfp4_quantize", "regenvc_mxfp4_dequantize",
-    "regenvc_mxfp4_project", "regenvc_mxfp4_linear",
+    "regenvc_mxfp4_project", "regenvc_mxfp4_linear", "regenvc_mxfp4_linear_scratch_bytes",
 ]
 
 
@@ -106,16 +107,18 @@ def lib() -> ctypes.CDLL:
     L.regenvc_out_project.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
     L.regenvc_out_project.restype = i32
     i64 = ctypes.c_longlong
-    L.regenvc_block_norm_forward.argtypes = [ctypes.POINTER(BlockNormDesc)] + [vp] * 11
+    L.regenvc_block_norm_forward.argtypes = [vp] * 12
     L.regenvc_block_norm_forward.restype = i32
     L.regenvc_block_norm_workspace_bytes.argtypes = [i32, i32]
     L.regenvc_block_norm_workspace_bytes.restype = sz
-    L.regenvc_block_norm_backward.argtypes = [ctypes.POINTER(BlockNormDesc)] + [vp] * 18 + [sz, vp]
+    L.regenvc_block_norm_backward.argtypes = [vp] * 19 + [sz, vp]
     L.regenvc_block_norm_backward.restype = i32
-    L.regenvc_rope_axes.argtypes = [ctypes.POINTER(RopeAxesDesc)] + [vp] * 6
+    L.regenvc_rope_axes.argtypes = [vp] * 7
     L.regenvc_rope_axes.restype = i32
     L.regenvc_mxfp4_bytes.argtypes = [i32, i32]
     L.regenvc_mxfp4_bytes.restype = sz
+    L.regenvc_mxfp4_linear_scratch_bytes.argtypes = [i32, i32]
+    L.regenvc_mxfp4_linear_scratch_bytes.restype = sz
     L.regenvc_mxfp4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp]
     L.regenvc_mxfp4_quantize.restype = i32
     L.regenvc_mxfp4_dequantize.argtypes = [vp, vp, i32, i32, i32, i64, vp]
@@ -304,6 +307,10 @@ def regenvc_out_project(attn_out, w_o, b_o, y=None, stream=None):
 
 
 # ---------------------------------------------------------------------------- steps around the attention of a block
+_NORM_DESC, _ROPE_DESC = struct.Struct("@7i3f8q"), struct.Struct("@10if4i9q")   # the fields of the two descriptions
+assert _NORM_DESC.size == ctypes.sizeof(BlockNormDesc) and _ROPE_DESC.size == ctypes.sizeof(RopeAxesDesc)
+
+
 def _addr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -318,54 +325,66 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _on_current_device(first, *others):
-    """All operands on the device the library launches on (the current one)."""
+def _place(first, *others) -> int:
+    """All operands on the device the library launches on (the current one); returns its index."""
     if not first.is_cuda:
         raise TypeError("expected CUDA tensors")
-    dev = first.device
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"operands are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    index = first.get_device()
+    if index != torch.cuda.current_device():
+        raise ValueError(f"operands are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
     for t in others:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != index:
             raise ValueError("operands are on different devices")
+    return index
 
 
-def _rows(t, name: str, dtype, shape):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise TypeError(f"{name} must be {dtype} {list(shape)} with neighbouring columns")
-    _row_stride(t, name)
+def _launch_stream(stream, index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+
+
+def _rows(t, name: str, dtype, n: int, c: int) -> int:
+    """Checks a matrix and returns the elements between its rows as the library takes them (0: packed)."""
+    if t.dtype is not dtype or t.shape != (n, c):
+        raise TypeError(f"{name} must be {dtype} [{n}, {c}]")
+    return _row_stride(t, name)
 
 
 def _row_stride(t, name: str = "the tensor") -> int:
     """Elements between rows as the library takes them (0: packed); rows that share memory are refused here, since an
     expanded tensor's stride of 0 would read as "packed"."""
-    if t is None or t.shape[0] < 2:
+    if t is None:
         return 0
-    if t.stride(0) < t.shape[1]:
+    rows, cols = t.shape
+    between, step = t.stride()
+    if step != 1 and cols > 1:
+        raise TypeError(f"{name} must have neighbouring columns")
+    if rows < 2:
+        return 0
+    if between < cols:
         raise ValueError(f"{name} has rows that overlap (an expanded tensor?)")
-    return t.stride(0)
+    return between
 
 
 def _vector(t, name: str, size: int):
-    if t is not None and (t.dtype != torch.float32 or t.numel() != size or not t.is_contiguous()):
+    if t is not None and (t.dtype is not torch.float32 or t.numel() != size or not t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous fp32 tensor of {size} elements (or None)")
 
 
-def _modulation(n: int, c: int, tokens_per_mod, tensors):
+def _modulation(n: int, c: int, tokens_per_mod, gate, scale, shift):
     """Checks the modulation tables and returns (tokens_per_mod, rows, row stride)."""
     per = n if tokens_per_mod is None else int(tokens_per_mod)
     if per < 1:
         raise ValueError("tokens_per_mod must be at least 1")
+    per = min(per, n)
     rows = -(-n // per)
-    strides = set()
-    for t, name in tensors:
+    stride = 0
+    for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
         if t is not None:
-            _rows(t, name, torch.float32, (rows, c))
-            if rows > 1:
-                strides.add(t.stride(0))
-    if len(strides) > 1:
-        raise ValueError("gate, scale and shift must have the same distance between rows")
-    return per, rows, strides.pop() if strides else 0
+            s = _rows(t, name, torch.float32, rows, c)
+            if stride and s != stride:
+                raise ValueError("gate, scale and shift must have the same distance between rows")
+            stride = s
+    return per, rows, stride
 
 
 def regenvc_block_norm_forward(x, y=None, *, gate=None, post_norm: int = NORM_NONE, post_weight=None,
@@ -379,36 +398,35 @@ def regenvc_block_norm_forward(x, y=None, *, gate=None, post_norm: int = NORM_NO
     ``x_out`` (in place)."""
     if x.dim() != 2 or x.dtype not in TYPES:
         raise TypeError("x must be [tokens, C] in bf16, fp16 or fp32")
-    _on_current_device(x, y, gate, post_weight, weight, bias, scale, shift, x_out, h)
+    index = _place(x, y, gate, post_weight, weight, bias, scale, shift, x_out, h)
     n, c = x.shape
     io = h.dtype if h is not None else h_dtype or (y.dtype if y is not None else x.dtype)
     if io not in TYPES:
         raise TypeError("h must be bf16, fp16 or fp32")
-    _rows(x, "x", x.dtype, (n, c))
-    if y is not None:
-        _rows(y, "y", io, (n, c))
-    for t, name in ((post_weight, "post_weight"), (weight, "weight"), (bias, "bias")):
-        _vector(t, name, c)
-    per, _, mod_stride = _modulation(n, c, tokens_per_mod, ((gate, "gate"), (scale, "scale"), (shift, "shift")))
-    if y is None:
-        if x_out is not None:
-            raise ValueError("x_out needs y")
-    elif x_out is None:
-        x_out = _new((n, c), x.dtype, x.device, stream)
-    if norm == NORM_NONE:
-        if h is not None:
-            raise ValueError("h needs a norm")
-    elif h is None:
-        h = _new((n, c), io, x.device, stream)
+    x_stride = _row_stride(x, "x")
+    y_stride = 0 if y is None else _rows(y, "y", io, n, c)
+    _vector(post_weight, "post_weight", c)
+    _vector(weight, "weight", c)
+    _vector(bias, "bias", c)
+    per, _, mod_stride = _modulation(n, c, tokens_per_mod, gate, scale, shift)
+    x_out_stride = h_stride = 0
     if x_out is not None:
-        _rows(x_out, "x_out", x.dtype, (n, c))
+        if y is None:
+            raise ValueError("x_out needs y")
+        x_out_stride = _rows(x_out, "x_out", x.dtype, n, c)
+    elif y is not None:
+        x_out = _new((n, c), x.dtype, x.device, stream)
     if h is not None:
-        _rows(h, "h", io, (n, c))
-    d = BlockNormDesc(n, c, min(per, 2**31 - 1), TYPES[x.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
-                      mod_stride, _row_stride(x), _row_stride(y), _row_stride(x_out), _row_stride(h))
-    _check(lib().regenvc_block_norm_forward(ctypes.byref(d), x.data_ptr(), _addr(y), _addr(gate), _addr(post_weight),
-                                            _addr(weight), _addr(bias), _addr(scale), _addr(shift), _addr(x_out), _addr(h),
-                                            _stream(stream)))
+        if norm == NORM_NONE:
+            raise ValueError("h needs a norm")
+        h_stride = _rows(h, "h", io, n, c)
+    elif norm != NORM_NONE:
+        h = _new((n, c), io, x.device, stream)
+    d = _NORM_DESC.pack(n, c, per, TYPES[x.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
+                        mod_stride, x_stride, y_stride, x_out_stride, h_stride, 0, 0, 0)
+    _check(lib().regenvc_block_norm_forward(d, x.data_ptr(), _addr(y), _addr(gate), _addr(post_weight), _addr(weight),
+                                            _addr(bias), _addr(scale), _addr(shift), _addr(x_out), _addr(h),
+                                            _launch_stream(stream, index)))
     return x_out, h
 
 
@@ -427,20 +445,21 @@ def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, po
     like = x_out if x_out is not None else dx_out
     if like is None or like.dim() != 2 or like.dtype not in TYPES:
         raise TypeError("x_out must be [tokens, C] in bf16, fp16 or fp32")
-    _on_current_device(like, x_out, dh, dx_out, y, gate, post_weight, weight, bias, scale, shift, dx, workspace)
+    index = _place(like, x_out, dh, dx_out, y, gate, post_weight, weight, bias, scale, shift, dx, workspace)
     n, c = like.shape
     io = dh.dtype if dh is not None else (y.dtype if y is not None else like.dtype)
     if io not in TYPES:
         raise TypeError("dh must be bf16, fp16 or fp32")
-    for t, name, dtype in ((x_out, "x_out", like.dtype), (dh, "dh", io), (dx_out, "dx_out", like.dtype), (y, "y", io)):
-        if t is not None:
-            _rows(t, name, dtype, (n, c))
+    strides = [0 if t is None else _rows(t, name, dtype, n, c) for t, name, dtype in
+               ((y, "y", io), (x_out, "x_out", like.dtype), (dh, "dh", io), (dx_out, "dx_out", like.dtype))]
     for t, name in ((post_weight, "post_weight"), (weight, "weight"), (bias, "bias")):
         _vector(t, name, c)
-    per, rows, mod_stride = _modulation(n, c, tokens_per_mod, ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+    per, rows, mod_stride = _modulation(n, c, tokens_per_mod, gate, scale, shift)
     new = lambda shape, dtype: _new(shape, dtype, like.device, stream)  # noqa: E731
-    dx = new((n, c), like.dtype) if dx is None else dx
-    _rows(dx, "dx", like.dtype, (n, c))
+    if dx is None:
+        dx, dx_stride = new((n, c), like.dtype), 0
+    else:
+        dx_stride = _rows(dx, "dx", like.dtype, n, c)
     f32 = torch.float32
     g = {"dx": dx, "dy": None if y is None else new((n, c), io)}
     for t, name in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")):
@@ -450,14 +469,13 @@ def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, po
     need = regenvc_block_norm_workspace_bytes(n, c)
     if workspace is None:
         workspace = new((need,), torch.uint8)
-    d = BlockNormDesc(n, c, min(per, 2**31 - 1), TYPES[like.dtype], TYPES[io], norm, post_norm, eps, post_eps,
-                      residual_scale, mod_stride, 0, _row_stride(y), _row_stride(x_out), _row_stride(dh),
-                      _row_stride(dx_out), _row_stride(dx), 0)
+    d = _NORM_DESC.pack(n, c, per, TYPES[like.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
+                        mod_stride, 0, *strides, dx_stride, 0)
     _check(lib().regenvc_block_norm_backward(
-        ctypes.byref(d), _addr(x_out), _addr(y), _addr(gate), _addr(post_weight), _addr(weight), _addr(bias), _addr(scale),
+        d, _addr(x_out), _addr(y), _addr(gate), _addr(post_weight), _addr(weight), _addr(bias), _addr(scale),
         _addr(dh), _addr(dx_out), dx.data_ptr(), _addr(g["dy"]), _addr(g["dgate"]), _addr(g["dpost_weight"]),
         _addr(g["dweight"]), _addr(g["dbias"]), _addr(g["dscale"]), _addr(g["dshift"]), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        workspace.numel() * workspace.element_size(), _launch_stream(stream, index)))
     return g
 
 
@@ -469,7 +487,7 @@ def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, h
     gradient."""
     if q.dim() != 3 or q.dtype not in TYPES:
         raise TypeError("q must be [tokens, heads, head_dim] in bf16, fp16 or fp32")
-    _on_current_device(q, k, positions, q_out, k_out)
+    index = _place(q, k, positions, q_out, k_out)
     n, hq, d = q.shape
     widths = [int(w) for w in widths]
     if positions.dtype not in (torch.int32, torch.float32) or tuple(positions.shape) != (len(widths), n) or \
@@ -479,7 +497,7 @@ def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, h
         raise TypeError("k must be [tokens, heads, head_dim] of q's type")
     if k is None and k_out is not None:
         raise ValueError("k_out needs k")
-    if len(widths) > 4:
+    if not 1 <= len(widths) <= 4:
         raise RegenvcError(ERR_BAD_SHAPE, status_string(ERR_BAD_SHAPE))
     if q_out is None:
         q_out = _new(q.shape, q.dtype, q.device, stream)
@@ -498,11 +516,11 @@ def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, h
         # the stride of an axis with one entry is never used: name the packed one
         head = t.stride(1) if t.shape[1] > 1 else d
         strides += [t.stride(0) if n > 1 else max(t.shape[1] * head, d), head]
-    desc = RopeAxesDesc(n, hq, hk, d, TYPES[q.dtype], len(widths), (ctypes.c_int * 4)(*widths), float(rope_theta), int(halves),
-                        int(whole_ladder), int(positions.dtype == torch.float32), int(inverse),
-                        positions.stride(0) if len(widths) > 1 else 0, *strides)
-    _check(lib().regenvc_rope_axes(ctypes.byref(desc), q.data_ptr(), _addr(k), positions.data_ptr(), q_out.data_ptr(),
-                                   _addr(k_out), _stream(stream)))
+    desc = _ROPE_DESC.pack(n, hq, hk, d, TYPES[q.dtype], len(widths), *(widths + [0, 0, 0])[:4], rope_theta, bool(halves),
+                           bool(whole_ladder), positions.dtype is torch.float32, bool(inverse),
+                           positions.stride(0) if len(widths) > 1 else 0, *strides)
+    _check(lib().regenvc_rope_axes(desc, q.data_ptr(), _addr(k), positions.data_ptr(), q_out.data_ptr(),
+                                   _addr(k_out), _launch_stream(stream, index)))
     return q_out, k_out
 
 
@@ -510,49 +528,63 @@ def regenvc_mxfp4_bytes(rows: int, cols: int) -> int:
     return int(lib().regenvc_mxfp4_bytes(rows, cols))
 
 
+def _mx_bytes(rows: int, cols: int) -> int:
+    """regenvc_mxfp4_bytes() without the call, for sizes the library then checks itself."""
+    blocks = -(-cols // 128)
+    return -(-rows * blocks // 8) * 512 + -(-rows // 128) * blocks * 512
+
+
 def _mx_packed(t, name: str, rows: int, cols: int):
-    need = regenvc_mxfp4_bytes(rows, cols)
-    if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < need or need == 0:
+    need = _mx_bytes(rows, cols)
+    if t.dtype is not torch.uint8 or t.numel() < need or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous uint8 tensor of at least {need} bytes")
 
 
-def _mx_values(t, name: str):
-    if t.dim() != 2 or t.dtype not in TYPES or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TypeError(f"{name} must be [rows, cols] in bf16, fp16 or fp32 with neighbouring columns")
+def _mx_values(t, name: str) -> int:
+    if t.dim() != 2 or t.dtype not in TYPES:
+        raise TypeError(f"{name} must be [rows, cols] in bf16, fp16 or fp32")
+    return _row_stride(t, name)
 
 
 def regenvc_mxfp4_quantize(src, packed=None, stream=None):
     """Rows of bf16, fp16 or fp32 [rows, cols] to microscaled 4-bit form; returns the ``packed`` uint8 tensor."""
-    _mx_values(src, "src")
-    _on_current_device(src, packed)
+    stride = _mx_values(src, "src")
+    index = _place(src, packed)
     rows, cols = src.shape
     if packed is None:
-        packed = _new((regenvc_mxfp4_bytes(rows, cols),), torch.uint8, src.device, stream)
-    _mx_packed(packed, "packed", rows, cols)
-    _check(lib().regenvc_mxfp4_quantize(src.data_ptr(), TYPES[src.dtype], rows, cols, _row_stride(src), packed.data_ptr(),
-                                        _stream(stream)))
+        packed = _new((_mx_bytes(rows, cols),), torch.uint8, src.device, stream)
+    else:
+        _mx_packed(packed, "packed", rows, cols)
+    _check(lib().regenvc_mxfp4_quantize(src.data_ptr(), TYPES[src.dtype], rows, cols, stride, packed.data_ptr(),
+                                        _launch_stream(stream, index)))
     return packed
 
 
 def regenvc_mxfp4_dequantize(packed, rows: int, cols: int, dtype=torch.bfloat16, out=None, stream=None):
     """The [rows, cols] values that a packed matrix stands for."""
     _mx_packed(packed, "packed", rows, cols)
-    _on_current_device(packed, out)
+    index = _place(packed, out)
     if out is None:
         out = _new((rows, cols), dtype, packed.device, stream)
-    _mx_values(out, "out")
-    if tuple(out.shape) != (rows, cols):
+    stride = _mx_values(out, "out")
+    if out.shape != (rows, cols):
         raise TypeError(f"out must be [{rows}, {cols}]")
-    _check(lib().regenvc_mxfp4_dequantize(packed.data_ptr(), out.data_ptr(), TYPES[out.dtype], rows, cols, _row_stride(out),
-                                          _stream(stream)))
+    _check(lib().regenvc_mxfp4_dequantize(packed.data_ptr(), out.data_ptr(), TYPES[out.dtype], rows, cols, stride,
+                                          _launch_stream(stream, index)))
     return out
 
 
+def regenvc_mxfp4_linear_scratch_bytes(n_tokens: int, in_features: int) -> int:
+    return int(lib().regenvc_mxfp4_linear_scratch_bytes(n_tokens, in_features))
+
+
 def _mx_result(y, y_dtype, n: int, features: int, device, stream):
+    if (y_dtype if y is None else y.dtype) not in (torch.bfloat16, torch.float16):
+        raise TypeError("y must be bf16 or fp16")
     if y is None:
-        y = _new((n, features), y_dtype, device, stream)
-    if y.dtype not in (torch.bfloat16, torch.float16) or tuple(y.shape) != (n, features) or not y.is_contiguous():
-        raise TypeError(f"y must be a contiguous bf16 or fp16 tensor [{n}, {features}]")
+        return _new((n, features), y_dtype, device, stream)
+    if y.shape != (n, features) or not y.is_contiguous():
+        raise TypeError(f"y must be a contiguous tensor [{n}, {features}]")
     return y
 
 
@@ -563,29 +595,31 @@ def regenvc_mxfp4_project(x_packed, w_packed, n_tokens: int, out_features: int, 
     _mx_packed(x_packed, "x_packed", n_tokens, in_features)
     _mx_packed(w_packed, "w_packed", out_features, in_features)
     _vector(bias, "bias", out_features)
-    _on_current_device(x_packed, w_packed, bias, y)
+    index = _place(x_packed, w_packed, bias, y)
     y = _mx_result(y, y_dtype, n_tokens, out_features, x_packed.device, stream)
     _check(lib().regenvc_mxfp4_project(x_packed.data_ptr(), w_packed.data_ptr(), _addr(bias), y.data_ptr(), TYPES[y.dtype],
-                                       n_tokens, out_features, in_features, _stream(stream)))
+                                       n_tokens, out_features, in_features, _launch_stream(stream, index)))
     return y
 
 
 def regenvc_mxfp4_linear(x, w_packed, out_features: int, bias=None, *, y_dtype=torch.bfloat16, y=None, scratch=None,
                          stream=None):
     """y [tokens, out_features] = Q(x) w^T + bias: x [tokens, in_features] (bf16, fp16 or fp32) is taken to 4 bits in the
-    call, w is packed (regenvc_mxfp4_quantize).  ``scratch``: uint8, regenvc_mxfp4_bytes(tokens, in_features)."""
-    _mx_values(x, "x")
+    call, w is packed (regenvc_mxfp4_quantize).  ``scratch``: uint8, regenvc_mxfp4_linear_scratch_bytes() long."""
+    stride = _mx_values(x, "x")
     n, cols = x.shape
     _mx_packed(w_packed, "w_packed", out_features, cols)
     _vector(bias, "bias", out_features)
-    _on_current_device(x, w_packed, bias, y, scratch)
+    index = _place(x, w_packed, bias, y, scratch)
     y = _mx_result(y, y_dtype, n, out_features, x.device, stream)
-    if scratch is None:
-        scratch = _new((regenvc_mxfp4_bytes(n, cols),), torch.uint8, x.device, stream)
-    _mx_packed(scratch, "scratch", n, cols)
-    _check(lib().regenvc_mxfp4_linear(x.data_ptr(), TYPES[x.dtype], _row_stride(x), w_packed.data_ptr(), _addr(bias),
-                                      y.data_ptr(), TYPES[y.dtype], n, out_features, cols, scratch.data_ptr(),
-                                      _stream(stream)))
+    need = regenvc_mxfp4_linear_scratch_bytes(n, cols)
+    if scratch is None and need:
+        scratch = _new((need,), torch.uint8, x.device, stream)
+    if scratch is not None and (scratch.dtype != torch.uint8 or not scratch.is_contiguous() or scratch.numel() < need):
+        raise TypeError(f"scratch must be a contiguous uint8 tensor of at least {need} bytes")
+    _check(lib().regenvc_mxfp4_linear(x.data_ptr(), TYPES[x.dtype], stride, w_packed.data_ptr(), _addr(bias),
+                                      y.data_ptr(), TYPES[y.dtype], n, out_features, cols, _addr(scratch),
+                                      _launch_stream(stream, index)))
     return y
 
 

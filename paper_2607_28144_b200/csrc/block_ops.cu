@@ -170,6 +170,29 @@ int mx_project(const void* x, const void* w, const void* bias, void* y, int y_ty
     return launch_done(e, "launch of the 4-bit product", e == cudaSuccess ? 1 : 0);
 }
 
+// Few tokens: one launch, from x itself (type) or from its packed form (x_stride < 0).
+int mx_rows(const void* x, int type, long long x_stride, const void* w, const void* bias, void* y, int y_type, int n,
+            int features, int cols, int sm_count, cudaStream_t stream) {
+    const MxLayout lx(n, cols), lw(features, cols);
+    const bool packed = x_stride < 0;
+    MxRowsParams p{};
+    p.x = x;
+    p.x_stride = x_stride ? x_stride : cols;
+    p.w = reinterpret_cast<const uint8_t*>(w);
+    p.bias = reinterpret_cast<const float*>(bias);
+    p.y = y;
+    p.cols_pad = lx.cols_pad;
+    p.x_scale_at = lx.scale_at;
+    p.w_scale_at = lw.scale_at;
+    p.n_tokens = n;
+    p.features = features;
+    p.cols = cols;
+    p.vec = !packed && aligned(x, 16) && p.x_stride % 8 == 0;
+    p.y_f16 = y_type == REGENVC_F16;
+    const cudaError_t e = launch_mxfp4_rows(p, type, packed, sm_count, stream);
+    return launch_done(e, "launch of the 4-bit product of a few rows", e == cudaSuccess ? 1 : 0);
+}
+
 }  // namespace
 
 extern "C" {
@@ -401,26 +424,40 @@ int regenvc_mxfp4_project(const void* x_packed, const void* w_packed, const void
     int sm_count = 0, *status = nullptr;
     rc = op_device(&sm_count, &status);
     if (rc != REGENVC_OK) return rc;
+    if (mxfp4_rows_fits(n_tokens, MxLayout(n_tokens, in_features).cols_pad))
+        return mx_rows(x_packed, REGENVC_BF16, -1, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count,
+                       (cudaStream_t)stream);
     return mx_project(x_packed, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count, status,
                       (cudaStream_t)stream);
 }
 
+size_t regenvc_mxfp4_linear_scratch_bytes(int n_tokens, int in_features) {
+    if (!mx_shape_ok(n_tokens, in_features)) return 0;
+    const MxLayout l(n_tokens, in_features);
+    return mxfp4_rows_fits(n_tokens, l.cols_pad) ? 0 : (size_t)l.bytes;
+}
+
 int regenvc_mxfp4_linear(const void* x, int x_type, long long x_stride, const void* w_packed, const void* bias, void* y,
                          int y_type, int n_tokens, int out_features, int in_features, void* scratch, void* stream) {
-    if (!x || !scratch) return REGENVC_ERR_NULL_POINTER;
+    if (!x) return REGENVC_ERR_NULL_POINTER;
     int rc = mx_project_checks(w_packed, bias, y, y_type, n_tokens, out_features, in_features);
     if (rc != REGENVC_OK) return rc;
     if (!type_ok(x_type)) return REGENVC_ERR_UNSUPPORTED;
     if (x_stride != 0 && (x_stride < in_features || x_stride > kMaxStride)) return REGENVC_ERR_BAD_SHAPE;
-    if (!aligned(x, type_size(x_type)) || !aligned(scratch, 256)) return REGENVC_ERR_MISALIGNED;
+    const bool few = mxfp4_rows_fits(n_tokens, MxLayout(n_tokens, in_features).cols_pad);
+    if (!few && !scratch) return REGENVC_ERR_NULL_POINTER;
+    if (!aligned(x, type_size(x_type)) || (!few && !aligned(scratch, 256))) return REGENVC_ERR_MISALIGNED;
     const Span xs = rows_span(x, n_tokens, x_stride ? x_stride : in_features, in_features, type_size(x_type));
-    const Span ss{scratch, (size_t)MxLayout(n_tokens, in_features).bytes};
+    const Span ss{few ? nullptr : scratch, (size_t)MxLayout(n_tokens, in_features).bytes};
     const Span ys{y, (size_t)n_tokens * out_features * 2}, ws{w_packed, (size_t)MxLayout(out_features, in_features).bytes};
     if (meet(ys, xs) || meet(ys, ss) || meet(ss, xs) || meet(ss, ws) || meet(ss, Span{bias, (size_t)out_features * 4}))
         return REGENVC_ERR_ALIASING;
     int sm_count = 0, *status = nullptr;
     rc = op_device(&sm_count, &status);
     if (rc != REGENVC_OK) return rc;
+    if (few)
+        return mx_rows(x, x_type, x_stride, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count,
+                       (cudaStream_t)stream);
     rc = mx_convert(x, x_type, n_tokens, in_features, x_stride, scratch, true, (cudaStream_t)stream);
     if (rc != REGENVC_OK) return rc;
     return mx_project(scratch, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count, status,

@@ -52,4 +52,20 @@ cudaError_t launch_mxfp4_project(const MxProjectPlan& plan, const CUtensorMap& x
                                  const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, int sm_count,
                                  cudaStream_t stream);
 
+// The product for a few tokens (mxfp4_rows.cu), from x of any type or packed.
+constexpr int kMxFewRows = 4;
+struct MxRowsParams {
+    const void* x;
+    long long x_stride;       // elements between rows (not packed)
+    const uint8_t* w;         // packed
+    const float* bias;        // [features] or nullptr
+    void* y;                  // [n_tokens][features] 16-bit
+    long long cols_pad, x_scale_at, w_scale_at;
+    int n_tokens, features, cols;
+    int vec;                  // x's address and stride allow 16-byte accesses
+    int y_f16;
+};
+bool mxfp4_rows_fits(int n_tokens, long long cols_pad);
+cudaError_t launch_mxfp4_rows(const MxRowsParams& p, int type, bool packed, int sm_count, cudaStream_t stream);
+
 }  // namespace regenvc

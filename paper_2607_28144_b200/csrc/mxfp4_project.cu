@@ -324,9 +324,10 @@ cudaError_t launch_cfg(const CUtensorMap& x, const CUtensorMap& xs, const CUtens
 }  // namespace
 
 MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int sm_count) {
-    const long long tiles = (n_tokens + kTile - 1) / kTile;
-    // fewer wide items than SMs: narrow ones
-    if (tiles * ((features + 191) / 192) < sm_count) return MxProjectPlan{0, 64, 64};
+    const long long tiles = (n_tokens + kTile - 1) / kTile, wide = (features + 191) / 192;
+    // at least one item for every pair of CTAs: pairs; else single CTAs, on narrow items where wide ones leave SMs idle
+    if ((tiles + 1) / 2 * wide >= sm_count / 2) return MxProjectPlan{1, 192, 96};
+    if (tiles * wide < sm_count) return MxProjectPlan{0, 64, 64};
     return MxProjectPlan{0, 192, 192};
 }
 
@@ -334,12 +335,15 @@ cudaError_t configure_mxfp4_project() {
     cudaError_t e = cudaFuncSetAttribute(mxfp4_project_kernel<1, 192>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mx_smem<1, 192>());
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(mxfp4_project_kernel<1, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mx_smem<1, 64>());
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(mxfp4_project_kernel<2, 192>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mx_smem<2, 192>());
     return e;
 }
 
 cudaError_t launch_mxfp4_project(const MxProjectPlan& plan, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& w,
                                  const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, int sm_count,
                                  cudaStream_t stream) {
+    if (plan.pair) return launch_cfg<2, 192>(x, xs, w, ws, y, p, sm_count, stream);
     if (plan.tile_features == 64) return launch_cfg<1, 64>(x, xs, w, ws, y, p, sm_count, stream);
     return launch_cfg<1, 192>(x, xs, w, ws, y, p, sm_count, stream);
 }
