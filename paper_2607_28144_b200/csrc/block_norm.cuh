@@ -5,8 +5,8 @@
 
 namespace regenvc {
 
-constexpr int kNormMaxChannels = 8192;   // eight columns per thread, at most 1024 threads
-constexpr int kNormMaxCtas = 608;        // the grids never exceed this; it bounds the workspace of the backward pass
+constexpr int kNormMaxChannels = 8192;   // sixteen columns per thread, at most 512 threads
+constexpr int kNormMaxCtas = 608;        // the backward pass's grid never exceeds this: it bounds the workspace
 constexpr int kNormLayer = 1, kNormRms = 2;
 
 struct BlockNormParams {
