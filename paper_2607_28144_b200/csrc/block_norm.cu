@@ -43,8 +43,13 @@ __device__ __forceinline__ float join(f32x2 v) {
     return a + b;
 }
 
-__device__ __forceinline__ void copy_async16(uint32_t smem, const void* global) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory");
+// 16 bytes, or 16 zeros without a read where bytes is 0 (dead columns).
+__device__ __forceinline__ void copy_async16(uint32_t smem, const void* global, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(global), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void store16_if(bool on, void* p, uint4 v) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %0, 0;\n\t@q st.global.v4.b32 [%1], {%2, %3, %4, %5};\n\t}"
+                 ::"r"((uint32_t)on), "l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // Waits until at most `stages` - 1 of this thread's groups are under way.
@@ -82,69 +87,118 @@ struct Place {
     }
 };
 
-// Bytes of one thread's columns of a row, and those of a row in the ring.
+// Bytes of one thread's columns of a row of T.
 template <typename T>
 constexpr uint32_t kMine = kCols * sizeof(T);
 
-// One tensor's rows: through the ring (VEC) or straight from global memory.
-template <typename T, bool VEC>
+// One tensor's rows, taken in order.  VEC: copied ahead into this warp's part of a ring stage (16-byte words of
+// neighbouring lanes are neighbours in global and in shared memory: word w of a warp's data is lane w % 32's copy
+// number w / 32).  A 16-bit lane reads back its own words.  An fp32 group of eight columns is two words: lane l reads
+// words 2l and 2l + 1, which other lanes of its warp copied, so a warp synchronises behind its waits; the words of every
+// other eight are swapped in pairs, which keeps those reads off each other's banks.  Otherwise read straight from global
+// memory.
+template <typename T, bool VEC, uint32_t AT, int MAXT>
 struct Rows {
-    const T* base;
+    enum { kWords = (int)sizeof(T) / 2 };   // 16-byte words per lane and group
+    const T* next;        // VEC: this thread's first word of the row to fetch next; else its first column of the row to read
     long long stride;
-    uint32_t ring;        // this thread's place in stage 0 (VEC); stages are `stage_bytes` apart
-    __device__ __forceinline__ void fetch(const Place<VEC>& at, long long row, uint32_t stage) const {
+    uint32_t bytes;       // VEC: what each of the copies moves, a byte of this number for each (16, or 0 in dead columns)
+    __device__ __forceinline__ Rows(const void* base, long long row_stride, int row0, const Place<VEC>& at, int channels)
+        : next(nullptr), stride(row_stride), bytes(0) {
+        if (!base) return;
+        const T* row = reinterpret_cast<const T*>(base) + row0 * row_stride;
         if constexpr (VEC) {
-            const T* p = base + row * stride;
+            const int first = word_column(at, 0, 0);
+            next = row + (first < channels ? first : 0);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                if (at.on(8 * j))
 #pragma unroll
-                    for (int k = 0; k < (int)sizeof(T) / 2; ++k)   // 16-byte pieces of eight elements
-                        copy_async16(ring + stage + (j * (int)sizeof(T) / 2 + k) * at.threads * 16,
-                                     p + at.col(8 * j) + k * (16 / (int)sizeof(T)));
+                for (int k = 0; k < kWords; ++k)
+                    bytes |= (word_column(at, j, k) < channels ? 16u : 0u) << (j * kWords + k) * 8;
+        } else {
+            next = row + (at.on(0) ? at.col(0) : 0);
         }
     }
-    __device__ __forceinline__ void read(const Place<VEC>& at, long long row, uint32_t stage, f32x2* v) const {
+    // First column of the word that this lane copies as its k-th of group j.
+    static __device__ __forceinline__ int word_column(const Place<VEC>& at, int j, int k) {
+        return ((j * at.threads + (at.tid & ~31)) * kWords + k * 32 + (at.tid & 31)) * (16 / (int)sizeof(T));
+    }
+    static __device__ __forceinline__ uint32_t word_place(uint32_t w) { return kWords == 1 ? w : w ^ (w >> 3 & 1); }
+    // `stage`: the stage's address plus this warp's share, 16 bytes per lane (the part of group j, copy k is a constant on)
+    __device__ __forceinline__ void fetch(const Place<VEC>& at, uint32_t stage) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) {
+                    const uint32_t size = bytes >> (j * kWords + k) * 8 & 0xFFu;
+                    copy_async16(stage + AT * MAXT + j * (MAXT * kWords * 16) + (at.tid >> 5) * (kWords * 512) +
+                                     word_place(k * 32 + (at.tid & 31)) * 16,
+                                 next + (size ? j * at.threads * 8 + k * (32 * 16 / (int)sizeof(T)) : 0), size);
+                }
+            next += stride;
+        }
+    }
+    __device__ __forceinline__ void read(const Place<VEC>& at, uint32_t stage, f32x2* v) {
         if constexpr (VEC) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 Raw8<T> r;
 #pragma unroll
-                for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-                    const uint32_t a = ring + stage + (j * (int)sizeof(T) / 2 + k) * at.threads * 16;
+                for (int k = 0; k < kWords; ++k)
                     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(r.w[k].x), "=r"(r.w[k].y), "=r"(r.w[k].z), "=r"(r.w[k].w) : "r"(a) : "memory");
-                }
+                                 : "=r"(r.w[k].x), "=r"(r.w[k].y), "=r"(r.w[k].z), "=r"(r.w[k].w)
+                                 : "r"(stage + AT * MAXT + j * (MAXT * kWords * 16) + (at.tid >> 5) * (kWords * 512) +
+                                       word_place((at.tid & 31) * kWords + k) * 16) : "memory");
                 float e[8];
                 widen8(r, e);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[4 * j + i] = pack2(e[2 * i], e[2 * i + 1]);
             }
         } else {
-            const T* p = base + row * stride;
             float e[kCols];
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) e[i] = at.on(i) ? to_f32(p[at.col(i)]) : 0.0f;
+            for (int i = 0; i < kCols; ++i) e[i] = at.on(i) ? to_f32(next[i * at.threads]) : 0.0f;
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) v[i] = pack2(e[2 * i], e[2 * i + 1]);
         }
     }
-};
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_row(T* row, const Place<VEC>& at, const f32x2* v) {
-    float e[kCols];
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) unpack2(v[i], e[2 * i], e[2 * i + 1]);
-    if constexpr (VEC) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (at.on(8 * j)) store8(row + at.col(8 * j), e + 8 * j);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kCols; ++i)
-            if (at.on(i)) from_f32(e[i], row[at.col(i)]);
+    __device__ __forceinline__ void done() {   // with the row that read() reads
+        if constexpr (!VEC) next += stride;
     }
-}
+};
+// A result's rows, written in order.
+template <typename T, bool VEC>
+struct Results {
+    T* next;
+    long long stride;
+    __device__ __forceinline__ Results(void* base, long long row_stride, int row0, const Place<VEC>& at)
+        : next(reinterpret_cast<T*>(base) + (base ? row0 * row_stride + at.col(0) : 0)), stride(row_stride) {}
+    __device__ __forceinline__ void write(const Place<VEC>& at, const f32x2* v) {
+        float e[kCols];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) unpack2(v[i], e[2 * i], e[2 * i + 1]);
+        if constexpr (VEC) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                T* to = next + j * at.threads * 8;
+                const float* x = e + 8 * j;
+                if constexpr (sizeof(T) == 4) {
+                    store16_if(at.on(8 * j), to, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])));
+                    store16_if(at.on(8 * j), to + 4, make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])));
+                } else {
+                    const T* tag = nullptr;
+                    store16_if(at.on(8 * j), to, make_uint4(narrow2(x[0], x[1], tag), narrow2(x[2], x[3], tag), narrow2(x[4], x[5], tag), narrow2(x[6], x[7], tag)));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCols; ++i)
+                if (at.on(i)) from_f32(e[i], next[i * at.threads]);
+        }
+        next += stride;
+    }
+};
 // A vector of parameters at this thread's columns; `absent` without one and in dead columns.
 template <bool VEC>
 __device__ __forceinline__ void read_vector(const float* base, float absent, const Place<VEC>& at, f32x2* v) {
@@ -171,7 +225,7 @@ __device__ __forceinline__ void read_vector(const float* base, float absent, con
 // Sums over the thread block, the same value in every thread, in a fixed order.  Two buffers used in turn make one
 // barrier per sum enough: a buffer is written again only behind the next sum's barrier.
 struct BlockSum {
-    float (*buf)[2][16];   // [2 buffers][2 values][warp]
+    float (*buf)[4][16];   // [2 buffers][4 values][warp]
     int warps, turn;
     template <int N>
     __device__ __forceinline__ void run(float* v) {
@@ -198,8 +252,8 @@ struct BlockSum {
         }
     }
 };
-__device__ __forceinline__ BlockSum block_sum_init(float (*buf)[2][16]) {
-    for (int i = threadIdx.x; i < 64; i += blockDim.x) (&buf[0][0][0])[i] = 0.0f;   // entries past the last warp stay 0
+__device__ __forceinline__ BlockSum block_sum_init(float (*buf)[4][16]) {
+    for (int i = threadIdx.x; i < 128; i += blockDim.x) (&buf[0][0][0])[i] = 0.0f;   // entries past the last warp stay 0
     __syncthreads();
     return BlockSum{buf, (int)(blockDim.x + 31) / 32, 0};
 }
@@ -215,42 +269,63 @@ struct Channels {
     }
 };
 
-// v -> normalised v (dead columns hold and keep 0); returns the reciprocal deviation.
-template <bool VEC>
-__device__ __forceinline__ float normalise(f32x2* v, int kind, float eps, const Channels& ch, const Place<VEC>& at, BlockSum& sum) {
-    float s[1];
-    if (kind == kNormLayer) {
-        f32x2 t = add2(v[0], v[1]), u = add2(v[2], v[3]);
+// This thread's share of a row's sum, and of the sum of its squares.
+__device__ __forceinline__ float total(const f32x2* v) {
+    f32x2 t = add2(v[0], v[1]), u = add2(v[2], v[3]);
 #pragma unroll
-        for (int i = 4; i < kPairs; i += 2) {
-            t = add2(t, v[i]);
-            u = add2(u, v[i + 1]);
-        }
-        s[0] = join(add2(t, u));
-        sum.run<1>(s);
-        const float mean = ch.mean(s[0]);
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], at.masked(i, -mean));
+    for (int i = 4; i < kPairs; i += 2) {
+        t = add2(t, v[i]);
+        u = add2(u, v[i + 1]);
     }
+    return join(add2(t, u));
+}
+__device__ __forceinline__ float total_squares(const f32x2* v) {
     f32x2 t = mul2(v[0], v[0]), u = mul2(v[1], v[1]);
 #pragma unroll
     for (int i = 2; i < kPairs; i += 2) {
         t = fma2(v[i], v[i], t);
         u = fma2(v[i + 1], v[i + 1], u);
     }
-    s[0] = join(add2(t, u));
-    sum.run<1>(s);
-    const float r = rsqrtf(ch.mean(s[0]) + eps);
-    const f32x2 r2 = both(r);
+    return join(add2(t, u));
+}
+// v - mean in the live columns (dead ones hold and keep 0)
+template <bool VEC>
+__device__ __forceinline__ void subtract(f32x2* v, float mean, const Place<VEC>& at) {
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], r2);
-    return r;
+    for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], at.masked(i, -mean));
+}
+// v -> normalised v
+template <bool VEC>
+__device__ __forceinline__ void normalise(f32x2* v, int kind, float eps, const Channels& ch, const Place<VEC>& at, BlockSum& sum) {
+    float s[1];
+    if (kind == kNormLayer) {
+        s[0] = total(v);
+        sum.run<1>(s);
+        subtract<VEC>(v, ch.mean(s[0]), at);
+    }
+    s[0] = total_squares(v);
+    sum.run<1>(s);
+    const f32x2 r = both(rsqrtf(ch.mean(s[0]) + eps));
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], r);
 }
 
-// Dead columns are never copied: their places in the ring hold 0 from the start.
-__device__ __forceinline__ void clear_ring(uint4* ring, uint32_t bytes) {
-    for (uint32_t i = threadIdx.x; i < bytes / 16; i += blockDim.x) ring[i] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
+// A vector of this thread's columns kept in shared memory (only this thread reads and writes it).
+template <int MAXT>
+__device__ __forceinline__ void keep(float4* mem, const f32x2* v) {
+#pragma unroll
+    for (int i = 0; i < kPairs / 2; ++i) {
+        float4 q;
+        unpack2(v[2 * i], q.x, q.y);
+        unpack2(v[2 * i + 1], q.z, q.w);
+        mem[i * MAXT + threadIdx.x] = q;
+    }
+}
+template <int MAXT>
+__device__ __forceinline__ void recall(const float4* mem, int i, f32x2* a, f32x2* b) {   // pairs 2i and 2i + 1
+    const float4 q = mem[i * MAXT + threadIdx.x];
+    *a = pack2(q.x, q.y);
+    *b = pack2(q.z, q.w);
 }
 
 // The rows of up to four tensors copied ahead: `stages` rows' worth of shared memory in turn.  A stage is filled again one
@@ -261,8 +336,8 @@ struct Ring {
 };
 
 template <typename TX, typename TIO, bool VEC, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 512 ? 1 : 640 / MAXT) block_norm_forward_kernel(const BlockNormParams p, const Ring ring) {
-    __shared__ alignas(16) float buf[2][2][16];
+__global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_forward_kernel(const BlockNormParams p, const Ring ring) {
+    __shared__ alignas(16) float buf[2][4][16];
     extern __shared__ uint4 ring_mem[];
     BlockSum sum = block_sum_init(buf);
     const Place<VEC> at(p.channels);
@@ -270,25 +345,27 @@ __global__ void __launch_bounds__(MAXT, MAXT == 512 ? 1 : 640 / MAXT) block_norm
     const int row0 = blockIdx.x * p.rows_per_cta;
     const int row1 = min(p.n_tokens, row0 + p.rows_per_cta);
     const bool residual = p.y != nullptr;
-    if (VEC && p.channels < at.threads * kCols) clear_ring(ring_mem, ring.stages * ring.bytes);
-    const uint32_t mine = smem_u32(ring_mem) + at.tid * 16;
-    const Rows<TX, VEC> xs{reinterpret_cast<const TX*>(p.x), p.x_stride, mine};
-    const Rows<TIO, VEC> ys{reinterpret_cast<const TIO*>(p.y), p.y_stride, mine + at.threads * kMine<TX>};
-    auto fetch = [&](int row, int stage) {
+    const uint32_t mine = smem_u32(ring_mem), ring_end = mine + ring.stages * ring.bytes;
+    Rows<TX, VEC, 0, MAXT> xs(p.x, p.x_stride, row0, at, p.channels);
+    Rows<TIO, VEC, kMine<TX>, MAXT> ys(p.y, p.y_stride, row0, at, p.channels);
+    Results<TX, VEC> xo(p.x_out, p.x_out_stride, row0, at);
+    Results<TIO, VEC> ho(p.h, p.h_stride, row0, at);
+    int ahead = row0;     // next row to fetch
+    auto fetch = [&](uint32_t record) {
         if constexpr (VEC) {
-            if (row < row1) {
-                xs.fetch(at, row, stage * ring.bytes);
-                if (residual) ys.fetch(at, row, stage * ring.bytes);
+            if (ahead++ < row1) {
+                xs.fetch(at, record);
+                if (residual) ys.fetch(at, record);
             }
             copy_commit();
         }
     };
-    for (int s = 0; s < ring.stages - 1; ++s) fetch(row0 + s, s);
+    for (int s = 0; s < ring.stages - 1; ++s) fetch(mine + s * ring.bytes);
 
     int mod_end = row0;   // first token behind the modulation row held in registers
     f32x2 w[kPairs], b[kPairs], g[kPairs];
     const f32x2 alpha = both(p.residual_scale);
-    int stage = 0;
+    uint32_t here = mine, before = ring_end - ring.bytes;   // this row's record, and the one to fill again
     for (int row = row0; row < row1; ++row) {
         if (row >= mod_end) {
             const int mod = row / p.tokens_per_mod;
@@ -311,13 +388,15 @@ __global__ void __launch_bounds__(MAXT, MAXT == 512 ? 1 : 640 / MAXT) block_norm
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) g[i] = mul2(g[i], t[i]);
         }
-        fetch(row + ring.stages - 1, stage == 0 ? ring.stages - 1 : stage - 1);
+        if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();   // all lanes have read what is filled again
+        fetch(before);
         if constexpr (VEC) copy_wait(ring.stages);
+        if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();
         f32x2 v[kPairs];
-        xs.read(at, row, stage * ring.bytes, v);
+        xs.read(at, here, v);
         if (residual) {
             f32x2 z[kPairs];
-            ys.read(at, row, stage * ring.bytes, z);
+            ys.read(at, here, z);
             if (p.post_norm) normalise<VEC>(z, p.post_norm, p.post_eps, ch, at, sum);
             // (dead columns: z and x are 0, so x' is)
             if (p.residual_scale != 1.0f)
@@ -325,15 +404,19 @@ __global__ void __launch_bounds__(MAXT, MAXT == 512 ? 1 : 640 / MAXT) block_norm
                 for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], alpha);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) v[i] = fma2(g[i], z[i], v[i]);
-            if (p.x_out) store_row<TX, VEC>(reinterpret_cast<TX*>(p.x_out) + row * p.x_out_stride, at, v);
+            if (p.x_out) xo.write(at, v);
         }
         if (p.norm) {   // on x' before its rounding to the residual stream's type
             normalise<VEC>(v, p.norm, p.eps, ch, at, sum);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) v[i] = fma2(v[i], w[i], b[i]);
-            store_row<TIO, VEC>(reinterpret_cast<TIO*>(p.h) + row * p.h_stride, at, v);
+            ho.write(at, v);
         }
-        stage = stage + 1 == ring.stages ? 0 : stage + 1;
+        xs.done();
+        ys.done();
+        before = here;
+        here += ring.bytes;
+        if (here == ring_end) here = mine;
     }
 }
 
@@ -351,10 +434,14 @@ __device__ __forceinline__ float* slot_of(const BlockNormParams& p, int cta, int
     return p.partials + ((long long)cta * 9 + which * 3) * p.channels;
 }
 
+// (w = weight (1 + scale) and g = gate post_weight live in shared memory: the registers hold three sums per column.)
 template <typename TX, typename TIO, bool VEC, int MAXT>
-__global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNormParams p, const Ring ring) {
-    __shared__ alignas(16) float buf[2][2][16];
-    extern __shared__ uint4 ring_mem[];
+__global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward_kernel(const BlockNormParams p, const Ring ring) {
+    __shared__ alignas(16) float buf[2][4][16];
+    extern __shared__ uint4 shared_mem[];
+    float4* w_mem = reinterpret_cast<float4*>(shared_mem);
+    float4* g_mem = w_mem + kCols / 4 * MAXT;
+    uint4* ring_mem = shared_mem + 2 * (kCols / 4) * MAXT;
     BlockSum sum = block_sum_init(buf);
     const Place<VEC> at(p.channels);
     const Channels ch(p.channels);
@@ -364,30 +451,32 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
     const bool want_w = p.dweight || p.dbias || p.dpost_weight;
     const bool want_mod = p.dscale || p.dshift || p.dgate;
     const bool normed = p.norm != 0, branch = p.y != nullptr, more = p.dx_out != nullptr;
-    if (VEC && p.channels < at.threads * kCols) clear_ring(ring_mem, ring.stages * ring.bytes);
-    uint32_t mine = smem_u32(ring_mem) + at.tid * 16;
-    const Rows<TX, VEC> xs{reinterpret_cast<const TX*>(p.x), p.x_stride, mine};
-    const Rows<TIO, VEC> hs{reinterpret_cast<const TIO*>(p.dh), p.h_stride, mine += at.threads * kMine<TX>};
-    const Rows<TX, VEC> ds{reinterpret_cast<const TX*>(p.dx_out), p.dx_out_stride, mine += at.threads * kMine<TIO>};
-    const Rows<TIO, VEC> ys{reinterpret_cast<const TIO*>(p.y), p.y_stride, mine += at.threads * kMine<TX>};
-    auto fetch = [&](int row, int stage) {
+    const uint32_t mine = smem_u32(ring_mem), ring_end = mine + ring.stages * ring.bytes;
+    Rows<TX, VEC, 0, MAXT> xs(p.x, p.x_stride, row0, at, p.channels);
+    Rows<TIO, VEC, kMine<TX>, MAXT> hs(p.dh, p.h_stride, row0, at, p.channels);
+    Rows<TX, VEC, kMine<TX> + kMine<TIO>, MAXT> ds(p.dx_out, p.dx_out_stride, row0, at, p.channels);
+    Rows<TIO, VEC, 2 * kMine<TX> + kMine<TIO>, MAXT> ys(p.y, p.y_stride, row0, at, p.channels);
+    Results<TX, VEC> dxo(p.dx, p.dx_stride, row0, at);
+    Results<TIO, VEC> dyo(p.dy, p.dy_stride, row0, at);
+    int ahead = row0;     // next row to fetch
+    auto fetch = [&](uint32_t record) {
         if constexpr (VEC) {
-            if (row < row1) {
+            if (ahead++ < row1) {
                 if (normed) {
-                    xs.fetch(at, row, stage * ring.bytes);
-                    hs.fetch(at, row, stage * ring.bytes);
+                    xs.fetch(at, record);
+                    hs.fetch(at, record);
                 }
-                if (more) ds.fetch(at, row, stage * ring.bytes);
-                if (branch) ys.fetch(at, row, stage * ring.bytes);
+                if (more) ds.fetch(at, record);
+                if (branch) ys.fetch(at, record);
             }
             copy_commit();
         }
     };
-    for (int s = 0; s < ring.stages - 1; ++s) fetch(row0 + s, s);
+    for (int s = 0; s < ring.stages - 1; ++s) fetch(mine + s * ring.bytes);
 
-    f32x2 s0[kPairs], s1[kPairs], s2[kPairs], w[kPairs], g[kPairs];
+    f32x2 s0[kPairs], s1[kPairs], s2[kPairs];
     const f32x2 alpha = both(p.residual_scale);
-    int stage = 0;
+    uint32_t here = mine, before = ring_end - ring.bytes;   // this row's record, and the one to fill again
     bool first_flush = true;
     for (int row = row0; row < row1;) {
         const int mod = row / p.tokens_per_mod;
@@ -397,49 +486,88 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
         const bool complete = row == begin && end == whole_end;
         const long long from = mod * p.mod_stride;
         {
-            f32x2 t[kPairs];
+            f32x2 t[kPairs], w[kPairs];
             read_vector<VEC>(p.weight, 1.0f, at, w);
             read_vector<VEC>(p.scale ? p.scale + from : nullptr, 0.0f, at, t);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) w[i] = fma2(w[i], t[i], w[i]);
-            read_vector<VEC>(p.gate ? p.gate + from : nullptr, 1.0f, at, g);
+            keep<MAXT>(w_mem, w);
+            read_vector<VEC>(p.gate ? p.gate + from : nullptr, 1.0f, at, w);
             read_vector<VEC>(p.post_weight, 1.0f, at, t);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
-                g[i] = mul2(g[i], t[i]);
+                w[i] = mul2(w[i], t[i]);
                 s0[i] = s1[i] = s2[i] = 0ull;
             }
+            keep<MAXT>(g_mem, w);
         }
         for (; row < end; ++row) {
-            fetch(row + ring.stages - 1, stage == 0 ? ring.stages - 1 : stage - 1);
+            if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();   // all lanes have read what is filled again
+            fetch(before);
             if constexpr (VEC) copy_wait(ring.stages);
-            const uint32_t here = stage * ring.bytes;
+            if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();
             f32x2 d[kPairs], v[kPairs];
-            if (normed) {
-                xs.read(at, row, here, v);
-                const float r = normalise<VEC>(v, p.norm, p.eps, ch, at, sum);
-                hs.read(at, row, here, d);
-                f32x2 ta = 0ull, tb = 0ull;
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    s0[i] = add2(s0[i], d[i]);
-                    s1[i] = fma2(d[i], v[i], s1[i]);
-                    d[i] = mul2(d[i], w[i]);
-                    ta = add2(ta, d[i]);
-                    tb = fma2(d[i], v[i], tb);
+            float y_mean = 0.0f, y_r = 1.0f;
+            if (normed || p.post_norm) {
+                // All sums of the row that do not need dx' take two barriers: the means, then the centred squares of x' and
+                // y and the sums of d = dh (1 + s) w and of d against the centred x' (one barrier where both are RMS norms).
+                float m[2] = {0.0f, 0.0f}, q[4];
+                if (normed) xs.read(at, here, v);
+                if (p.norm == kNormLayer) m[0] = total(v);
+                if (p.post_norm == kNormLayer) {
+                    ys.read(at, here, d);
+                    m[1] = total(d);
                 }
-                float t[2] = {join(ta), join(tb)};
-                sum.run<2>(t);
-                // r (d - m0 - xhat m1)
-                const f32x2 m0 = both(p.norm == kNormLayer ? -r * ch.mean(t[0]) : 0.0f), m1 = both(-r * ch.mean(t[1])), r2 = both(r);
+                if (p.norm == kNormLayer || p.post_norm == kNormLayer) sum.run<2>(m);
+                y_mean = ch.mean(m[1]);
+                q[2] = 0.0f;
+                if (p.post_norm) {
+                    ys.read(at, here, d);
+                    if (p.post_norm == kNormLayer) subtract<VEC>(d, y_mean, at);
+                    q[2] = total_squares(d);
+                }
+                if (normed) {
+                    if (p.norm == kNormLayer) subtract<VEC>(v, ch.mean(m[0]), at);
+                    q[3] = total_squares(v);
+                    hs.read(at, here, d);
+                    f32x2 ta = 0ull, tb = 0ull;
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) d[i] = fma2(v[i], m1, fma2(d[i], r2, m0));
-            } else {
+                    for (int i = 0; i < kPairs; i += 2) {
+                        f32x2 w0, w1;
+                        recall<MAXT>(w_mem, i / 2, &w0, &w1);
+                        w0 = mul2(d[i], w0);
+                        w1 = mul2(d[i + 1], w1);
+                        ta = add2(ta, add2(w0, w1));
+                        tb = fma2(w1, v[i + 1], fma2(w0, v[i], tb));
+                    }
+                    q[0] = join(ta);
+                    q[1] = join(tb);
+                    sum.run<4>(q);
+                    const float r = rsqrtf(ch.mean(q[3]) + p.eps);
+                    // dx' = r (d - m0 - xhat m1), xhat = r times the centred x'
+                    const f32x2 r2 = both(r), m0 = both(p.norm == kNormLayer ? -r * ch.mean(q[0]) : 0.0f), m1 = both(-(r * (r * (r * ch.mean(q[1])))));
+#pragma unroll
+                    for (int i = 0; i < kPairs; i += 2) {
+                        f32x2 wi[2];
+                        recall<MAXT>(w_mem, i / 2, &wi[0], &wi[1]);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            s0[i + k] = add2(s0[i + k], d[i + k]);
+                            s1[i + k] = fma2(mul2(d[i + k], r2), v[i + k], s1[i + k]);
+                            d[i + k] = fma2(v[i + k], m1, fma2(mul2(d[i + k], wi[k]), r2, m0));
+                        }
+                    }
+                } else {
+                    sum.run<1>(q + 2);
+                }
+                if (p.post_norm) y_r = rsqrtf(ch.mean(q[2]) + p.post_eps);
+            }
+            if (!normed) {
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) d[i] = 0ull;
             }
             if (more) {
-                ds.read(at, row, here, v);
+                ds.read(at, here, v);
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) d[i] = add2(d[i], v[i]);
             }
@@ -447,20 +575,26 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
                 if (p.residual_scale != 1.0f) {
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) v[i] = mul2(d[i], alpha);
-                    store_row<TX, VEC>(reinterpret_cast<TX*>(p.dx) + row * p.dx_stride, at, v);
+                    dxo.write(at, v);
                 } else {
-                    store_row<TX, VEC>(reinterpret_cast<TX*>(p.dx) + row * p.dx_stride, at, d);
+                    dxo.write(at, d);
                 }
             }
             if (branch) {
-                ys.read(at, row, here, v);
-                float r = 1.0f;
-                if (p.post_norm) r = normalise<VEC>(v, p.post_norm, p.post_eps, ch, at, sum);
+                ys.read(at, here, v);
+                if (p.post_norm == kNormLayer) subtract<VEC>(v, y_mean, at);
+                if (p.post_norm)
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], both(y_r));
                 f32x2 ta = 0ull, tb = 0ull;
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
+                for (int i = 0; i < kPairs; i += 2) {
+                    f32x2 g0, g1;
+                    recall<MAXT>(g_mem, i / 2, &g0, &g1);
                     s2[i] = fma2(d[i], v[i], s2[i]);
-                    d[i] = mul2(d[i], g[i]);
+                    s2[i + 1] = fma2(d[i + 1], v[i + 1], s2[i + 1]);
+                    d[i] = mul2(d[i], g0);
+                    d[i + 1] = mul2(d[i + 1], g1);
                 }
                 if (p.post_norm) {
 #pragma unroll
@@ -472,13 +606,19 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
                     }
                     float t[2] = {join(ta), join(tb)};
                     sum.run<2>(t);
-                    const f32x2 m0 = both(p.post_norm == kNormLayer ? -r * ch.mean(t[0]) : 0.0f), m1 = both(-r * ch.mean(t[1])), r2 = both(r);
+                    const f32x2 m0 = both(p.post_norm == kNormLayer ? -y_r * ch.mean(t[0]) : 0.0f), m1 = both(-y_r * ch.mean(t[1])), r2 = both(y_r);
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) d[i] = fma2(v[i], m1, fma2(d[i], r2, m0));
                 }
-                if (p.dy) store_row<TIO, VEC>(reinterpret_cast<TIO*>(p.dy) + row * p.dy_stride, at, d);
+                if (p.dy) dyo.write(at, d);
             }
-            stage = stage + 1 == ring.stages ? 0 : stage + 1;
+            xs.done();
+            hs.done();
+            ds.done();
+            ys.done();
+            before = here;
+            here += ring.bytes;
+            if (here == ring_end) here = mine;
         }
         // the modulation row's sums: final where all of its tokens are this block's, else a slot of the workspace
         if (want_w || want_mod) {
@@ -516,12 +656,13 @@ __global__ void __launch_bounds__(MAXT) block_norm_backward_kernel(const BlockNo
     }
 }
 
-// Joins the slots.  Thread block (32 columns, job): 32 lanes of threads take every 32nd slot each, then one of them
-// adds the 32 sums.  Jobs below n_jobs are modulation rows that no single thread block of the first kernel held whole;
+// Joins the slots.  Thread block (32 columns, job): 16 lanes of threads take every 16th slot each, then one of them
+// adds the 16 sums.  Jobs below n_jobs are modulation rows that no single thread block of the first kernel held whole;
 // job n_jobs is the weights' gradients.
-__global__ void __launch_bounds__(1024) block_norm_join_kernel(const BlockNormParams p, const int n_ctas, const int n_jobs,
+constexpr int kJoinLanes = 16;
+__global__ void __launch_bounds__(32 * kJoinLanes, 2) block_norm_join_kernel(const BlockNormParams p, const int n_ctas, const int n_jobs,
                                                               const int by_boundary) {
-    __shared__ float part[3][32][33];
+    __shared__ float part[3][kJoinLanes][33];
     const int c = blockIdx.x * 32 + threadIdx.x, lane = threadIdx.y, job = blockIdx.y;
     const bool weights = job == n_jobs;
     int mod = job, a = 0, b = n_ctas;
@@ -541,7 +682,8 @@ __global__ void __launch_bounds__(1024) block_norm_join_kernel(const BlockNormPa
     }
     float s[3] = {0.0f, 0.0f, 0.0f};
     if (c < p.channels)
-        for (int cta = a + lane; cta < b; cta += 32) {
+#pragma unroll 4
+        for (int cta = a + lane; cta < b; cta += kJoinLanes) {
             const int which = weights ? 2 : ((long long)cta * p.rows_per_cta / p.tokens_per_mod == mod ? 0 : 1);
             const float* slot = slot_of(p, cta, which) + c;
 #pragma unroll
@@ -554,7 +696,7 @@ __global__ void __launch_bounds__(1024) block_norm_join_kernel(const BlockNormPa
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         s[k] = 0.0f;
-        for (int i = 0; i < 32; ++i) s[k] += part[k][i][threadIdx.x];
+        for (int i = 0; i < kJoinLanes; ++i) s[k] += part[k][i][threadIdx.x];
     }
     if (weights) {
         if (p.dweight) p.dweight[c] = s[0];
@@ -591,11 +733,11 @@ cudaError_t plan(BlockNormParams* p, K kernel, int threads, size_t smem, int sm_
 
 // Stages: as many as fit a share of the SM's shared memory (for about `threads_wanted` threads on it), two to four; one
 // where two rows do not fit an SM (fp32 gradients of more than 7000 channels).
-Ring plan_ring(bool vec, uint32_t stage_bytes, int threads, int threads_wanted) {
+Ring plan_ring(bool vec, uint32_t stage_bytes, uint32_t other_bytes, int threads, int threads_wanted) {
     if (!vec) return Ring{1, 0};
     const int blocks = threads_wanted / threads > 1 ? threads_wanted / threads : 1;
-    int stages = (int)(200000u / blocks / stage_bytes);
-    if (stages < 2) stages = 2 * stage_bytes <= 225000u ? 2 : 1;
+    int stages = (int)((224000u / blocks - other_bytes) / stage_bytes);
+    if (stages < 2) stages = 2 * stage_bytes + other_bytes <= 228000u ? 2 : 1;
     if (stages > 4) stages = 4;
     return Ring{stages, stage_bytes};
 }
@@ -603,7 +745,7 @@ Ring plan_ring(bool vec, uint32_t stage_bytes, int threads, int threads_wanted) 
 template <typename TX, typename TIO, bool VEC, int MAXT>
 cudaError_t forward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     const int threads = threads_for(p.channels);
-    const Ring ring = plan_ring(VEC, threads * (kMine<TX> + (p.y ? kMine<TIO> : 0)), threads, 640);
+    const Ring ring = plan_ring(VEC, MAXT * (kMine<TX> + kMine<TIO>), 0, threads, MAXT == 128 ? 480 : 320);
     const size_t smem = (size_t)ring.stages * ring.bytes;
     const cudaError_t e = plan(&p, block_norm_forward_kernel<TX, TIO, VEC, MAXT>, threads, smem, sm_count, 1 << 30, ctas);
     if (e != cudaSuccess) return e;
@@ -613,15 +755,14 @@ cudaError_t forward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_
 template <typename TX, typename TIO, bool VEC, int MAXT>
 cudaError_t backward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     const int threads = threads_for(p.channels);
-    // (all four tensors have their place, wanted or not)
-    const Ring ring = plan_ring(VEC, threads * 2 * (kMine<TX> + kMine<TIO>), threads, 384);
-    const size_t smem = (size_t)ring.stages * ring.bytes;
+    const Ring ring = plan_ring(VEC, MAXT * 2 * (kMine<TX> + kMine<TIO>), 2 * kMine<float> * MAXT, threads, 384);
+    const size_t smem = (size_t)ring.stages * ring.bytes + 2 * kMine<float> * MAXT;
     const cudaError_t e = plan(&p, block_norm_backward_kernel<TX, TIO, VEC, MAXT>, threads, smem, sm_count, kNormMaxCtas, ctas);
     if (e != cudaSuccess) return e;
     block_norm_backward_kernel<TX, TIO, VEC, MAXT><<<*ctas, threads, smem, stream>>>(p, ring);
     return cudaGetLastError();
 }
-// Builds by the registers that a row's threads leave: up to 2048 channels (forward only), 5120, 8192.
+// Builds by the registers that a row's threads leave: up to 2048 channels, 5120, 8192.
 template <typename TX, typename TIO, bool VEC>
 cudaError_t forward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     if (threads_for(p.channels) <= 128) return forward_one<TX, TIO, VEC, 128>(p, sm_count, ctas, stream);
@@ -630,6 +771,7 @@ cudaError_t forward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStrea
 }
 template <typename TX, typename TIO, bool VEC>
 cudaError_t backward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
+    if (threads_for(p.channels) <= 128) return backward_one<TX, TIO, VEC, 128>(p, sm_count, ctas, stream);
     if (threads_for(p.channels) <= 320) return backward_one<TX, TIO, VEC, 320>(p, sm_count, ctas, stream);
     return backward_one<TX, TIO, VEC, 512>(p, sm_count, ctas, stream);
 }
@@ -666,7 +808,7 @@ cudaError_t launch_block_norm_backward(BlockNormParams p, int x_type, int io_typ
     const int n_mods = (int)(((long long)p.n_tokens + p.tokens_per_mod - 1) / p.tokens_per_mod);
     const int jobs = !want_mod || ctas == 1 ? 0 : (by_boundary ? ctas - 1 : n_mods);   // at most `ctas` either way
     if (jobs + (want_w ? 1 : 0) == 0) return cudaSuccess;
-    block_norm_join_kernel<<<dim3((p.channels + 31) / 32, jobs + (want_w ? 1 : 0)), dim3(32, 32), 0, stream>>>(p, ctas, jobs,
+    block_norm_join_kernel<<<dim3((p.channels + 31) / 32, jobs + (want_w ? 1 : 0)), dim3(32, kJoinLanes), 0, stream>>>(p, ctas, jobs,
                                                                                                           by_boundary ? 1 : 0);
     e = cudaGetLastError();
     if (e == cudaSuccess) *launches = 2;
