@@ -143,7 +143,7 @@ int mx_project_checks(const void* w, const void* bias, const void* y, int y_type
 int mx_project(const void* x, const void* w, const void* bias, void* y, int y_type, int n, int features, int cols,
                int sm_count, int* status, cudaStream_t stream) {
     const MxLayout lx(n, cols), lw(features, cols);
-    const MxProjectPlan plan = plan_mxfp4_project(n, features, sm_count);
+    const MxProjectPlan plan = plan_mxfp4_project(n, features, cols, sm_count);
     CUtensorMap mx, mxs, mw, mws, my;
     char* xb = reinterpret_cast<char*>(const_cast<void*>(x));
     char* wb = reinterpret_cast<char*>(const_cast<void*>(w));

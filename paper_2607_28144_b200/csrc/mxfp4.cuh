@@ -46,7 +46,7 @@ struct MxProjectPlan {
     int tile_features;    // output features per work item
     int w_box_rows;       // rows of one weight load
 };
-MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int sm_count);
+MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int in_features, int sm_count);
 cudaError_t configure_mxfp4_project();
 cudaError_t launch_mxfp4_project(const MxProjectPlan& plan, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& w,
                                  const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, int sm_count,

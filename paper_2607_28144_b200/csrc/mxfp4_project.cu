@@ -9,7 +9,11 @@
 //   warp 1      copies the scales of a stage to tensor memory (tcgen05.cp, replicated to the four lane groups), issues
 //               the MMAs and commits
 //   warps 2-9   epilogue: accumulator -> + bias -> 16 bits -> swizzled staging tile -> tiled store
-// Two accumulators of NT columns, used in turn; the scales live behind them, in two sets used in turn.
+// Two accumulators of NT columns, used in turn, the scales behind them.
+//
+// Bound: the operands' way from L2.  All CTAs together take about 11.7 TB/s (45 bytes per SM and cycle), and a pair's
+// 256 x 192 tile needs 31 KB per CTA for 384 cycles of tensor work, a 256 x 256 tile 35 KB for 512: at 31200 x 5120 x
+// 15360 the two take 1.02 and 0.9x ms, single CTAs (43 KB for 128 x 192) 1.33 ms.
 #include "common.cuh"
 #include "cta_pair.cuh"
 #include "mxfp4.cuh"
@@ -36,7 +40,12 @@ struct Cfg {
     static constexpr uint32_t kOut = NT / 64 * kOutBlock;
     static constexpr int kStages = (int)((232448 - 4096 - kOut) / kStage) < 6 ? (int)((232448 - 4096 - kOut) / kStage) : 6;
     static constexpr int kColsHalf = NT / 2;                   // accumulator columns per epilogue thread
-    static_assert(NT % 64 == 0 && 2 * NT + 2 * kScaleColumns <= 512, "tensor memory");
+    // Tensor-memory columns: two accumulators used in turn, then two sets of scales.  Two of 256 columns and the scales do
+    // not fit 512 columns: the accumulators then share 48 columns, which an epilogue reads out first.
+    static constexpr bool kShare = 2 * NT + 2 * kScaleColumns > 512;
+    static constexpr uint32_t kAccStep = kShare ? 512 - 2 * kScaleColumns - NT : NT;
+    static constexpr uint32_t kScaleBase = kAccStep + NT;
+    static_assert(NT % 64 == 0 && kScaleBase + 2 * kScaleColumns <= 512 && NT - kAccStep <= 64, "tensor memory");
     // instruction descriptor of kind::mxf4: A and B e2m1 (1 at bits 7 and 10), N / 8 at bit 17, scales e8m0 (bit 23),
     // M / 16 at bit 24; the scales' place inside their words (bits 4 and 29) is added per instruction
     static constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) |
@@ -127,7 +136,7 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&sh->acc_full[b]), 1);
-            mbar_init(smem_u32(&sh->acc_empty[b]), CG);
+            mbar_init(smem_u32(&sh->acc_empty[b]), CG * (kEpiThreads / 32));
         }
         sh->abort_flag = (*reinterpret_cast<volatile int*>(p.status) != 0) ? 1 : 0;
         fence_mbar_init();
@@ -182,11 +191,14 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
             bool ok = true;
             for (int slice = slice0; ok && slice < n_slices; slice += slice_step, ++it) {
                 const int b = it & 1;
-                const uint32_t acc = tmem_base + b * NT;
+                const uint32_t acc = tmem_base + b * C::kAccStep;
                 // a tile that starts in the middle of 128 features takes its scales from the middle of their columns
                 const uint32_t sb_off = (uint32_t)(slice % n_rank * NT % 128) / 32;
-                if (it >= 2) {
-                    ok = mbar_wait(smem_u32(&sh->acc_empty[b]), ((it >> 1) - 1) & 1, ctl);
+                // accumulator b was read out two slices ago; where it shares columns with the other one, that one's
+                // shared columns have been read too (which comes later)
+                if (it >= (C::kShare ? 1 : 2)) {
+                    const int before = it - (C::kShare ? 1 : 2);
+                    ok = mbar_wait(smem_u32(&sh->acc_empty[before & 1]), (before >> 1) & 1, ctl);
                     if (!ok) break;
                     tc_fence_after();
                 }
@@ -197,7 +209,7 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
                     tc_fence_after();
                     const uint32_t sa = smem_u32(base + s * C::kStage), sb = sa + kCodesA, sc = sb + C::kCodesB;
                     const uint64_t da = umma_smem_desc_k_sw128(sa), db = umma_smem_desc_k_sw128(sb);
-                    const uint32_t t_sc = tmem_base + 2 * NT + (fill & 1) * kScaleColumns;
+                    const uint32_t t_sc = tmem_base + C::kScaleBase + (fill & 1) * kScaleColumns;
                     const int halves = min(2, p.k_blocks - 2 * kb);
                     // copies and MMAs of one thread run in the order of their issue
                     for (int k2 = 0; k2 < halves; ++k2) {
@@ -231,7 +243,7 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
         for (int slice = slice0; slice < n_slices; slice += slice_step, ++it) {
             const int f0 = slice % n_rank * NT, b = it & 1;
             const int tile = CG * (slice / n_rank) + rank;
-            const uint32_t t_acc = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + b * NT + half * C::kColsHalf;
+            const uint32_t t_acc = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + b * C::kAccStep + half * C::kColsHalf;
             if (et < NT) sh->bias[et] = p.bias && f0 + et < p.features ? __ldg(p.bias + f0 + et) : 0.0f;
             if (tid == 64) tma_store_wait_read();
             epi_barrier();
@@ -239,11 +251,23 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
 #pragma unroll 1
-            for (int cb = 0; cb < C::kColsHalf / 32; ++cb) {
+            for (int i = 0; i < C::kColsHalf / 32; ++i) {
+                // accumulator 0 shares its last columns, accumulator 1 its first ones: those of this half go first
+                const int cb = C::kShare && b == 0 ? C::kColsHalf / 32 - 1 - i : i;
                 uint32_t a[32];
                 if (ok) {
                     tmem_ld32(t_acc + cb * 32, a);
                     tmem_wait_ld();
+                }
+                if (i == (C::kShare ? 1 : C::kColsHalf / 32 - 1)) {
+                    // this warp's part of what the next MMAs overwrite is in registers (all of the accumulator, or 64 of
+                    // its columns, and those of the slice before were finished earlier)
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (CG == 2) mbar_arrive_peer(map_to_rank(smem_u32(&sh->acc_empty[b]), 0));
+                        else mbar_arrive(smem_u32(&sh->acc_empty[b]));
+                    }
                 }
                 const float4* b4 = reinterpret_cast<const float4*>(sh->bias + half * C::kColsHalf + cb * 32);
 #pragma unroll
@@ -261,12 +285,9 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
                         *reinterpret_cast<uint4*>(stage_out + (col >> 6) * C::kOutBlock + sw128_offset(row, (col >> 3) & 7)) = w;
                 }
             }
-            tc_fence_before();
             fence_proxy_async_smem();
             epi_barrier();
             if (tid == 64) {
-                if constexpr (CG == 2) mbar_arrive_cluster(map_to_rank(smem_u32(&sh->acc_empty[b]), 0));
-                else mbar_arrive(smem_u32(&sh->acc_empty[b]));
                 if (ok && tile < n_tiles) {
                     // what lies past the last token or feature is dropped by the store
 #pragma unroll
@@ -323,12 +344,34 @@ cudaError_t launch_cfg(const CUtensorMap& x, const CUtensorMap& xs, const CUtens
 
 }  // namespace
 
-MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int sm_count) {
-    const long long tiles = (n_tokens + kTile - 1) / kTile, wide = (features + 191) / 192;
-    // at least one item for every pair of CTAs: pairs; else single CTAs, on narrow items where wide ones leave SMs idle
-    if ((tiles + 1) / 2 * wide >= sm_count / 2) return MxProjectPlan{1, 192, 96};
-    if (tiles * wide < sm_count) return MxProjectPlan{0, 64, 64};
-    return MxProjectPlan{0, 192, 192};
+// Which build: the one with the least estimated time.  An item costs its operand bytes at what an SM can take (80 bytes
+// per cycle alone, 45 when all SMs load) and about 1500 cycles beside, more for wider epilogues; items run in rounds.
+// Measured (us, pairs 256 / pairs 192 / single 192 / single 64): see the table of sizes in the notes on this kernel.
+MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int in_features, int sm_count) {
+    struct Build {
+        MxProjectPlan plan;
+        int kilobytes;   // per CTA and 256 elements of K
+    };
+    static const Build builds[4] = {{{1, 256, 128}, 35}, {{1, 192, 96}, 31}, {{0, 192, 192}, 43}, {{0, 64, 64}, 27}};
+    const long long tiles = (n_tokens + kTile - 1) / kTile;
+    const double stages = (in_features + 255) / 256;
+    double best = 0.0;
+    const Build* pick = nullptr;
+    for (const Build& b : builds) {
+        const int group = b.plan.pair ? 2 : 1;
+        const long long items = (tiles + group - 1) / group * ((features + b.plan.tile_features - 1) / b.plan.tile_features);
+        const long long slots = sm_count / group;
+        const long long rounds = (items + slots - 1) / slots;
+        const double busy = (double)(items < slots ? items : slots) * group;
+        double rate = 45.0 * sm_count / busy;
+        if (rate > 80.0) rate = 80.0;
+        const double cycles = rounds * (stages * b.kilobytes * 1024.0 / rate + 1500.0 + 4.0 * b.plan.tile_features);
+        if (!pick || cycles < best) {
+            best = cycles;
+            pick = &b;
+        }
+    }
+    return pick->plan;
 }
 
 cudaError_t configure_mxfp4_project() {
@@ -337,12 +380,15 @@ cudaError_t configure_mxfp4_project() {
         e = cudaFuncSetAttribute(mxfp4_project_kernel<1, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mx_smem<1, 64>());
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(mxfp4_project_kernel<2, 192>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mx_smem<2, 192>());
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(mxfp4_project_kernel<2, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mx_smem<2, 256>());
     return e;
 }
 
 cudaError_t launch_mxfp4_project(const MxProjectPlan& plan, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& w,
                                  const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, int sm_count,
                                  cudaStream_t stream) {
+    if (plan.pair && plan.tile_features == 256) return launch_cfg<2, 256>(x, xs, w, ws, y, p, sm_count, stream);
     if (plan.pair) return launch_cfg<2, 192>(x, xs, w, ws, y, p, sm_count, stream);
     if (plan.tile_features == 64) return launch_cfg<1, 64>(x, xs, w, ws, y, p, sm_count, stream);
     return launch_cfg<1, 192>(x, xs, w, ws, y, p, sm_count, stream);
