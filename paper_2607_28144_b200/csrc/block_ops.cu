@@ -119,7 +119,8 @@ int mx_convert(const void* values, int type, int rows, int cols, long long row_s
     const Span v = rows_span(values, rows, p.row_stride, cols, type_size(type));
     const Span k{packed, (size_t)MxLayout(rows, cols).bytes};
     if (meet(v, k)) return REGENVC_ERR_ALIASING;
-    p.vec = aligned(values, 16) && p.row_stride % 8 == 0;
+    const size_t step = (size_t)p.row_stride * type_size(type);
+    p.vec = aligned(values, 32) && step % 32 == 0 ? 2 : (aligned(values, 16) && step % 16 == 0 ? 1 : 0);
     p.src = quantize ? values : packed;
     p.dst = const_cast<void*>(quantize ? packed : values);
     int sm_count = 0, *status = nullptr;

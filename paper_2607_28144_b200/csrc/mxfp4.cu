@@ -1,9 +1,9 @@
 // To and from microscaled 4-bit floating point (blocks of 32 along a row share a power-of-two scale; layout in
-// mxfp4.cuh).  Bound: HBM.  Sixteen threads take 128 columns of a row, eight each: four threads hold one block, so the
-// largest magnitude is two exchanges away, reads are 16 bytes per thread and writes 64 contiguous bytes per row.  A
-// thread keeps its columns and walks down a range of rows, four rows of loads in flight at a time: no division per
-// element group (with a unit number split into row and column a 31200 x 5120 quantisation took 265 us in 64-bit and 123 us
-// in 32-bit arithmetic).
+// mxfp4.cuh).  Bound: HBM in bytes, instructions in practice: with eight values per thread the quantisation issued 110
+// instructions per thread and row and kept the schedulers busy for 65 % of its time.  Hence sixteen values per thread --
+// two threads hold one block, so its largest magnitude is one exchange away; 32-byte reads, 8-byte codes --, magnitudes
+// compared as packed 16-bit patterns, and threads that keep their columns and walk down a range of rows by adding strides,
+// several rows of loads in flight at a time.
 #include "mx_convert.cuh"
 #include "mxfp4.cuh"
 #include "row_io.cuh"
@@ -12,195 +12,270 @@ namespace regenvc {
 namespace {
 
 constexpr int kMaxThreads = 256;
-constexpr int kRowsAhead = 4;
+constexpr int kWarpCols = 512;            // columns of a warp: four groups of 128
+constexpr int kSpread = kWarpCols + kWarpCols / 4;
 
-// Largest magnitude of eight values as an fp32 bit pattern (magnitudes compare as their bits, NaN above infinity).
-__device__ __forceinline__ uint32_t top_of(const float* v) {
-    uint32_t top = 0;
+// Sixteen elements as they lie in memory.
+template <typename T>
+struct Raw16 {
+    uint32_t w[4 * sizeof(T)];
+};
+// wide: 32-byte accesses are allowed, else 16-byte ones
+template <typename T>
+__device__ __forceinline__ void load16(Raw16<T>& r, const T* p, bool wide) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return top;
-}
-// The same from packed 16-bit values: the bit patterns of magnitudes compare as unsigned halves.
-__device__ __forceinline__ uint32_t top16_of(const uint4& r) {
-    const uint32_t m = __vmaxu2(__vmaxu2(r.x & 0x7FFF7FFFu, r.y & 0x7FFF7FFFu), __vmaxu2(r.z & 0x7FFF7FFFu, r.w & 0x7FFF7FFFu));
-    return max(m >> 16, m & 0xFFFFu);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        uint32_t* w = r.w + 8 * i;
+        const T* q = p + i * (32 / (int)sizeof(T));
+        if (wide) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(q));
+        } else {
+            const uint4 a = reinterpret_cast<const uint4*>(q)[0], b = reinterpret_cast<const uint4*>(q)[1];
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+        }
+    }
 }
 template <typename T>
-__device__ __forceinline__ uint32_t top_raw(const Raw8<T>& r) {
+__device__ __forceinline__ void store16(T* p, const Raw16<T>& r, bool wide) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint32_t* w = r.w + 8 * i;
+        T* q = p + i * (32 / (int)sizeof(T));
+        if (wide) {
+            asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                         ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(q) : "memory");
+        } else {
+            reinterpret_cast<uint4*>(q)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            reinterpret_cast<uint4*>(q)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void widen16(const Raw16<T>& r, float* v) {
     if constexpr (sizeof(T) == 4) {
-        float v[8];
-        widen8(r, v);
-        return top_of(v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r.w[i]);
     } else {
-        const uint32_t h = top16_of(r.w[0]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) widen2(r.w[i], v[2 * i], v[2 * i + 1], (const T*)nullptr);
+    }
+}
+// Largest magnitude as an fp32 bit pattern (magnitudes compare as their bits, NaN above infinity; 16-bit ones as
+// unsigned halves).
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const Raw16<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = max(top, r.w[i] & 0x7FFFFFFFu);
+        return top;
+    } else {
+        uint32_t m = r.w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = __vmaxu2(m, r.w[i] & 0x7FFF7FFFu);
         float a, b;
-        widen2(h, a, b, (const T*)nullptr);
+        widen2(max(m >> 16, m & 0xFFFFu), a, b, (const T*)nullptr);
         return __float_as_uint(a);
     }
 }
-
-// A half warp's 128 values where rows do not allow 16-byte accesses: lane l reads elements l, l + 16, ... (neighbouring
-// lanes neighbouring elements), and an exchange through shared memory gives it elements 8l .. 8l + 7.
+// Element by element, for rows that do not allow wide accesses: a warp's 512 columns are read with neighbouring lanes on
+// neighbouring elements and exchanged through shared memory (16 elements every 20 words, off each other's banks).
+__device__ __forceinline__ int spread_at(int e) { return e + (e >> 4) * 4; }
 template <typename T>
-__device__ __forceinline__ void load_spread(const T* row, int c, int cols, int lane, float* buf, float* v) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i * 16 + lane < cols ? to_f32(row[c + i * 16 + lane]) : 0.0f;
+__device__ __forceinline__ void load_spread(const T* row, int c, int cols, int lane, float* buf, Raw16<float>& r) {
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) buf[i * 16 + lane] = v[i];
+    for (int i = 0; i < 16; ++i) buf[spread_at(i * 32 + lane)] = c + i * 32 + lane < cols ? to_f32(row[c + i * 32 + lane]) : 0.0f;
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float4 q = reinterpret_cast<const float4*>(buf)[lane * 2 + i];
-        v[4 * i] = q.x, v[4 * i + 1] = q.y, v[4 * i + 2] = q.z, v[4 * i + 3] = q.w;
+    for (int i = 0; i < 4; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(buf + lane * 20 + 4 * i);
+        r.w[4 * i] = __float_as_uint(q.x), r.w[4 * i + 1] = __float_as_uint(q.y);
+        r.w[4 * i + 2] = __float_as_uint(q.z), r.w[4 * i + 3] = __float_as_uint(q.w);
     }
 }
 
 // Place of the scale word (four blocks) of a row in the tiles of one column group, `groups` tiles per 128 rows.
-__device__ __forceinline__ long long scale_word(long long row, unsigned groups, unsigned g) {
+__device__ __forceinline__ long long scale_place(long long row, unsigned groups, unsigned g) {
     return (row / 128 * groups + g) * 512 + (row & 31) * 16 + (row & 127) / 32 * 4;
 }
 
-// Thread block (x: range of rows, y: column groups of 128, two per warp).  Rows behind the last one, up to a whole scale
-// tile, get scales of 0.
+// Codes (eight bytes) and the scales of the 128 columns around, from sixteen values in a thread.
+template <typename T>
+__device__ __forceinline__ uint2 quantise16(const Raw16<T>& r, int lane, uint32_t* scale_word) {
+    uint32_t top = top_of<T>(r);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const uint32_t byte = mx_scale_byte(top);
+    const float inv = mx_inverse_scale(byte);
+    float v[16];
+    widen16<T>(r, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= inv;
+    uint2 codes = make_uint2(mx_codes8(v), mx_codes8(v + 8));
+    if (byte == 255u) codes = make_uint2(0, 0);
+    uint32_t word = byte << (lane >> 1 & 3) * 8;
+    word |= __shfl_xor_sync(0xffffffffu, word, 2);
+    *scale_word = word | __shfl_xor_sync(0xffffffffu, word, 4);
+    return codes;
+}
+
+// Thread block (x: range of rows, y: warps' columns).  Rows behind the last one, up to a whole scale tile, get scales of 0.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kMaxThreads) mxfp4_quantize_kernel(const MxConvertParams p, const int rows_per_block) {
-    __shared__ alignas(16) float spread[VEC ? 1 : kMaxThreads / 16][VEC ? 4 : 128];
+    __shared__ alignas(16) float spread[VEC ? 1 : kMaxThreads / 32][VEC ? 4 : kSpread];
+    constexpr int kAhead = !VEC ? 1 : (sizeof(T) == 4 ? 2 : 4);   // rows of loads in flight
     const MxLayout lay(p.rows, p.cols);
     const unsigned groups = (unsigned)(lay.cols_pad / 128);
-    const int lane = threadIdx.x & 15, half = threadIdx.x >> 4;
-    const unsigned g = blockIdx.y * (blockDim.x / 16) + half;   // may lie behind the last group: the warp stays whole
-    const int c = (int)g * 128 + lane * 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = (int)(blockIdx.y * (blockDim.x / 32) + warp) * kWarpCols, c = c0 + lane * 16;
+    const unsigned g = (unsigned)c / 128;                       // may lie behind the last group: the warp stays whole
     const long long row0 = (long long)blockIdx.x * rows_per_block;
     const long long rows_pad = (lay.rows + 127) / 128 * 128;
     const int rows = (int)(rows_pad - row0 < rows_per_block ? rows_pad - row0 : rows_per_block);
     const int live = (int)(lay.rows - row0 < 0 ? 0 : (lay.rows - row0 < rows ? lay.rows - row0 : rows));
-    uint8_t* codes = reinterpret_cast<uint8_t*>(p.dst) + row0 * (lay.cols_pad / 2) + g * 64 + lane * 4;
+    const long long code_row = lay.cols_pad / 2;
+    uint8_t* codes = reinterpret_cast<uint8_t*>(p.dst) + row0 * code_row + c / 2;
     uint8_t* scales = reinterpret_cast<uint8_t*>(p.dst) + lay.scale_at;
     const T* src = reinterpret_cast<const T*>(p.src) + row0 * p.row_stride;
-    const bool mine = g < groups, whole = mine && c + 8 <= p.cols;
-    for (int r = 0; r < rows; r += kRowsAhead) {
-        Raw8<T> raw[kRowsAhead];
+    const bool mine = g < groups, whole = c + 16 <= p.cols, wide = p.vec > 1;
+    for (int r = 0; r < rows; r += kAhead) {
+        Raw16<T> raw[kAhead];
         if constexpr (VEC) {
 #pragma unroll
-            for (int k = 0; k < kRowsAhead; ++k)
-                if (whole && r + k < live) raw[k] = load_raw8(src + (r + k) * p.row_stride + c);
+            for (int k = 0; k < kAhead; ++k)
+                if (whole && r + k < live) load16(raw[k], src + k * p.row_stride + c, wide);
         }
 #pragma unroll
-        for (int k = 0; k < kRowsAhead; ++k) {
-            float v[8];
-            uint32_t top;
-            const T* row = src + (r + k) * p.row_stride;
+        for (int k = 0; k < kAhead; ++k) {
             const bool on = r + k < live;
+            const T* row = src + k * p.row_stride;
+            uint32_t word;
+            uint2 eight;
             if constexpr (VEC) {
-                if (whole && on) {
-                    widen8(raw[k], v);
-                    top = top_raw(raw[k]);
-                } else {
+                if (!(whole && on)) {   // the last columns of a row, or none
+                    Raw16<T> part;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = mine && on && c + i < p.cols ? to_f32(row[c + i]) : 0.0f;
-                    top = top_of(v);
+                    for (int i = 0; i < 16; ++i) {
+                        float f = on && c + i < p.cols ? to_f32(row[c + i]) : 0.0f;
+                        T e;
+                        from_f32(f, e);
+                        if constexpr (sizeof(T) == 4) {
+                            part.w[i] = __float_as_uint(e);
+                        } else {
+                            const uint32_t bits = *reinterpret_cast<const uint16_t*>(&e);
+                            part.w[i / 2] = i % 2 ? part.w[i / 2] | bits << 16 : bits;
+                        }
+                    }
+                    raw[k] = part;
                 }
+                eight = quantise16<T>(raw[k], lane, &word);
             } else {
-                load_spread(row, (int)g * 128, mine && on ? p.cols : 0, lane, spread[half], v);
-                top = top_of(v);
+                Raw16<float> f;
+                load_spread(row, c0, on ? p.cols : 0, lane, spread[warp], f);
+                eight = quantise16<float>(f, lane, &word);
             }
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const uint32_t byte = mx_scale_byte(top);
-            const float inv = mx_inverse_scale(byte);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= inv;
-            const uint32_t eight = byte == 255u ? 0u : mx_codes8(v);
-            // the four scales of these 128 columns side by side
-            uint32_t word = byte << (lane >> 2) * 8;
-            word |= __shfl_xor_sync(0xffffffffu, word, 4);
-            word |= __shfl_xor_sync(0xffffffffu, word, 8);
-            if (mine && on) *reinterpret_cast<uint32_t*>(codes + (r + k) * (lay.cols_pad / 2)) = eight;
-            if (mine && lane == 0 && r + k < rows) *reinterpret_cast<uint32_t*>(scales + scale_word(row0 + r + k, groups, g)) = word;
+            if (mine && on) *reinterpret_cast<uint2*>(codes + k * code_row) = eight;
+            if (mine && (lane & 7) == 0 && r + k < rows) *reinterpret_cast<uint32_t*>(scales + scale_place(row0 + r + k, groups, g)) = word;
         }
+        src += kAhead * p.row_stride;
+        codes += kAhead * code_row;
     }
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kMaxThreads) mxfp4_dequantize_kernel(const MxConvertParams p, const int rows_per_block) {
-    __shared__ alignas(16) float spread[VEC ? 1 : kMaxThreads / 16][VEC ? 4 : 128];
+    __shared__ alignas(16) float spread[VEC ? 1 : kMaxThreads / 32][VEC ? 4 : kSpread];
+    constexpr int kAhead = 4;
     const MxLayout lay(p.rows, p.cols);
     const unsigned groups = (unsigned)(lay.cols_pad / 128);
-    const int lane = threadIdx.x & 15, half = threadIdx.x >> 4;
-    const unsigned g = blockIdx.y * (blockDim.x / 16) + half;
-    const int c = (int)g * 128 + lane * 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = (int)(blockIdx.y * (blockDim.x / 32) + warp) * kWarpCols, c = c0 + lane * 16;
+    const unsigned g = (unsigned)c / 128;
     const long long row0 = (long long)blockIdx.x * rows_per_block;
     const int rows = (int)(lay.rows - row0 < rows_per_block ? lay.rows - row0 : rows_per_block);
-    const uint8_t* codes = reinterpret_cast<const uint8_t*>(p.src) + row0 * (lay.cols_pad / 2) + g * 64 + lane * 4;
-    const uint8_t* scales = reinterpret_cast<const uint8_t*>(p.src) + lay.scale_at + lane / 4;
+    const long long code_row = lay.cols_pad / 2;
+    const uint8_t* codes = reinterpret_cast<const uint8_t*>(p.src) + row0 * code_row + c / 2;
+    const uint8_t* scales = reinterpret_cast<const uint8_t*>(p.src) + lay.scale_at + (lane >> 1 & 3);
     T* dst = reinterpret_cast<T*>(p.dst) + row0 * p.row_stride;
-    const bool mine = g < groups;
-    for (int r = 0; r < rows; r += kRowsAhead) {
-        uint32_t q[kRowsAhead], s[kRowsAhead];
+    const bool mine = g < groups, whole = c + 16 <= p.cols, wide = p.vec > 1;
+    for (int r = 0; r < rows; r += kAhead) {
+        uint2 q[kAhead];
+        uint32_t s[kAhead];
 #pragma unroll
-        for (int k = 0; k < kRowsAhead; ++k) {
-            q[k] = s[k] = 0;
+        for (int k = 0; k < kAhead; ++k) {
+            q[k] = make_uint2(0, 0);
+            s[k] = 0;
             if (mine && r + k < rows) {
-                q[k] = *reinterpret_cast<const uint32_t*>(codes + (r + k) * (lay.cols_pad / 2));
-                s[k] = scales[scale_word(row0 + r + k, groups, g)];
+                q[k] = *reinterpret_cast<const uint2*>(codes + k * code_row);
+                s[k] = scales[scale_place(row0 + r + k, groups, g)];
             }
         }
 #pragma unroll
-        for (int k = 0; k < kRowsAhead; ++k) {
+        for (int k = 0; k < kAhead; ++k) {
             const bool on = mine && r + k < rows;
-            T* out = dst + (r + k) * p.row_stride;
-            uint32_t h2[4];
-            float v[8];
-            mx_values8(q[k], h2);
+            T* out = dst + k * p.row_stride;
+            uint32_t h2[8];
+            float v[16];
+            mx_values8(q[k].x, h2);
+            mx_values8(q[k].y, h2 + 4);
             const float scale = mx_scale_value(s[k]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 widen2(h2[i], v[2 * i], v[2 * i + 1], (const __half*)nullptr);
                 v[2 * i] *= scale;
                 v[2 * i + 1] *= scale;
             }
             if constexpr (VEC) {
-                if (on && c + 8 <= p.cols) {
-                    store8(out + c, v);
+                if (on && whole) {
+                    Raw16<T> w;
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w.w[i] = __float_as_uint(v[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w.w[i] = narrow2(v[2 * i], v[2 * i + 1], (const T*)nullptr);
+                    }
+                    store16(out + c, w, wide);
                 } else if (on) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < 16; ++i)
                         if (c + i < p.cols) from_f32(v[i], out[c + i]);
                 }
             } else {
                 // the exchange of load_spread() the other way round
-                float* buf = spread[half];
+                float* buf = spread[warp];
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    reinterpret_cast<float4*>(buf)[lane * 2 + i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<float4*>(buf + lane * 20 + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int e = (int)g * 128 + i * 16 + lane;
-                    if (on && e < p.cols) from_f32(buf[i * 16 + lane], out[e]);
+                for (int i = 0; i < 16; ++i) {
+                    const int e = i * 32 + lane;
+                    if (r + k < rows && c0 + e < p.cols) from_f32(buf[spread_at(e)], out[c0 + e]);
                 }
             }
         }
+        codes += kAhead * code_row;
+        dst += kAhead * p.row_stride;
     }
 }
 
-// Threads: two column groups per warp, at most eight warps; rows per block: a multiple of kRowsAhead, about five blocks of
-// 256 threads per SM in all.
+// A thread block is up to eight warps side by side; rows per block: a multiple of four, about 1280 threads per SM in all.
 struct ConvertPlan {
     dim3 grid;
     int threads, rows;
 };
-ConvertPlan plan_convert(long long rows, long long groups, int sm_count) {
+ConvertPlan plan_convert(long long rows, long long cols, int sm_count) {
     ConvertPlan c;
-    c.threads = (int)(groups >= 16 ? 256 : (groups + 1) / 2 * 32);
-    const long long across = (groups + c.threads / 16 - 1) / (c.threads / 16);
-    long long down = 5ll * sm_count * (256 / c.threads) / across;
+    const long long warps = (cols + kWarpCols - 1) / kWarpCols, across = (warps + 7) / 8;
+    const long long each = (warps + across - 1) / across;
+    c.threads = (int)each * 32;
+    long long down = 40ll * sm_count / (each * across);
     if (down < 1) down = 1;
     long long per = (rows + down - 1) / down;
-    per = (per + kRowsAhead - 1) / kRowsAhead * kRowsAhead;
+    per = (per + 3) / 4 * 4;
     if (per > 4096) per = 4096;
     c.rows = (int)per;
     c.grid = dim3((unsigned)((rows + per - 1) / per), (unsigned)across);
@@ -209,14 +284,14 @@ ConvertPlan plan_convert(long long rows, long long groups, int sm_count) {
 
 template <typename T>
 cudaError_t quantize_typed(const MxConvertParams& p, int sm_count, cudaStream_t stream) {
-    const ConvertPlan c = plan_convert(((long long)p.rows + 127) / 128 * 128, ((long long)p.cols + 127) / 128, sm_count);
+    const ConvertPlan c = plan_convert(((long long)p.rows + 127) / 128 * 128, p.cols, sm_count);
     if (p.vec) mxfp4_quantize_kernel<T, true><<<c.grid, c.threads, 0, stream>>>(p, c.rows);
     else mxfp4_quantize_kernel<T, false><<<c.grid, c.threads, 0, stream>>>(p, c.rows);
     return cudaGetLastError();
 }
 template <typename T>
 cudaError_t dequantize_typed(const MxConvertParams& p, int sm_count, cudaStream_t stream) {
-    const ConvertPlan c = plan_convert(p.rows, ((long long)p.cols + 127) / 128, sm_count);
+    const ConvertPlan c = plan_convert(p.rows, p.cols, sm_count);
     if (p.vec) mxfp4_dequantize_kernel<T, true><<<c.grid, c.threads, 0, stream>>>(p, c.rows);
     else mxfp4_dequantize_kernel<T, false><<<c.grid, c.threads, 0, stream>>>(p, c.rows);
     return cudaGetLastError();

@@ -29,7 +29,7 @@ struct MxConvertParams {
     void* dst;
     long long row_stride; // of the values, in elements
     int rows, cols;
-    int vec;              // the values' address and stride allow 16-byte accesses
+    int vec;              // the values' address and stride allow accesses of 32 bytes (2), 16 bytes (1) or neither (0)
 };
 cudaError_t launch_mxfp4_quantize(const MxConvertParams& p, int type, int sm_count, cudaStream_t stream);
 cudaError_t launch_mxfp4_dequantize(const MxConvertParams& p, int type, int sm_count, cudaStream_t stream);
