@@ -386,14 +386,20 @@ int regenvc_rope_axes(const regenvc_rope_axes_desc* d, const void* q, const void
         if (!(same[0] && apart(2, 1)) && meet(span[2], span[1])) return REGENVC_ERR_ALIASING;
         if (!(same[1] && apart(3, 0)) && meet(span[3], span[0])) return REGENVC_ERR_ALIASING;
     }
-    // frequencies in 64 bits, as turns per unit of position
-    const double two_pi = 6.283185307179586476925286766559;
+    // Frequencies as turns per unit of position: powers of one ratio per ladder, multiplied up in extended precision (64
+    // factors add up to 2^-58) and rounded to 64 bits.
+    const long double turn = 1.0L / 6.283185307179586476925286766559L;
     int j = 0;
-    for (int a = 0; a < d->n_axes; ++a)
-        for (int i = 0; i < d->widths[a] / 2; ++i, ++j) {
-            const double power = d->whole_ladder ? (double)j / p.n_pairs : (double)i / (d->widths[a] / 2);
-            p.turns[j] = std::pow((double)d->rope_theta, -power) / two_pi;
+    for (int a = 0; a < d->n_axes; ++a) {
+        const int pairs = d->widths[a] / 2;
+        if (a == 0 || !d->whole_ladder) {
+            p.turns[j] = (double)turn;
+            const long double ratio = std::pow((long double)d->rope_theta, -1.0L / (d->whole_ladder ? p.n_pairs : pairs));
+            long double f = turn;
+            for (int i = 1; i < (d->whole_ladder ? p.n_pairs : pairs); ++i) p.turns[j + i] = (double)(f *= ratio);
         }
+        j += pairs;
+    }
     int sm_count = 0, *status = nullptr;
     const int rc = op_device(&sm_count, &status);
     if (rc != REGENVC_OK) return rc;

@@ -21,6 +21,16 @@ constexpr int kBatch = 4;
 
 // One thread's share of a head.  kAdjacent: eight neighbouring elements.  kHalves: eight of the first and the matching
 // eight of the second half of the rotated part, or eight that are copied.  kElements: one pair, or one copied element.
+// Place of pair j in a token's table.  A thread reads the pairs of its item as 16-byte words of two; word i of item c lies
+// at i * items + c, so that neighbouring threads read neighbouring words (in the pairs' own order the reads of eight
+// threads fell on two banks, and waiting for them was the kernel's largest stall).
+template <int MODE>
+__device__ __forceinline__ int table_place(int j, int n_pairs) {
+    if constexpr (MODE == kAdjacent) return ((j >> 1 & 1) * ((n_pairs + 3) >> 2) + (j >> 2)) * 2 + (j & 1);
+    if constexpr (MODE == kHalves) return ((j >> 1 & 3) * (n_pairs >> 3) + (j >> 3)) * 2 + (j & 1);
+    return j;
+}
+
 template <typename T, int MODE>
 struct Item;
 template <typename T>
@@ -31,10 +41,11 @@ struct Item<T, kAdjacent> {
         float v[8];
         widen8(r, v);
         if (4 * c + 4 <= p.n_pairs) {
-            const float4* q = reinterpret_cast<const float4*>(cs + 4 * c);
+            const float4* q = reinterpret_cast<const float4*>(cs) + c;
+            const int items = (p.n_pairs + 3) >> 2;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float4 t = q[i];
+                const float4 t = q[i * items];
                 const float a = v[4 * i], b = v[4 * i + 1], a2 = v[4 * i + 2], b2 = v[4 * i + 3];
                 v[4 * i] = a * t.x - b * t.y;
                 v[4 * i + 1] = b * t.x + a * t.y;
@@ -45,7 +56,7 @@ struct Item<T, kAdjacent> {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (4 * c + i < p.n_pairs) {
-                    const float2 t = cs[4 * c + i];
+                    const float2 t = cs[table_place<kAdjacent>(4 * c + i, p.n_pairs)];
                     const float a = v[2 * i], b = v[2 * i + 1];
                     v[2 * i] = a * t.x - b * t.y;
                     v[2 * i + 1] = b * t.x + a * t.y;
@@ -70,10 +81,11 @@ struct Item<T, kHalves> {
         widen8(lo, a);
         if (8 * c < p.n_pairs) {
             widen8(hi, b);
-            const float4* q = reinterpret_cast<const float4*>(cs + 8 * c);
+            const float4* q = reinterpret_cast<const float4*>(cs) + c;
+            const int items = p.n_pairs >> 3;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float4 t = q[i];
+                const float4 t = q[i * items];
                 const float x = a[2 * i], y = b[2 * i], x2 = a[2 * i + 1], y2 = b[2 * i + 1];
                 a[2 * i] = x * t.x - y * t.y;
                 b[2 * i] = y * t.x + x * t.y;
@@ -113,8 +125,8 @@ struct Item<T, kElements> {
 template <typename T, int MODE>
 __global__ void __launch_bounds__(kRopeThreads) rope_axes_kernel(const __grid_constant__ RopeAxesParams p, const int per_head) {
     extern __shared__ float4 table_raw[];
-    float2* table = reinterpret_cast<float2*>(table_raw);   // [tokens_per_cta][n_pairs rounded up to 2] (cos, sin)
-    const int pitch = (p.n_pairs + 1) & ~1;
+    float2* table = reinterpret_cast<float2*>(table_raw);   // [tokens_per_cta][n_pairs rounded up to 4] (cos, sin)
+    const int pitch = (p.n_pairs + 3) & ~3;
     const int token0 = blockIdx.x * p.tokens_per_cta;
     const int tokens = min(p.tokens_per_cta, p.n_tokens - token0);
     const int lanes = blockDim.x / per_head;                // heads in hand at a time
@@ -131,7 +143,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_axes_kernel(const __grid_co
         const double turn = pos * p.turns[j];
         float s, k;
         sincospif(2.0f * (float)(turn - rint(turn)), &s, &k);
-        table[t * pitch + j] = make_float2(k, p.inverse ? -s : s);
+        table[t * pitch + table_place<MODE>(j, p.n_pairs)] = make_float2(k, p.inverse ? -s : s);
     }
     __syncthreads();
     if (lane >= lanes) return;
@@ -171,17 +183,19 @@ cudaError_t launch_typed(RopeAxesParams p, bool vec, int sm_count, cudaStream_t 
                        : mode == kHalves  ? p.n_pairs / 8 + (p.head_dim - rotated) / 8
                                           : p.n_pairs + p.head_dim - rotated;
     const int all = p.heads[0] + p.heads[1];
-    // tokens per thread block: enough vectors for eight per thread, but no fewer blocks than the device holds at a time
+    // tokens per thread block: enough vectors for about sixteen per thread; fewer where that would leave the device (about
+    // four blocks per SM at a time) less than one round
     int lanes = kRopeThreads / per_head;
-    int tokens = 8 * lanes / all;
-    if (tokens > 8) tokens = 8;
+    int tokens = 16 * lanes / all;
+    const long long even = ((long long)p.n_tokens + 4 * sm_count - 1) / (4 * sm_count);
+    if (tokens > even) tokens = (int)even;
+    if (tokens > 16) tokens = 16;
     if (tokens < 1) tokens = 1;
-    while (tokens > 1 && (p.n_tokens + tokens - 1) / tokens < 4 * sm_count) --tokens;
     if (lanes > all * tokens) lanes = all * tokens;
     p.tokens_per_cta = tokens;
     const int threads = lanes * per_head;
     const unsigned grid = (unsigned)((p.n_tokens + tokens - 1) / tokens);
-    const size_t smem = (size_t)tokens * ((p.n_pairs + 1) & ~1) * sizeof(float2);
+    const size_t smem = (size_t)tokens * ((p.n_pairs + 3) & ~3) * sizeof(float2);
     if (mode == kAdjacent) rope_axes_kernel<T, kAdjacent><<<grid, threads, smem, stream>>>(p, per_head);
     else if (mode == kHalves) rope_axes_kernel<T, kHalves><<<grid, threads, smem, stream>>>(p, per_head);
     else rope_axes_kernel<T, kElements><<<grid, threads, smem, stream>>>(p, per_head);
