@@ -175,31 +175,37 @@ __global__ void __launch_bounds__(kRopeThreads) rope_axes_kernel(const __grid_co
     }
 }
 
-template <typename T>
-cudaError_t launch_typed(RopeAxesParams p, bool vec, int sm_count, cudaStream_t stream) {
-    const int rotated = 2 * p.n_pairs;
-    const int mode = !vec || p.head_dim % 8 != 0 || (p.halves && p.n_pairs % 8 != 0) ? kElements : (p.halves ? kHalves : kAdjacent);
-    const int per_head = mode == kAdjacent ? p.head_dim / 8
-                       : mode == kHalves  ? p.n_pairs / 8 + (p.head_dim - rotated) / 8
-                                          : p.n_pairs + p.head_dim - rotated;
+template <typename T, int MODE>
+cudaError_t launch_mode(RopeAxesParams& p, int per_head, int sm_count, cudaStream_t stream) {
     const int all = p.heads[0] + p.heads[1];
-    // tokens per thread block: enough vectors for about sixteen per thread; fewer where that would leave the device (about
-    // four blocks per SM at a time) less than one round
     int lanes = kRopeThreads / per_head;
+    const int pitch = (p.n_pairs + 3) & ~3;
+    // tokens per thread block: enough vectors for about sixteen per thread; fewer where that would leave the device less
+    // than one round of blocks
     int tokens = 16 * lanes / all;
-    const long long even = ((long long)p.n_tokens + 4 * sm_count - 1) / (4 * sm_count);
-    if (tokens > even) tokens = (int)even;
     if (tokens > 16) tokens = 16;
+    if (tokens > 1) {
+        int per_sm = 1;
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, rope_axes_kernel<T, MODE>, kRopeThreads,
+                                                                            (size_t)tokens * pitch * sizeof(float2));
+        if (e != cudaSuccess) return e;
+        const long long slots = (long long)(per_sm > 0 ? per_sm : 1) * sm_count, even = (p.n_tokens + slots - 1) / slots;
+        if (tokens > even) tokens = (int)even;
+    }
     if (tokens < 1) tokens = 1;
     if (lanes > all * tokens) lanes = all * tokens;
     p.tokens_per_cta = tokens;
-    const int threads = lanes * per_head;
-    const unsigned grid = (unsigned)((p.n_tokens + tokens - 1) / tokens);
-    const size_t smem = (size_t)tokens * ((p.n_pairs + 3) & ~3) * sizeof(float2);
-    if (mode == kAdjacent) rope_axes_kernel<T, kAdjacent><<<grid, threads, smem, stream>>>(p, per_head);
-    else if (mode == kHalves) rope_axes_kernel<T, kHalves><<<grid, threads, smem, stream>>>(p, per_head);
-    else rope_axes_kernel<T, kElements><<<grid, threads, smem, stream>>>(p, per_head);
+    rope_axes_kernel<T, MODE><<<(unsigned)((p.n_tokens + tokens - 1) / tokens), lanes * per_head,
+                                (size_t)tokens * pitch * sizeof(float2), stream>>>(p, per_head);
     return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch_typed(RopeAxesParams& p, bool vec, int sm_count, cudaStream_t stream) {
+    const int rest = p.head_dim - 2 * p.n_pairs;
+    if (!vec || p.head_dim % 8 != 0 || (p.halves && p.n_pairs % 8 != 0))
+        return launch_mode<T, kElements>(p, p.n_pairs + rest, sm_count, stream);
+    if (p.halves) return launch_mode<T, kHalves>(p, (p.n_pairs + rest) / 8, sm_count, stream);
+    return launch_mode<T, kAdjacent>(p, p.head_dim / 8, sm_count, stream);
 }
 
 }  // namespace
