@@ -434,6 +434,9 @@ def regenvc_block_norm_workspace_bytes(n_tokens: int, channels: int) -> int:
     return int(lib().regenvc_block_norm_workspace_bytes(n_tokens, channels))
 
 
+_NORM_GRADS = ("dx", "dy", "dgate", "dscale", "dshift", "dpost_weight", "dweight", "dbias")
+
+
 def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, post_norm: int = NORM_NONE, post_weight=None,
                                 post_eps: float = 1e-6, residual_scale: float = 1.0, norm: int = NORM_LAYER, weight=None,
                                 bias=None, eps: float = 1e-6, scale=None, shift=None, tokens_per_mod=None, dx=None,
@@ -460,12 +463,14 @@ def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, po
         dx, dx_stride = new((n, c), like.dtype), 0
     else:
         dx_stride = _rows(dx, "dx", like.dtype, n, c)
-    f32 = torch.float32
-    g = {"dx": dx, "dy": None if y is None else new((n, c), io)}
-    for t, name in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")):
-        g[name] = None if t is None else new((rows, c), f32)
-    for t, name in ((post_weight, "dpost_weight"), (weight, "dweight"), (bias, "dbias")):
-        g[name] = None if t is None else new((c,), f32)
+    g = dict.fromkeys(_NORM_GRADS)
+    g["dx"], g["dy"] = dx, None if y is None else new((n, c), io)
+    # one allocation for the modulation's gradients and one for the vectors'
+    for shape, wanted in (((rows, c), [k for t, k in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")) if t is not None]),
+                          ((c,), [k for t, k in ((post_weight, "dpost_weight"), (weight, "dweight"), (bias, "dbias"))
+                                  if t is not None])):
+        if wanted:
+            g.update(zip(wanted, new((len(wanted), *shape), torch.float32).unbind(0)))
     need = regenvc_block_norm_workspace_bytes(n, c)
     if workspace is None:
         workspace = new((need,), torch.uint8)
@@ -489,8 +494,8 @@ def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, h
         raise TypeError("q must be [tokens, heads, head_dim] in bf16, fp16 or fp32")
     index = _place(q, k, positions, q_out, k_out)
     n, hq, d = q.shape
-    widths = [int(w) for w in widths]
-    if positions.dtype not in (torch.int32, torch.float32) or tuple(positions.shape) != (len(widths), n) or \
+    widths = list(widths)
+    if positions.dtype not in (torch.int32, torch.float32) or positions.shape != (len(widths), n) or \
             (n > 1 and positions.stride(1) != 1) or (len(widths) > 1 and positions.stride(0) < n):
         raise TypeError(f"positions must be int32 or fp32 [{len(widths)}, {n}] with neighbouring tokens")
     if k is not None and (k.dtype != q.dtype or k.dim() != 3 or k.shape[0] != n or k.shape[2] != d):
@@ -509,13 +514,18 @@ def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, h
         if t is None:
             strides += [0, 0]
             continue
-        if t.dtype != q.dtype or t.shape != like.shape or (d > 1 and t.stride(2) != 1):
+        if t.is_contiguous() and t.dtype is q.dtype and t.shape == like.shape:
+            strides += [0, 0]
+            continue
+        token, head, step = t.stride()
+        heads = t.shape[1]
+        if t.dtype is not q.dtype or t.shape != like.shape or (d > 1 and step != 1):
             raise TypeError(f"{name} must have its operand's type and shape and neighbouring elements of a head")
-        if (n > 1 and t.stride(0) < d) or (t.shape[1] > 1 and t.stride(1) < d):
+        if (n > 1 and token < d) or (heads > 1 and head < d):
             raise ValueError(f"{name} has vectors that overlap (an expanded tensor?)")
         # the stride of an axis with one entry is never used: name the packed one
-        head = t.stride(1) if t.shape[1] > 1 else d
-        strides += [t.stride(0) if n > 1 else max(t.shape[1] * head, d), head]
+        head = head if heads > 1 else d
+        strides += [token if n > 1 else heads * head, head]
     desc = _ROPE_DESC.pack(n, hq, hk, d, TYPES[q.dtype], len(widths), *(widths + [0, 0, 0])[:4], rope_theta, bool(halves),
                            bool(whole_ladder), positions.dtype is torch.float32, bool(inverse),
                            positions.stride(0) if len(widths) > 1 else 0, *strides)
