@@ -325,6 +325,13 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _like(t, stream):
+    """A packed result of an operand's shape and type."""
+    if stream is None and t.is_contiguous():
+        return torch.empty_like(t)
+    return _new(t.shape, t.dtype, t.device, stream)
+
+
 def _place(first, *others) -> int:
     """All operands on the device the library launches on (the current one); returns its index."""
     if not first.is_cuda:
@@ -415,13 +422,13 @@ def regenvc_block_norm_forward(x, y=None, *, gate=None, post_norm: int = NORM_NO
             raise ValueError("x_out needs y")
         x_out_stride = _rows(x_out, "x_out", x.dtype, n, c)
     elif y is not None:
-        x_out = _new((n, c), x.dtype, x.device, stream)
+        x_out = _like(x, stream)
     if h is not None:
         if norm == NORM_NONE:
             raise ValueError("h needs a norm")
         h_stride = _rows(h, "h", io, n, c)
     elif norm != NORM_NONE:
-        h = _new((n, c), io, x.device, stream)
+        h = _like(x, stream) if io is x.dtype else _new((n, c), io, x.device, stream)
     d = _NORM_DESC.pack(n, c, per, TYPES[x.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
                         mod_stride, x_stride, y_stride, x_out_stride, h_stride, 0, 0, 0)
     _check(lib().regenvc_block_norm_forward(d, x.data_ptr(), _addr(y), _addr(gate), _addr(post_weight), _addr(weight),
@@ -453,29 +460,31 @@ def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, po
     io = dh.dtype if dh is not None else (y.dtype if y is not None else like.dtype)
     if io not in TYPES:
         raise TypeError("dh must be bf16, fp16 or fp32")
-    strides = [0 if t is None else _rows(t, name, dtype, n, c) for t, name, dtype in
-               ((y, "y", io), (x_out, "x_out", like.dtype), (dh, "dh", io), (dx_out, "dx_out", like.dtype))]
+    y_stride = 0 if y is None else _rows(y, "y", io, n, c)
+    x_stride = 0 if x_out is None else _rows(x_out, "x_out", like.dtype, n, c)
+    h_stride = 0 if dh is None else _rows(dh, "dh", io, n, c)
+    more_stride = 0 if dx_out is None else _rows(dx_out, "dx_out", like.dtype, n, c)
     for t, name in ((post_weight, "post_weight"), (weight, "weight"), (bias, "bias")):
         _vector(t, name, c)
     per, rows, mod_stride = _modulation(n, c, tokens_per_mod, gate, scale, shift)
-    new = lambda shape, dtype: _new(shape, dtype, like.device, stream)  # noqa: E731
     if dx is None:
-        dx, dx_stride = new((n, c), like.dtype), 0
+        dx, dx_stride = _like(like, stream), 0
     else:
         dx_stride = _rows(dx, "dx", like.dtype, n, c)
     g = dict.fromkeys(_NORM_GRADS)
-    g["dx"], g["dy"] = dx, None if y is None else new((n, c), io)
-    # one allocation for the modulation's gradients and one for the vectors'
-    for shape, wanted in (((rows, c), [k for t, k in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")) if t is not None]),
-                          ((c,), [k for t, k in ((post_weight, "dpost_weight"), (weight, "dweight"), (bias, "dbias"))
-                                  if t is not None])):
-        if wanted:
-            g.update(zip(wanted, new((len(wanted), *shape), torch.float32).unbind(0)))
-    need = regenvc_block_norm_workspace_bytes(n, c)
+    g["dx"], g["dy"] = dx, None if y is None else _like(y, stream)
+    # the parameters' gradients are parts of one allocation
+    wanted = [(k, rows) for t, k in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")) if t is not None]
+    wanted += [(k, 0) for t, k in ((post_weight, "dpost_weight"), (weight, "dweight"), (bias, "dbias")) if t is not None]
+    if wanted:
+        sizes = [(r or 1) * c for _, r in wanted]
+        parts = _new((sum(sizes),), torch.float32, like.device, stream).split_with_sizes(sizes)
+        for (k, r), part in zip(wanted, parts):
+            g[k] = part.view(r, c) if r else part
     if workspace is None:
-        workspace = new((need,), torch.uint8)
+        workspace = _new((regenvc_block_norm_workspace_bytes(n, c),), torch.uint8, like.device, stream)
     d = _NORM_DESC.pack(n, c, per, TYPES[like.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
-                        mod_stride, 0, *strides, dx_stride, 0)
+                        mod_stride, 0, y_stride, x_stride, h_stride, more_stride, dx_stride, 0)
     _check(lib().regenvc_block_norm_backward(
         d, _addr(x_out), _addr(y), _addr(gate), _addr(post_weight), _addr(weight), _addr(bias), _addr(scale),
         _addr(dh), _addr(dx_out), dx.data_ptr(), _addr(g["dy"]), _addr(g["dgate"]), _addr(g["dpost_weight"]),
@@ -505,9 +514,9 @@ def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, h
     if not 1 <= len(widths) <= 4:
         raise RegenvcError(ERR_BAD_SHAPE, status_string(ERR_BAD_SHAPE))
     if q_out is None:
-        q_out = _new(q.shape, q.dtype, q.device, stream)
+        q_out = _like(q, stream)
     if k is not None and k_out is None:
-        k_out = _new(k.shape, k.dtype, k.device, stream)
+        k_out = _like(k, stream)
     hk = 0 if k is None else k.shape[1]
     strides = []
     for t, like, name in ((q, q, "q"), (k, k, "k"), (q_out, q, "q_out"), (k_out, k, "k_out")):
