@@ -277,8 +277,9 @@ int regenvc_rope_axes(const regenvc_rope_axes_desc* desc, const void* q, const v
  *   multiple of 8 (REGENVC_ERR_UNSUPPORTED).  Waits inside are bounded as in the attention kernels.
  * regenvc_mxfp4_linear(): the same from unpacked x, quantised in the call: as regenvc_mxfp4_quantize() into `scratch`
  *   (regenvc_mxfp4_linear_scratch_bytes() bytes, 256-byte aligned, its content unspecified afterwards) and
- *   regenvc_mxfp4_project().  Calls of up to four tokens run as one kernel that needs no scratch (0 bytes: NULL is
- *   accepted) up to in_features of 20096, and of one token up to 80640.
+ *   regenvc_mxfp4_project().  Calls of one token (in_features up to 80640), and of up to four on a small matrix (in_features
+ *   up to 20096, fewer than 2^24 weights counted with cols_pad), run as one kernel that needs no scratch: 0 bytes, NULL is
+ *   accepted.
  */
 size_t regenvc_mxfp4_bytes(int rows, int cols);
 int regenvc_mxfp4_quantize(const void* src, int type, int rows, int cols, long long row_stride, void* packed, void* stream);
@@ -286,7 +287,7 @@ int regenvc_mxfp4_dequantize(const void* packed, void* dst, int type, int rows, 
                              void* stream);
 int regenvc_mxfp4_project(const void* x_packed, const void* w_packed, const void* bias, void* y, int y_type,
                           int n_tokens, int out_features, int in_features, void* stream);
-size_t regenvc_mxfp4_linear_scratch_bytes(int n_tokens, int in_features);
+size_t regenvc_mxfp4_linear_scratch_bytes(int n_tokens, int out_features, int in_features);
 int regenvc_mxfp4_linear(const void* x, int x_type, long long x_stride, const void* w_packed, const void* bias, void* y,
                          int y_type, int n_tokens, int out_features, int in_features, void* scratch, void* stream);
 

@@ -117,7 +117,7 @@ def lib() -> ctypes.CDLL:
     L.regenvc_rope_axes.restype = i32
     L.regenvc_mxfp4_bytes.argtypes = [i32, i32]
     L.regenvc_mxfp4_bytes.restype = sz
-    L.regenvc_mxfp4_linear_scratch_bytes.argtypes = [i32, i32]
+    L.regenvc_mxfp4_linear_scratch_bytes.argtypes = [i32, i32, i32]
     L.regenvc_mxfp4_linear_scratch_bytes.restype = sz
     L.regenvc_mxfp4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp]
     L.regenvc_mxfp4_quantize.restype = i32
@@ -593,8 +593,8 @@ def regenvc_mxfp4_dequantize(packed, rows: int, cols: int, dtype=torch.bfloat16,
     return out
 
 
-def regenvc_mxfp4_linear_scratch_bytes(n_tokens: int, in_features: int) -> int:
-    return int(lib().regenvc_mxfp4_linear_scratch_bytes(n_tokens, in_features))
+def regenvc_mxfp4_linear_scratch_bytes(n_tokens: int, out_features: int, in_features: int) -> int:
+    return int(lib().regenvc_mxfp4_linear_scratch_bytes(n_tokens, out_features, in_features))
 
 
 def _mx_result(y, y_dtype, n: int, features: int, device, stream):
@@ -631,7 +631,7 @@ def regenvc_mxfp4_linear(x, w_packed, out_features: int, bias=None, *, y_dtype=t
     _vector(bias, "bias", out_features)
     index = _place(x, w_packed, bias, y, scratch)
     y = _mx_result(y, y_dtype, n, out_features, x.device, stream)
-    need = regenvc_mxfp4_linear_scratch_bytes(n, cols)
+    need = regenvc_mxfp4_linear_scratch_bytes(n, out_features, cols)
     if scratch is None and need:
         scratch = _new((need,), torch.uint8, x.device, stream)
     if scratch is not None and (scratch.dtype != torch.uint8 or not scratch.is_contiguous() or scratch.numel() < need):

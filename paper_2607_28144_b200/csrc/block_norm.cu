@@ -87,46 +87,47 @@ struct Place {
     }
 };
 
+// Bytes of a row's image: the row and what 16-byte words add at its ends.
+__host__ __device__ __forceinline__ uint32_t image_bytes(int channels, size_t size) {
+    return ((uint32_t)(channels * size) + 15) / 16 * 16 + 16;
+}
 // Bytes of one thread's columns of a row of T.
 template <typename T>
 constexpr uint32_t kMine = kCols * sizeof(T);
 
-// One tensor's rows, taken in order.  VEC: copied ahead into this warp's part of a ring stage (16-byte words of
+// One tensor's rows, taken in order.  Where rows allow 16-byte accesses they are copied ahead into this warp's part of a ring stage (16-byte words of
 // neighbouring lanes are neighbours in global and in shared memory: word w of a warp's data is lane w % 32's copy
 // number w / 32).  A 16-bit lane reads back its own words.  An fp32 group of eight columns is two words: lane l reads
 // words 2l and 2l + 1, which other lanes of its warp copied, so a warp synchronises behind its waits; the words of every
-// other eight are swapped in pairs, which keeps those reads off each other's banks.  Otherwise read straight from global
-// memory.
+// other eight are swapped in pairs, which keeps those reads off each other's banks.
 template <typename T, bool VEC, uint32_t AT, int MAXT>
-struct Rows {
+struct Rows;
+template <typename T, uint32_t AT, int MAXT>
+struct Rows<T, true, AT, MAXT> {
     enum { kWords = (int)sizeof(T) / 2 };   // 16-byte words per lane and group
-    const T* next;        // VEC: this thread's first word of the row to fetch next; else its first column of the row to read
+    const T* next;        // this thread's first word of the row to fetch next
     long long stride;
-    uint32_t bytes;       // VEC: what each of the copies moves, a byte of this number for each (16, or 0 in dead columns)
-    __device__ __forceinline__ Rows(const void* base, long long row_stride, int row0, const Place<VEC>& at, int channels)
+    uint32_t bytes;       // what each of the copies moves, a byte of this number for each (16, or 0 in dead columns)
+    __device__ __forceinline__ Rows(const void* base, long long row_stride, int row0, const Place<true>& at, const BlockNormParams& p, uint32_t&)
         : next(nullptr), stride(row_stride), bytes(0) {
         if (!base) return;
         const T* row = reinterpret_cast<const T*>(base) + row0 * row_stride;
-        if constexpr (VEC) {
-            const int first = word_column(at, 0, 0);
-            next = row + (first < channels ? first : 0);
+        const int first = word_column(at, 0, 0);
+        next = row + (first < p.channels ? first : 0);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int k = 0; k < kWords; ++k)
-                    bytes |= (word_column(at, j, k) < channels ? 16u : 0u) << (j * kWords + k) * 8;
-        } else {
-            next = row + (at.on(0) ? at.col(0) : 0);
-        }
+            for (int k = 0; k < kWords; ++k)
+                bytes |= (word_column(at, j, k) < p.channels ? 16u : 0u) << (j * kWords + k) * 8;
     }
     // First column of the word that this lane copies as its k-th of group j.
-    static __device__ __forceinline__ int word_column(const Place<VEC>& at, int j, int k) {
+    static __device__ __forceinline__ int word_column(const Place<true>& at, int j, int k) {
         return ((j * at.threads + (at.tid & ~31)) * kWords + k * 32 + (at.tid & 31)) * (16 / (int)sizeof(T));
     }
     static __device__ __forceinline__ uint32_t word_place(uint32_t w) { return kWords == 1 ? w : w ^ (w >> 3 & 1); }
     // `stage`: the stage's address plus this warp's share, 16 bytes per lane (the part of group j, copy k is a constant on)
-    __device__ __forceinline__ void fetch(const Place<VEC>& at, uint32_t stage) {
-        if constexpr (VEC) {
+    __device__ __forceinline__ void fetch(const Place<true>& at, uint32_t stage) {
+        {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -139,8 +140,8 @@ struct Rows {
             next += stride;
         }
     }
-    __device__ __forceinline__ void read(const Place<VEC>& at, uint32_t stage, f32x2* v) {
-        if constexpr (VEC) {
+    __device__ __forceinline__ void read(const Place<true>& at, uint32_t stage, f32x2* v) {
+        {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 Raw8<T> r;
@@ -155,17 +156,63 @@ struct Rows {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[4 * j + i] = pack2(e[2 * i], e[2 * i + 1]);
             }
-        } else {
-            float e[kCols];
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) e[i] = at.on(i) ? to_f32(next[i * at.threads]) : 0.0f;
-#pragma unroll
-            for (int i = 0; i < kPairs; ++i) v[i] = pack2(e[2 * i], e[2 * i + 1]);
         }
     }
-    __device__ __forceinline__ void done() {   // with the row that read() reads
-        if constexpr (!VEC) next += stride;
+    __device__ __forceinline__ void done() {}
+};
+// The other rows (odd widths, strides or addresses): every 16-byte word that a row touches is copied into an image of the
+// row in the stage, by whichever thread comes to it, and the elements are read from there wherever they fall.  Words are
+// whole 16-byte words of global memory, cut off at the tensor's last element; the one that would begin before its first
+// element goes element by element.
+template <typename T, uint32_t AT, int MAXT>
+struct Rows<T, false, AT, MAXT> {
+    uintptr_t first, end, next, here;   // the tensor's ends, the row to fetch next and the one to read
+    long long step;
+    uint32_t place, width;
+    __device__ __forceinline__ Rows(const void* base, long long row_stride, int row0, const Place<false>&, const BlockNormParams& p,
+                                    uint32_t& used)
+        : first((uintptr_t)base), step(row_stride * (long long)sizeof(T)), place(used), width(p.channels * (uint32_t)sizeof(T)) {
+        end = first + (uintptr_t)(p.n_tokens - 1) * (uintptr_t)step + width;
+        next = here = first + (uintptr_t)row0 * (uintptr_t)step;
+        if (base) used += image_bytes(p.channels, sizeof(T));
     }
+    __device__ __forceinline__ void fetch(const Place<false>& at, uint32_t stage) {
+        const uintptr_t from = next & ~(uintptr_t)15, to = next + width;
+        for (uint32_t w = at.tid; from + 16 * w < to; w += at.threads) {
+            const uintptr_t g = from + 16 * w;
+            const uint32_t s = stage + place + 16 * w;
+            if (g >= first) {
+                copy_async16(s, reinterpret_cast<const void*>(g), end - g < 16 ? (uint32_t)(end - g) : 16u);
+            } else {
+                for (uintptr_t e = first; e < g + 16 && e < end; e += sizeof(T)) store_shared(s + (uint32_t)(e - g), *reinterpret_cast<const T*>(e));
+            }
+        }
+        next += (uintptr_t)step;
+    }
+    static __device__ __forceinline__ void store_shared(uint32_t a, T v) {
+        if constexpr (sizeof(T) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(__float_as_uint(v)) : "memory");
+        else asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"(*reinterpret_cast<const uint16_t*>(&v)) : "memory");
+    }
+    static __device__ __forceinline__ float load_shared(uint32_t a) {
+        if constexpr (sizeof(T) == 4) {
+            uint32_t u;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u) : "r"(a) : "memory");
+            return __uint_as_float(u);
+        } else {
+            uint16_t u;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(a) : "memory");
+            return to_f32(*reinterpret_cast<const T*>(&u));
+        }
+    }
+    __device__ __forceinline__ void read(const Place<false>& at, uint32_t stage, f32x2* v) {
+        const uint32_t a = stage + place + (uint32_t)(here & 15) + at.tid * (uint32_t)sizeof(T);
+        float e[kCols];
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) e[i] = at.on(i) ? load_shared(a + i * at.threads * (uint32_t)sizeof(T)) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = pack2(e[2 * i], e[2 * i + 1]);
+    }
+    __device__ __forceinline__ void done() { here += (uintptr_t)step; }   // with the row that read() reads
 };
 // A result's rows, written in order.
 template <typename T, bool VEC>
@@ -335,6 +382,29 @@ struct Ring {
     uint32_t bytes;      // of a stage
 };
 
+// Starts the copies into the stage that was read last (`before`) and makes this row's ones visible to whoever reads them:
+// the thread itself (OWN), its warp, or, for images, the whole thread block.
+template <bool VEC, bool OWN, typename F>
+__device__ __forceinline__ void next_row(F& fetch, uint32_t before, int stages) {
+    if constexpr (VEC) {
+        if constexpr (!OWN) __syncwarp();   // all lanes have read what is filled again
+        fetch(before);
+        copy_wait(stages);
+        if constexpr (!OWN) __syncwarp();
+    } else {
+        if (stages == 1) {
+            __syncthreads();
+            fetch(before);
+            copy_wait(1);
+            __syncthreads();
+        } else {
+            copy_wait(stages - 1);
+            __syncthreads();                // this row has arrived, and everyone has read the one before
+            fetch(before);
+        }
+    }
+}
+
 template <typename TX, typename TIO, bool VEC, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_forward_kernel(const BlockNormParams p, const Ring ring) {
     __shared__ alignas(16) float buf[2][4][16];
@@ -346,19 +416,18 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_forward_
     const int row1 = min(p.n_tokens, row0 + p.rows_per_cta);
     const bool residual = p.y != nullptr;
     const uint32_t mine = smem_u32(ring_mem), ring_end = mine + ring.stages * ring.bytes;
-    Rows<TX, VEC, 0, MAXT> xs(p.x, p.x_stride, row0, at, p.channels);
-    Rows<TIO, VEC, kMine<TX>, MAXT> ys(p.y, p.y_stride, row0, at, p.channels);
+    uint32_t used = 0;
+    Rows<TX, VEC, 0, MAXT> xs(p.x, p.x_stride, row0, at, p, used);
+    Rows<TIO, VEC, kMine<TX>, MAXT> ys(p.y, p.y_stride, row0, at, p, used);
     Results<TX, VEC> xo(p.x_out, p.x_out_stride, row0, at);
     Results<TIO, VEC> ho(p.h, p.h_stride, row0, at);
     int ahead = row0;     // next row to fetch
     auto fetch = [&](uint32_t record) {
-        if constexpr (VEC) {
-            if (ahead++ < row1) {
-                xs.fetch(at, record);
-                if (residual) ys.fetch(at, record);
-            }
-            copy_commit();
+        if (ahead++ < row1) {
+            xs.fetch(at, record);
+            if (residual) ys.fetch(at, record);
         }
+        copy_commit();
     };
     for (int s = 0; s < ring.stages - 1; ++s) fetch(mine + s * ring.bytes);
 
@@ -388,10 +457,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_forward_
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) g[i] = mul2(g[i], t[i]);
         }
-        if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();   // all lanes have read what is filled again
-        fetch(before);
-        if constexpr (VEC) copy_wait(ring.stages);
-        if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();
+        next_row<VEC, sizeof(TX) + sizeof(TIO) <= 4>(fetch, before, ring.stages);
         f32x2 v[kPairs];
         xs.read(at, here, v);
         if (residual) {
@@ -428,6 +494,30 @@ __device__ __forceinline__ void write_mod_grads(const BlockNormParams& p, long l
     if (p.dgate) p.dgate[at] = (p.post_weight ? p.post_weight[c] : 1.0f) * s2;
 }
 
+// `N` neighbouring fp32 values (16-byte aligned where N is 4).
+template <int N>
+__device__ __forceinline__ void read_run(const float* from, float absent, float* v) {
+    if (from == nullptr) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = absent;
+    } else if constexpr (N == 4) {
+        const float4 q = *reinterpret_cast<const float4*>(from);
+        v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = from[k];
+    }
+}
+template <int N>
+__device__ __forceinline__ void write_run(float* to, const float* v) {
+    if constexpr (N == 4) {
+        *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) to[k] = v[k];
+    }
+}
+
 // Workspace: per thread block two slots of [3][channels] sums (its first modulation row, and its last one where that is
 // another) that are not complete inside the block, then [3][channels] of sums for the weights' gradients.
 __device__ __forceinline__ float* slot_of(const BlockNormParams& p, int cta, int which) {
@@ -452,25 +542,24 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
     const bool want_mod = p.dscale || p.dshift || p.dgate;
     const bool normed = p.norm != 0, branch = p.y != nullptr, more = p.dx_out != nullptr;
     const uint32_t mine = smem_u32(ring_mem), ring_end = mine + ring.stages * ring.bytes;
-    Rows<TX, VEC, 0, MAXT> xs(p.x, p.x_stride, row0, at, p.channels);
-    Rows<TIO, VEC, kMine<TX>, MAXT> hs(p.dh, p.h_stride, row0, at, p.channels);
-    Rows<TX, VEC, kMine<TX> + kMine<TIO>, MAXT> ds(p.dx_out, p.dx_out_stride, row0, at, p.channels);
-    Rows<TIO, VEC, 2 * kMine<TX> + kMine<TIO>, MAXT> ys(p.y, p.y_stride, row0, at, p.channels);
+    uint32_t used = 0;
+    Rows<TX, VEC, 0, MAXT> xs(p.x, p.x_stride, row0, at, p, used);
+    Rows<TIO, VEC, kMine<TX>, MAXT> hs(p.dh, p.h_stride, row0, at, p, used);
+    Rows<TX, VEC, kMine<TX> + kMine<TIO>, MAXT> ds(p.dx_out, p.dx_out_stride, row0, at, p, used);
+    Rows<TIO, VEC, 2 * kMine<TX> + kMine<TIO>, MAXT> ys(p.y, p.y_stride, row0, at, p, used);
     Results<TX, VEC> dxo(p.dx, p.dx_stride, row0, at);
     Results<TIO, VEC> dyo(p.dy, p.dy_stride, row0, at);
     int ahead = row0;     // next row to fetch
     auto fetch = [&](uint32_t record) {
-        if constexpr (VEC) {
-            if (ahead++ < row1) {
-                if (normed) {
-                    xs.fetch(at, record);
-                    hs.fetch(at, record);
-                }
-                if (more) ds.fetch(at, record);
-                if (branch) ys.fetch(at, record);
+        if (ahead++ < row1) {
+            if (normed) {
+                xs.fetch(at, record);
+                hs.fetch(at, record);
             }
-            copy_commit();
+            if (more) ds.fetch(at, record);
+            if (branch) ys.fetch(at, record);
         }
+        copy_commit();
     };
     for (int s = 0; s < ring.stages - 1; ++s) fetch(mine + s * ring.bytes);
 
@@ -502,10 +591,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
             keep<MAXT>(g_mem, w);
         }
         for (; row < end; ++row) {
-            if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();   // all lanes have read what is filled again
-            fetch(before);
-            if constexpr (VEC) copy_wait(ring.stages);
-            if constexpr (VEC && sizeof(TX) + sizeof(TIO) > 4) __syncwarp();
+            next_row<VEC, sizeof(TX) + sizeof(TIO) <= 4>(fetch, before, ring.stages);
             f32x2 d[kPairs], v[kPairs];
             float y_mean = 0.0f, y_r = 1.0f;
             if (normed || p.post_norm) {
@@ -624,31 +710,58 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
         if (want_w || want_mod) {
             float* slot = slot_of(p, blockIdx.x, mod == first_mod ? 0 : 1);
             float* wslot = slot_of(p, blockIdx.x, 2);
-            float e0[kCols], e1[kCols], e2[kCols];
+            constexpr int kRun = VEC ? 4 : 1;   // neighbouring columns written at a time
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                unpack2(s0[i], e0[2 * i], e0[2 * i + 1]);
-                unpack2(s1[i], e1[2 * i], e1[2 * i + 1]);
-                unpack2(s2[i], e2[2 * i], e2[2 * i + 1]);
-            }
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) {
+            for (int i = 0; i < kCols; i += kRun) {
                 if (!at.on(i)) continue;
                 const int c = at.col(i);
+                float e0[kRun], e1[kRun], e2[kRun];
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) {
+                    float lo, hi;
+                    unpack2(s0[(i + k) / 2], lo, hi);
+                    e0[k] = (i + k) % 2 ? hi : lo;
+                    unpack2(s1[(i + k) / 2], lo, hi);
+                    e1[k] = (i + k) % 2 ? hi : lo;
+                    unpack2(s2[(i + k) / 2], lo, hi);
+                    e2[k] = (i + k) % 2 ? hi : lo;
+                }
                 if (want_w) {   // this thread's own columns of this block's own slot
-                    const float s = p.scale ? 1.0f + p.scale[from + c] : 1.0f;
-                    const float gate = p.gate ? p.gate[from + c] : 1.0f;
-                    wslot[c] = fmaf(s, e1[i], first_flush ? 0.0f : wslot[c]);
-                    wslot[p.channels + c] = fmaf(s, e0[i], first_flush ? 0.0f : wslot[p.channels + c]);
-                    wslot[2 * p.channels + c] = fmaf(gate, e2[i], first_flush ? 0.0f : wslot[2 * p.channels + c]);
+                    float s[kRun], gate[kRun], o0[kRun], o1[kRun], o2[kRun];
+                    read_run<kRun>(p.scale ? p.scale + from + c : nullptr, 0.0f, s);
+                    read_run<kRun>(p.gate ? p.gate + from + c : nullptr, 1.0f, gate);
+                    read_run<kRun>(first_flush ? nullptr : wslot + c, 0.0f, o0);
+                    read_run<kRun>(first_flush ? nullptr : wslot + p.channels + c, 0.0f, o1);
+                    read_run<kRun>(first_flush ? nullptr : wslot + 2 * p.channels + c, 0.0f, o2);
+#pragma unroll
+                    for (int k = 0; k < kRun; ++k) {
+                        o0[k] += fmaf(s[k], e1[k], e1[k]);
+                        o1[k] += fmaf(s[k], e0[k], e0[k]);
+                        o2[k] = fmaf(gate[k], e2[k], o2[k]);
+                    }
+                    write_run<kRun>(wslot + c, o0);
+                    write_run<kRun>(wslot + p.channels + c, o1);
+                    write_run<kRun>(wslot + 2 * p.channels + c, o2);
                 }
                 if (!want_mod) continue;
                 if (complete) {
-                    write_mod_grads(p, mod, c, e0[i], e1[i], e2[i]);
+                    const long long to = (long long)mod * p.channels + c;
+                    float w[kRun], b[kRun], pw[kRun];
+                    read_run<kRun>(p.weight ? p.weight + c : nullptr, 1.0f, w);
+                    read_run<kRun>(p.bias ? p.bias + c : nullptr, 0.0f, b);
+                    read_run<kRun>(p.post_weight ? p.post_weight + c : nullptr, 1.0f, pw);
+                    if (p.dshift) write_run<kRun>(p.dshift + to, e0);
+#pragma unroll
+                    for (int k = 0; k < kRun; ++k) {
+                        e1[k] = fmaf(w[k], e1[k], b[k] * e0[k]);
+                        e2[k] *= pw[k];
+                    }
+                    if (p.dscale) write_run<kRun>(p.dscale + to, e1);
+                    if (p.dgate) write_run<kRun>(p.dgate + to, e2);
                 } else {
-                    slot[c] = e0[i];
-                    slot[p.channels + c] = e1[i];
-                    slot[2 * p.channels + c] = e2[i];
+                    write_run<kRun>(slot + c, e0);
+                    write_run<kRun>(slot + p.channels + c, e1);
+                    write_run<kRun>(slot + 2 * p.channels + c, e2);
                 }
             }
             first_flush = false;
@@ -733,8 +846,7 @@ cudaError_t plan(BlockNormParams* p, K kernel, int threads, size_t smem, int sm_
 
 // Stages: as many as fit a share of the SM's shared memory (for about `threads_wanted` threads on it), two to four; one
 // where two rows do not fit an SM (fp32 gradients of more than 7000 channels).
-Ring plan_ring(bool vec, uint32_t stage_bytes, uint32_t other_bytes, int threads, int threads_wanted) {
-    if (!vec) return Ring{1, 0};
+Ring plan_ring(uint32_t stage_bytes, uint32_t other_bytes, int threads, int threads_wanted) {
     const int blocks = threads_wanted / threads > 1 ? threads_wanted / threads : 1;
     int stages = (int)((224000u / blocks - other_bytes) / stage_bytes);
     if (stages < 2) stages = 2 * stage_bytes + other_bytes <= 228000u ? 2 : 1;
@@ -745,7 +857,7 @@ Ring plan_ring(bool vec, uint32_t stage_bytes, uint32_t other_bytes, int threads
 template <typename TX, typename TIO, bool VEC, int MAXT>
 cudaError_t forward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     const int threads = threads_for(p.channels);
-    const Ring ring = plan_ring(VEC, MAXT * (kMine<TX> + kMine<TIO>), 0, threads, MAXT == 128 ? 480 : 320);
+    const Ring ring = plan_ring(VEC ? MAXT * (kMine<TX> + kMine<TIO>) : image_bytes(p.channels, sizeof(TX)) + image_bytes(p.channels, sizeof(TIO)), 0, threads, MAXT == 128 ? 480 : 320);
     const size_t smem = (size_t)ring.stages * ring.bytes;
     const cudaError_t e = plan(&p, block_norm_forward_kernel<TX, TIO, VEC, MAXT>, threads, smem, sm_count, 1 << 30, ctas);
     if (e != cudaSuccess) return e;
@@ -755,7 +867,7 @@ cudaError_t forward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_
 template <typename TX, typename TIO, bool VEC, int MAXT>
 cudaError_t backward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     const int threads = threads_for(p.channels);
-    const Ring ring = plan_ring(VEC, MAXT * 2 * (kMine<TX> + kMine<TIO>), 2 * kMine<float> * MAXT, threads, 384);
+    const Ring ring = plan_ring(VEC ? MAXT * 2 * (kMine<TX> + kMine<TIO>) : 2 * (image_bytes(p.channels, sizeof(TX)) + image_bytes(p.channels, sizeof(TIO))), 2 * kMine<float> * MAXT, threads, 384);
     const size_t smem = (size_t)ring.stages * ring.bytes + 2 * kMine<float> * MAXT;
     const cudaError_t e = plan(&p, block_norm_backward_kernel<TX, TIO, VEC, MAXT>, threads, smem, sm_count, kNormMaxCtas, ctas);
     if (e != cudaSuccess) return e;

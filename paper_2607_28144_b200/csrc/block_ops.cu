@@ -431,17 +431,17 @@ int regenvc_mxfp4_project(const void* x_packed, const void* w_packed, const void
     int sm_count = 0, *status = nullptr;
     rc = op_device(&sm_count, &status);
     if (rc != REGENVC_OK) return rc;
-    if (mxfp4_rows_fits(n_tokens, MxLayout(n_tokens, in_features).cols_pad))
+    if (mxfp4_rows_fits(n_tokens, out_features, MxLayout(n_tokens, in_features).cols_pad))
         return mx_rows(x_packed, REGENVC_BF16, -1, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count,
                        (cudaStream_t)stream);
     return mx_project(x_packed, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count, status,
                       (cudaStream_t)stream);
 }
 
-size_t regenvc_mxfp4_linear_scratch_bytes(int n_tokens, int in_features) {
-    if (!mx_shape_ok(n_tokens, in_features)) return 0;
+size_t regenvc_mxfp4_linear_scratch_bytes(int n_tokens, int out_features, int in_features) {
+    if (!mx_shape_ok(n_tokens, in_features) || !mx_shape_ok(out_features, in_features)) return 0;
     const MxLayout l(n_tokens, in_features);
-    return mxfp4_rows_fits(n_tokens, l.cols_pad) ? 0 : (size_t)l.bytes;
+    return mxfp4_rows_fits(n_tokens, out_features, l.cols_pad) ? 0 : (size_t)l.bytes;
 }
 
 int regenvc_mxfp4_linear(const void* x, int x_type, long long x_stride, const void* w_packed, const void* bias, void* y,
@@ -451,7 +451,7 @@ int regenvc_mxfp4_linear(const void* x, int x_type, long long x_stride, const vo
     if (rc != REGENVC_OK) return rc;
     if (!type_ok(x_type)) return REGENVC_ERR_UNSUPPORTED;
     if (x_stride != 0 && (x_stride < in_features || x_stride > kMaxStride)) return REGENVC_ERR_BAD_SHAPE;
-    const bool few = mxfp4_rows_fits(n_tokens, MxLayout(n_tokens, in_features).cols_pad);
+    const bool few = mxfp4_rows_fits(n_tokens, out_features, MxLayout(n_tokens, in_features).cols_pad);
     if (!few && !scratch) return REGENVC_ERR_NULL_POINTER;
     if (!aligned(x, type_size(x_type)) || (!few && !aligned(scratch, 256))) return REGENVC_ERR_MISALIGNED;
     const Span xs = rows_span(x, n_tokens, x_stride ? x_stride : in_features, in_features, type_size(x_type));

@@ -65,7 +65,7 @@ struct MxRowsParams {
     int vec;                  // x's address and stride allow 16-byte accesses
     int y_f16;
 };
-bool mxfp4_rows_fits(int n_tokens, long long cols_pad);
+bool mxfp4_rows_fits(int n_tokens, int features, long long cols_pad);
 cudaError_t launch_mxfp4_rows(const MxRowsParams& p, int type, bool packed, int sm_count, cudaStream_t stream);
 
 }  // namespace regenvc

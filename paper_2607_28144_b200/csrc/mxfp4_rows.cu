@@ -1,10 +1,12 @@
-// Product of a few rows with a 4-bit matrix, y = Q(x) w^T + b for up to four tokens: the modulation rows of a denoising
-// step, embeddings, single tokens.  x is quantised in the kernel (or read packed), so such a call is one launch.
+// Product of a few rows with a 4-bit matrix, y = Q(x) w^T + b: the modulation row of a denoising step, embeddings, single
+// tokens (and up to four where the matrix is small).  x is quantised in the kernel (or read packed), so such a call is one
+// launch.
 //
-// Bound: the weights' bytes from HBM (17 / 32 byte per weight), and at small sizes the launch itself; the tensor
-// instruction would compute 128 rows for one.  Every thread block first takes all of x to e2m1 values (as fp16, which
-// holds them) in shared memory.  A half warp then owns FP output features: a lane reads 16 bytes = one block of 32
-// weights per feature, all of its loads in flight at a time.  Sixteen products are summed in packed fp16 -- exactly:
+// Bound: the weights' bytes from HBM (17 / 32 byte per weight), and at small sizes the launch itself.  For more than one
+// token and 2^24 weights or more the tensor-core product takes over, although it computes 128 rows (2 x 5120 -> 15360: 23
+// against 46 us; 4 x 5120 -> 5120: 19 against 21 us).  Every thread block first takes all of x to e2m1 values (as fp16,
+// which holds them) in shared memory, while its first weights are on their way.  A half warp then walks over groups of FP
+// output features: a lane reads 16 bytes = one block of 32 weights per feature, up to eight of them in flight at a time.  Sixteen products are summed in packed fp16 -- exactly:
 // products of two e2m1 values are multiples of 1/4 up to 36, and eight of them in one half of a pair stay below 2^11
 // quarters -- then joined in fp32 and scaled by the two blocks' powers of two.
 #include "common.cuh"
@@ -51,6 +53,26 @@ __global__ void __launch_bounds__(kThreads) mxfp4_rows_kernel(const MxRowsParams
     uint4* xv = smem4;
     uint8_t* xscale = reinterpret_cast<uint8_t*>(smem4 + (size_t)MR * 4 * blocks);   // [MR][blocks]
     const int lane = threadIdx.x & 15;
+
+    constexpr int kAhead = 8 / FP;   // blocks per lane and feature in flight
+    uint4 q[kAhead][FP];
+    uint32_t s[kAhead][FP];
+    int f0 = (blockIdx.x * kHalfWarps + (threadIdx.x >> 4)) * FP;   // features is a multiple of 8, so of FP
+    auto load = [&](int b0) {
+        const uint8_t* codes = p.w + (long long)f0 * (p.cols_pad / 2);
+        const uint8_t* scales = p.w + p.w_scale_at + (long long)(f0 / 128) * (p.cols_pad / 128) * 512 + f0 % 32 * 16 + f0 % 128 / 32 * 4;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int b = b0 + 16 * k;
+            if (b < blocks)
+#pragma unroll
+                for (int f = 0; f < FP; ++f) {   // the FP rows lie in one tile of scales: f0 is a multiple of FP
+                    q[k][f] = __ldg(reinterpret_cast<const uint4*>(codes + (long long)f * (p.cols_pad / 2)) + b);
+                    s[k][f] = __ldg(scales + (long long)(b / 4) * 512 + f * 16 + b % 4);
+                }
+        }
+    };
+    if (f0 < p.features) load(lane);
 
     if constexpr (sizeof(T) == 1) {   // Packed
         const uint8_t* codes = reinterpret_cast<const uint8_t*>(p.x);
@@ -99,30 +121,14 @@ __global__ void __launch_bounds__(kThreads) mxfp4_rows_kernel(const MxRowsParams
     }
     __syncthreads();
 
-    const int f0 = (blockIdx.x * kHalfWarps + (threadIdx.x >> 4)) * FP;   // features is a multiple of 8, so of FP
-    const bool on = f0 < p.features;
-    float acc[FP][MR];
+    while (f0 < p.features) {
+        float acc[FP][MR];
 #pragma unroll
-    for (int f = 0; f < FP; ++f)
+        for (int f = 0; f < FP; ++f)
 #pragma unroll
-        for (int m = 0; m < MR; ++m) acc[f][m] = 0.0f;
-    if (on) {
-        const uint8_t* codes = p.w + (long long)f0 * (p.cols_pad / 2);
-        const uint8_t* scales = p.w + p.w_scale_at + (long long)(f0 / 128) * (p.cols_pad / 128) * 512 + f0 % 32 * 16 + f0 % 128 / 32 * 4;
-        constexpr int kAhead = FP == 1 ? 6 : 3;   // blocks per lane in flight
-        for (int b0 = lane; b0 < blocks; b0 += 16 * kAhead) {
-            uint4 q[kAhead][FP];
-            uint32_t s[kAhead][FP];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int b = b0 + 16 * k;
-                if (b < blocks)
-#pragma unroll
-                    for (int f = 0; f < FP; ++f) {   // the FP rows lie in one tile of scales: f0 is a multiple of FP
-                        q[k][f] = __ldg(reinterpret_cast<const uint4*>(codes + (long long)f * (p.cols_pad / 2)) + b);
-                        s[k][f] = __ldg(scales + (long long)(b / 4) * 512 + f * 16 + b % 4);
-                    }
-            }
+            for (int m = 0; m < MR; ++m) acc[f][m] = 0.0f;
+        for (int b0 = lane; b0 - lane < blocks; b0 += 16 * kAhead) {
+            if (b0 != lane) load(b0);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const int b = b0 + 16 * k;
@@ -149,50 +155,64 @@ __global__ void __launch_bounds__(kThreads) mxfp4_rows_kernel(const MxRowsParams
                 }
             }
         }
-    }
+        const int done = f0;
+        f0 += gridDim.x * kHalfWarps * FP;
+        if (f0 < p.features) load(lane);   // the next features' first weights, in flight during the sums
+        // (the sixteen lanes of a half warp are here together; the other half may have left the loop)
+        const uint32_t mates = 0xFFFFu << (threadIdx.x & 16);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1)
+        for (int o = 8; o > 0; o >>= 1)
 #pragma unroll
-        for (int f = 0; f < FP; ++f)
+            for (int f = 0; f < FP; ++f)
 #pragma unroll
-            for (int m = 0; m < MR; ++m) acc[f][m] += __shfl_xor_sync(0xffffffffu, acc[f][m], o);
-    if (!on || lane != 0) return;
+                for (int m = 0; m < MR; ++m) acc[f][m] += __shfl_xor_sync(mates, acc[f][m], o);
+        if (lane != 0) continue;
 #pragma unroll
-    for (int m = 0; m < MR; ++m) {
-        if (m >= p.n_tokens) continue;
+        for (int m = 0; m < MR; ++m) {
+            if (m >= p.n_tokens) continue;
 #pragma unroll
-        for (int f = 0; f < FP; ++f) {
-            const float r = acc[f][m] + (p.bias ? p.bias[f0 + f] : 0.0f);
-            const long long at = (long long)m * p.features + f0 + f;
-            if (p.y_f16) reinterpret_cast<__half*>(p.y)[at] = __float2half_rn(r);
-            else reinterpret_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(r);
+            for (int f = 0; f < FP; ++f) {
+                const float r = acc[f][m] + (p.bias ? p.bias[done + f] : 0.0f);
+                const long long at = (long long)m * p.features + done + f;
+                if (p.y_f16) reinterpret_cast<__half*>(p.y)[at] = __float2half_rn(r);
+                else reinterpret_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(r);
+            }
         }
     }
 }
 
 template <typename T, int MR, int FP>
-cudaError_t launch_one(const MxRowsParams& p, cudaStream_t stream) {
+cudaError_t launch_one(const MxRowsParams& p, int sm_count, cudaStream_t stream) {
     const size_t smem = (size_t)MR * (p.cols_pad * 2 + p.cols_pad / 32);
     if (smem > 48000) {
         const cudaError_t e = cudaFuncSetAttribute(mxfp4_rows_kernel<T, MR, FP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
     const int per_block = kHalfWarps * FP;
-    mxfp4_rows_kernel<T, MR, FP><<<(unsigned)((p.features + per_block - 1) / per_block), kThreads, smem, stream>>>(p);
+    int blocks = (p.features + per_block - 1) / per_block;
+    if (blocks > sm_count) {   // no more than the device holds at a time: every block quantises x once
+        int per_sm = 1;
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, mxfp4_rows_kernel<T, MR, FP>, kThreads, smem);
+        if (e != cudaSuccess) return e;
+        if (per_sm < 1) per_sm = 1;
+        if (blocks > per_sm * sm_count) blocks = per_sm * sm_count;
+    }
+    mxfp4_rows_kernel<T, MR, FP><<<(unsigned)blocks, kThreads, smem, stream>>>(p);
     return cudaGetLastError();
 }
 template <typename T>
 cudaError_t launch_typed(const MxRowsParams& p, int sm_count, cudaStream_t stream) {
-    // four features per half warp once that still gives three quarters of the SMs a block
-    const bool wide = (long long)p.features * 4 >= 3ll * sm_count * kHalfWarps * 4;
-    if (p.n_tokens == 1) return wide ? launch_one<T, 1, 4>(p, stream) : launch_one<T, 1, 1>(p, stream);
-    return wide ? launch_one<T, 4, 4>(p, stream) : launch_one<T, 4, 1>(p, stream);
+    if (p.n_tokens > 1) return launch_one<T, 4, 1>(p, sm_count, stream);
+    // two features per half warp once that still gives every SM a block
+    if (p.features >= 2 * kHalfWarps * sm_count) return launch_one<T, 1, 2>(p, sm_count, stream);
+    return launch_one<T, 1, 1>(p, sm_count, stream);
 }
 
 }  // namespace
 
-bool mxfp4_rows_fits(int n_tokens, long long cols_pad) {
-    return n_tokens <= kMxFewRows && (n_tokens == 1 ? 1 : 4) * (cols_pad * 2 + cols_pad / 32) <= 160 * 1024;
+bool mxfp4_rows_fits(int n_tokens, int features, long long cols_pad) {
+    if (n_tokens > kMxFewRows || (n_tokens > 1 && features * cols_pad >= 1ll << 24)) return false;
+    return (n_tokens == 1 ? 1 : 4) * (cols_pad * 2 + cols_pad / 32) <= 160 * 1024;
 }
 
 cudaError_t launch_mxfp4_rows(const MxRowsParams& p, int type, bool packed, int sm_count, cudaStream_t stream) {

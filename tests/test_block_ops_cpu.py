@@ -159,9 +159,10 @@ def test_mxfp4_sizes_and_refusals(L):
     assert p(A[0], A[1], None, A[0], 0, 4, 8, 32, None) == B.ERR_ALIASING
     assert p(A[0], A[1], A[2] + 32, A[2], 0, 4, 8, 32, None) == B.ERR_ALIASING
     s = B.regenvc_mxfp4_linear_scratch_bytes
-    assert s(1, 80640) == 0 and s(1, 80641) == B.regenvc_mxfp4_bytes(1, 80641)
-    assert s(4, 20096) == 0 and s(4, 20097) == B.regenvc_mxfp4_bytes(4, 20097)
-    assert s(5, 32) == B.regenvc_mxfp4_bytes(5, 32) and s(0, 32) == 0
+    assert s(1, 8, 80640) == 0 and s(1, 8, 80641) == B.regenvc_mxfp4_bytes(1, 80641)
+    assert s(4, 8, 20096) == 0 and s(4, 8, 20097) == B.regenvc_mxfp4_bytes(4, 20097)
+    assert s(1, 1 << 17, 4096) == 0 and s(2, 4096, 4096) == B.regenvc_mxfp4_bytes(2, 4096) and s(2, 4088, 4096) == 0
+    assert s(5, 8, 32) == B.regenvc_mxfp4_bytes(5, 32) and s(0, 8, 32) == 0 and s(1, 0, 32) == 0
     f = L.regenvc_mxfp4_linear
     assert f(None, 0, 0, A[1], None, A[2], 0, 4, 8, 32, None, None) == B.ERR_NULL_POINTER
     assert f(A[0], 0, 0, A[1], None, A[2], 0, 5, 8, 32, None, None) == B.ERR_NULL_POINTER
