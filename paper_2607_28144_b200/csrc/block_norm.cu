@@ -357,24 +357,39 @@ __device__ __forceinline__ void normalise(f32x2* v, int kind, float eps, const C
     for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], r);
 }
 
-// A vector of this thread's columns kept in shared memory (only this thread reads and writes it).
-template <int MAXT>
-__device__ __forceinline__ void keep(float4* mem, const f32x2* v) {
+// A vector of this thread's columns that the gradients' rows share: in shared memory (only this thread reads and writes
+// it), or in registers in the build of 160 to 320 threads, which has one block per SM, registers to spare and, without
+// these 40 KB, room for a third row ahead (12480 x 5120 sandwich: 333 -> 321 us).
+template <int MAXT, bool REGS>
+struct Kept {
+    float4* mem;
+    __device__ __forceinline__ void set(const f32x2* v) {
 #pragma unroll
-    for (int i = 0; i < kPairs / 2; ++i) {
-        float4 q;
-        unpack2(v[2 * i], q.x, q.y);
-        unpack2(v[2 * i + 1], q.z, q.w);
-        mem[i * MAXT + threadIdx.x] = q;
+        for (int i = 0; i < kPairs / 2; ++i) {
+            float4 q;
+            unpack2(v[2 * i], q.x, q.y);
+            unpack2(v[2 * i + 1], q.z, q.w);
+            mem[i * MAXT + threadIdx.x] = q;
+        }
     }
-}
+    __device__ __forceinline__ void get(int i, f32x2* a, f32x2* b) const {   // pairs 2i and 2i + 1
+        const float4 q = mem[i * MAXT + threadIdx.x];
+        *a = pack2(q.x, q.y);
+        *b = pack2(q.z, q.w);
+    }
+};
 template <int MAXT>
-__device__ __forceinline__ void recall(const float4* mem, int i, f32x2* a, f32x2* b) {   // pairs 2i and 2i + 1
-    const float4 q = mem[i * MAXT + threadIdx.x];
-    *a = pack2(q.x, q.y);
-    *b = pack2(q.z, q.w);
-}
-
+struct Kept<MAXT, true> {
+    f32x2 r[kPairs];
+    __device__ __forceinline__ void set(const f32x2* v) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) r[i] = v[i];
+    }
+    __device__ __forceinline__ void get(int i, f32x2* a, f32x2* b) const {
+        *a = r[2 * i];
+        *b = r[2 * i + 1];
+    }
+};
 // The rows of up to four tensors copied ahead: `stages` rows' worth of shared memory in turn.  A stage is filled again one
 // row after it was read, behind that row's barriers.
 struct Ring {
@@ -524,14 +539,19 @@ __device__ __forceinline__ float* slot_of(const BlockNormParams& p, int cta, int
     return p.partials + ((long long)cta * 9 + which * 3) * p.channels;
 }
 
-// (w = weight (1 + scale) and g = gate post_weight live in shared memory: the registers hold three sums per column.)
+// w = weight (1 + scale), g = gate post_weight; the registers hold three sums per column.
 template <typename TX, typename TIO, bool VEC, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward_kernel(const BlockNormParams p, const Ring ring) {
     __shared__ alignas(16) float buf[2][4][16];
     extern __shared__ uint4 shared_mem[];
-    float4* w_mem = reinterpret_cast<float4*>(shared_mem);
-    float4* g_mem = w_mem + kCols / 4 * MAXT;
-    uint4* ring_mem = shared_mem + 2 * (kCols / 4) * MAXT;
+    constexpr bool kRegs = MAXT == 320;
+    Kept<MAXT, kRegs> w_kept, g_kept;
+    uint4* ring_mem = shared_mem;
+    if constexpr (!kRegs) {
+        w_kept.mem = reinterpret_cast<float4*>(shared_mem);
+        g_kept.mem = w_kept.mem + kCols / 4 * MAXT;
+        ring_mem += 2 * (kCols / 4) * MAXT;
+    }
     BlockSum sum = block_sum_init(buf);
     const Place<VEC> at(p.channels);
     const Channels ch(p.channels);
@@ -580,7 +600,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
             read_vector<VEC>(p.scale ? p.scale + from : nullptr, 0.0f, at, t);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) w[i] = fma2(w[i], t[i], w[i]);
-            keep<MAXT>(w_mem, w);
+            w_kept.set(w);
             read_vector<VEC>(p.gate ? p.gate + from : nullptr, 1.0f, at, w);
             read_vector<VEC>(p.post_weight, 1.0f, at, t);
 #pragma unroll
@@ -588,7 +608,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
                 w[i] = mul2(w[i], t[i]);
                 s0[i] = s1[i] = s2[i] = 0ull;
             }
-            keep<MAXT>(g_mem, w);
+            g_kept.set(w);
         }
         for (; row < end; ++row) {
             next_row<VEC, sizeof(TX) + sizeof(TIO) <= 4>(fetch, before, ring.stages);
@@ -620,7 +640,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
 #pragma unroll
                     for (int i = 0; i < kPairs; i += 2) {
                         f32x2 w0, w1;
-                        recall<MAXT>(w_mem, i / 2, &w0, &w1);
+                        w_kept.get(i / 2, &w0, &w1);
                         w0 = mul2(d[i], w0);
                         w1 = mul2(d[i + 1], w1);
                         ta = add2(ta, add2(w0, w1));
@@ -635,7 +655,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
 #pragma unroll
                     for (int i = 0; i < kPairs; i += 2) {
                         f32x2 wi[2];
-                        recall<MAXT>(w_mem, i / 2, &wi[0], &wi[1]);
+                        w_kept.get(i / 2, &wi[0], &wi[1]);
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
                             s0[i + k] = add2(s0[i + k], d[i + k]);
@@ -676,7 +696,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward
 #pragma unroll
                 for (int i = 0; i < kPairs; i += 2) {
                     f32x2 g0, g1;
-                    recall<MAXT>(g_mem, i / 2, &g0, &g1);
+                    g_kept.get(i / 2, &g0, &g1);
                     s2[i] = fma2(d[i], v[i], s2[i]);
                     s2[i + 1] = fma2(d[i + 1], v[i + 1], s2[i + 1]);
                     d[i] = mul2(d[i], g0);
@@ -867,8 +887,9 @@ cudaError_t forward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_
 template <typename TX, typename TIO, bool VEC, int MAXT>
 cudaError_t backward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     const int threads = threads_for(p.channels);
-    const Ring ring = plan_ring(VEC ? MAXT * 2 * (kMine<TX> + kMine<TIO>) : 2 * (image_bytes(p.channels, sizeof(TX)) + image_bytes(p.channels, sizeof(TIO))), 2 * kMine<float> * MAXT, threads, 384);
-    const size_t smem = (size_t)ring.stages * ring.bytes + 2 * kMine<float> * MAXT;
+    constexpr uint32_t kept = MAXT == 320 ? 0 : 2 * kMine<float> * MAXT;
+    const Ring ring = plan_ring(VEC ? MAXT * 2 * (kMine<TX> + kMine<TIO>) : 2 * (image_bytes(p.channels, sizeof(TX)) + image_bytes(p.channels, sizeof(TIO))), kept, threads, 384);
+    const size_t smem = (size_t)ring.stages * ring.bytes + kept;
     const cudaError_t e = plan(&p, block_norm_backward_kernel<TX, TIO, VEC, MAXT>, threads, smem, sm_count, kNormMaxCtas, ctas);
     if (e != cudaSuccess) return e;
     block_norm_backward_kernel<TX, TIO, VEC, MAXT><<<*ctas, threads, smem, stream>>>(p, ring);
