@@ -8,12 +8,16 @@
 //               (tiles of 512 bytes, no swizzle), all counted on the stage's barrier
 //   warp 1      copies the scales of a stage to tensor memory (tcgen05.cp, replicated to the four lane groups), issues
 //               the MMAs and commits
-//   warps 2-9   epilogue: accumulator -> + bias -> 16 bits -> swizzled staging tile -> tiled store
+//   warps 2-9   epilogue: accumulator -> + bias -> 16 bits -> swizzled staging block -> tiled store, in two halves that work
+//               on alternate blocks of 64 columns (as one group with one staging tile the epilogue was the longest part of
+//               an item at inner extents of 1536: 10920 x 1536 -> 4608 took 49 us instead of 43.5)
 // Two accumulators of NT columns, used in turn, the scales behind them.
 //
 // Bound: the operands' way from L2.  All CTAs together take about 11.7 TB/s (45 bytes per SM and cycle), and a pair's
 // 256 x 192 tile needs 31 KB per CTA for 384 cycles of tensor work, a 256 x 256 tile 35 KB for 512: at 31200 x 5120 x
-// 15360 the two take 1.02 and 0.9x ms, single CTAs (43 KB for 128 x 192) 1.33 ms.
+// 15360 the two take 1.02 and 0.93 ms, single CTAs (43 KB for 128 x 192) 1.33 ms.  (Keeping a tile's weights in shared
+// memory while the tokens go by, possible up to inner extents of 1536, halves those bytes there but leaves room for three
+// stages only: 47.6 us.)
 #include "common.cuh"
 #include "cta_pair.cuh"
 #include "mxfp4.cuh"
@@ -37,9 +41,8 @@ struct Cfg {
     static constexpr uint32_t kCodesB = NT / CG * kRowBytes;   // this CTA's share of the weight rows
     static constexpr uint32_t kStage = kCodesA + kCodesB + kScalesA + kScalesB;
     static constexpr uint32_t kOutBlock = kTile * 64 * 2;      // [128 tokens][64 features] 16-bit, staged for TMA
-    static constexpr uint32_t kOut = NT / 64 * kOutBlock;
+    static constexpr uint32_t kOut = (NT > 64 ? 4 : 2) * kOutBlock;   // two slots for each half of the epilogue warps
     static constexpr int kStages = (int)((232448 - 4096 - kOut) / kStage) < 6 ? (int)((232448 - 4096 - kOut) / kStage) : 6;
-    static constexpr int kColsHalf = NT / 2;                   // accumulator columns per epilogue thread
     // Tensor-memory columns: two accumulators used in turn, then two sets of scales.  Two of 256 columns and the scales do
     // not fit 512 columns: the accumulators then share 48 columns, which an epilogue reads out first.
     static constexpr bool kShare = 2 * NT + 2 * kScaleColumns > 512;
@@ -106,7 +109,16 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
     }
 }
 
-__device__ __forceinline__ void epi_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory"); }
+// The 128 threads of one half of the epilogue warps.
+__device__ __forceinline__ void epi_barrier(int half) { asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory"); }
+// All of this thread's stores but the last have read their shared memory.
+__device__ __forceinline__ void tma_store_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+// One arrival of a warp that has read an accumulator out (the barrier that counts is the leader's).
+template <int CG>
+__device__ __forceinline__ void release_accumulator(uint64_t* bar) {
+    if constexpr (CG == 2) mbar_arrive_peer(map_to_rank(smem_u32(bar), 0));
+    else mbar_arrive(smem_u32(bar));
+}
 
 template <int CG, int NT>
 __global__ void __launch_bounds__(kThreadsMx, 1)
@@ -235,44 +247,54 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
         }
     } else {
         // ------------------------------------------------------------ epilogue warps
+        // Blocks of 64 columns; the four warps of half h (128 threads, one per accumulator row) take blocks h, h + 2, ...
+        // on their own, through two staging slots in turn: a slot is written again once the store before last has read it.
         const int half = (warp - 2) >> 2;
         const int row = (warp & 3) * 32 + lane;       // accumulator row = TMEM lane
-        const int et = tid - 64;
+        const int et = (tid - 64) & 127;
+        constexpr int kBlocks = NT / 64;
+        const int mine = (kBlocks - half + 1) / 2;    // blocks of this half
+        float* bias = sh->bias + half * 128;
+        uint8_t* slots = stage_out + half * 2 * C::kOutBlock;
         bool ok = true;
-        int it = 0;
+        int it = 0, used = 0;
         for (int slice = slice0; slice < n_slices; slice += slice_step, ++it) {
             const int f0 = slice % n_rank * NT, b = it & 1;
             const int tile = CG * (slice / n_rank) + rank;
-            const uint32_t t_acc = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + b * C::kAccStep + half * C::kColsHalf;
-            if (et < NT) sh->bias[et] = p.bias && f0 + et < p.features ? __ldg(p.bias + f0 + et) : 0.0f;
-            if (tid == 64) tma_store_wait_read();
-            epi_barrier();
+            const uint32_t t_acc = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + b * C::kAccStep;
+            if (et < mine * 64) {   // (the slice before's readers are past the barrier behind their last block)
+                const int f = f0 + (half + et / 64 * 2) * 64 + et % 64;
+                bias[et] = p.bias && f < p.features ? __ldg(p.bias + f) : 0.0f;
+            }
             if (ok) ok = mbar_wait(smem_u32(&sh->acc_full[b]), (it >> 1) & 1, ctl);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
+            if (mine == 0 && lane == 0) release_accumulator<CG>(&sh->acc_empty[b]);
 #pragma unroll 1
-            for (int i = 0; i < C::kColsHalf / 32; ++i) {
-                // accumulator 0 shares its last columns, accumulator 1 its first ones: those of this half go first
-                const int cb = C::kShare && b == 0 ? C::kColsHalf / 32 - 1 - i : i;
-                uint32_t a[32];
+            for (int i = 0; i < mine; ++i, ++used) {
+                // accumulator 0 shares its last columns with the other one, accumulator 1 its first: those go first
+                const int k = C::kShare && b == 0 ? mine - 1 - i : i;
+                const int col = (half + 2 * k) * 64;
+                uint32_t a[64];
                 if (ok) {
-                    tmem_ld32(t_acc + cb * 32, a);
+                    tmem_ld32(t_acc + col, a);
+                    tmem_ld32(t_acc + col + 32, a + 32);
                     tmem_wait_ld();
                 }
-                if (i == (C::kShare ? 1 : C::kColsHalf / 32 - 1)) {
-                    // this warp's part of what the next MMAs overwrite is in registers (all of the accumulator, or 64 of
-                    // its columns, and those of the slice before were finished earlier)
+                if (i == (C::kShare ? 0 : mine - 1)) {
+                    // this warp's part of what the next MMAs overwrite is in registers: all of the accumulator, or the
+                    // shared columns (and the slice before's accumulator was finished earlier)
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 2) mbar_arrive_peer(map_to_rank(smem_u32(&sh->acc_empty[b]), 0));
-                        else mbar_arrive(smem_u32(&sh->acc_empty[b]));
-                    }
+                    if (lane == 0) release_accumulator<CG>(&sh->acc_empty[b]);
                 }
-                const float4* b4 = reinterpret_cast<const float4*>(sh->bias + half * C::kColsHalf + cb * 32);
+                uint8_t* slot = slots + (used & 1) * C::kOutBlock;
+                if (et == 0) tma_store_wait_read_but_one();
+                epi_barrier(half);
 #pragma unroll
-                for (int c8 = 0; c8 < 4; ++c8) {
-                    const float4 b0 = b4[2 * c8], b1 = b4[2 * c8 + 1];
+                for (int c8 = 0; c8 < 8; ++c8) {
+                    const float4* b4 = reinterpret_cast<const float4*>(bias + k * 64 + c8 * 8);
+                    const float4 b0 = b4[0], b1 = b4[1];
                     const float v0 = __uint_as_float(a[c8 * 8 + 0]) + b0.x, v1 = __uint_as_float(a[c8 * 8 + 1]) + b0.y;
                     const float v2 = __uint_as_float(a[c8 * 8 + 2]) + b0.z, v3 = __uint_as_float(a[c8 * 8 + 3]) + b0.w;
                     const float v4 = __uint_as_float(a[c8 * 8 + 4]) + b1.x, v5 = __uint_as_float(a[c8 * 8 + 5]) + b1.y;
@@ -280,25 +302,18 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
                     const uint4 w = p.y_f16
                         ? make_uint4(pack_f16x2(v0, v1), pack_f16x2(v2, v3), pack_f16x2(v4, v5), pack_f16x2(v6, v7))
                         : make_uint4(pack_bf16x2(v0, v1), pack_bf16x2(v2, v3), pack_bf16x2(v4, v5), pack_bf16x2(v6, v7));
-                    const int col = half * C::kColsHalf + cb * 32 + c8 * 8;
-                    if (ok)
-                        *reinterpret_cast<uint4*>(stage_out + (col >> 6) * C::kOutBlock + sw128_offset(row, (col >> 3) & 7)) = w;
+                    if (ok) *reinterpret_cast<uint4*>(slot + sw128_offset(row, c8)) = w;
                 }
-            }
-            fence_proxy_async_smem();
-            epi_barrier();
-            if (tid == 64) {
-                if (ok && tile < n_tiles) {
+                fence_proxy_async_smem();
+                epi_barrier(half);
+                if (et == 0) {
                     // what lies past the last token or feature is dropped by the store
-#pragma unroll
-                    for (int i = 0; i < NT / 64; ++i)
-                        if (f0 + i * 64 < p.features)
-                            tma_store_2d(&tmap_y, f0 + i * 64, tile * kTile, smem_u32(stage_out + i * C::kOutBlock));
+                    if (ok && tile < n_tiles && f0 + col < p.features) tma_store_2d(&tmap_y, f0 + col, tile * kTile, smem_u32(slot));
                     tma_store_commit();
                 }
             }
         }
-        if (tid == 64) tma_store_wait_read();
+        if (et == 0) tma_store_wait_read();
         __syncwarp();
     }
 
@@ -346,7 +361,8 @@ cudaError_t launch_cfg(const CUtensorMap& x, const CUtensorMap& xs, const CUtens
 
 // Which build: the one with the least estimated time.  An item costs its operand bytes at what an SM can take (80 bytes
 // per cycle alone, 45 when all SMs load) and about 1500 cycles beside, more for wider epilogues; items run in rounds.
-// Measured (us, pairs 256 / pairs 192 / single 192 / single 64): see the table of sizes in the notes on this kernel.
+// (With pairs or 192-wide single items wherever there were enough of them and 64-wide ones elsewhere, 512 x 5120 -> 5120
+// took 27 us instead of 17 and 128 x 5120 -> 15360 24 instead of 15.)
 MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int in_features, int sm_count) {
     struct Build {
         MxProjectPlan plan;
