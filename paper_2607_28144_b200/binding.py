@@ -379,10 +379,10 @@ def _vector(t, name: str, size: int):
 
 def _modulation(n: int, c: int, tokens_per_mod, gate, scale, shift):
     """Checks the modulation tables and returns (tokens_per_mod, rows, row stride)."""
-    per = n if tokens_per_mod is None else int(tokens_per_mod)
+    most = max(n, 1)   # (no tokens at all: the library refuses that)
+    per = most if tokens_per_mod is None else min(int(tokens_per_mod), most)
     if per < 1:
         raise ValueError("tokens_per_mod must be at least 1")
-    per = min(per, n)
     rows = -(-n // per)
     stride = 0
     for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):

@@ -508,14 +508,18 @@ namespace regenvc {
 void count_launch() { launched(); }
 int record_cuda_failure(cudaError_t e, const char* what) { return cuda_fail(e, what); }
 int op_device(int* sm_count, int** status) {
-    std::lock_guard<std::mutex> lock(g_mu);
-    int dev = 0;
-    DeviceState* st = nullptr;
-    const int rc = device_state(&dev, &st);
-    if (rc != REGENVC_OK) return rc;
-    *sm_count = st->sm_count;
-    *status = st->status;
-    return REGENVC_OK;
+    try {
+        std::lock_guard<std::mutex> lock(g_mu);
+        int dev = 0;
+        DeviceState* st = nullptr;
+        const int rc = device_state(&dev, &st);
+        if (rc != REGENVC_OK) return rc;
+        *sm_count = st->sm_count;
+        *status = st->status;
+        return REGENVC_OK;
+    } catch (...) {   // out of host memory: no exception leaves a C entry point
+        return REGENVC_ERR_CUDA;
+    }
 }
 int encode_map(CUtensorMap* m, CUtensorMapDataType type, void* base, uint64_t inner, uint64_t outer, uint64_t row_bytes,
                uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swizzle) {
