@@ -541,7 +541,7 @@ __device__ __forceinline__ float* slot_of(const BlockNormParams& p, int cta, int
 
 // w = weight (1 + scale), g = gate post_weight; the registers hold three sums per column.
 template <typename TX, typename TIO, bool VEC, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_backward_kernel(const BlockNormParams p, const Ring ring) {
+__global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) block_norm_backward_kernel(const BlockNormParams p, const Ring ring) {
     __shared__ alignas(16) float buf[2][4][16];
     extern __shared__ uint4 shared_mem[];
     constexpr bool kRegs = MAXT == 320;
@@ -888,14 +888,15 @@ template <typename TX, typename TIO, bool VEC, int MAXT>
 cudaError_t backward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     const int threads = threads_for(p.channels);
     constexpr uint32_t kept = MAXT == 320 ? 0 : 2 * kMine<float> * MAXT;
-    const Ring ring = plan_ring(VEC ? MAXT * 2 * (kMine<TX> + kMine<TIO>) : 2 * (image_bytes(p.channels, sizeof(TX)) + image_bytes(p.channels, sizeof(TIO))), kept, threads, 384);
+    const Ring ring = plan_ring(VEC ? MAXT * 2 * (kMine<TX> + kMine<TIO>) : 2 * (image_bytes(p.channels, sizeof(TX)) + image_bytes(p.channels, sizeof(TIO))), kept, threads, MAXT == 96 ? 480 : 384);
     const size_t smem = (size_t)ring.stages * ring.bytes + kept;
     const cudaError_t e = plan(&p, block_norm_backward_kernel<TX, TIO, VEC, MAXT>, threads, smem, sm_count, kNormMaxCtas, ctas);
     if (e != cudaSuccess) return e;
     block_norm_backward_kernel<TX, TIO, VEC, MAXT><<<*ctas, threads, smem, stream>>>(p, ring);
     return cudaGetLastError();
 }
-// Builds by the registers that a row's threads leave: up to 2048 channels, 5120, 8192.
+// Builds by the registers and the shared memory that a row's threads leave: up to 1536 channels (gradients: five blocks
+// per SM instead of four), 2048, 5120, 8192.
 template <typename TX, typename TIO, bool VEC>
 cudaError_t forward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     if (threads_for(p.channels) <= 128) return forward_one<TX, TIO, VEC, 128>(p, sm_count, ctas, stream);
@@ -904,6 +905,7 @@ cudaError_t forward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStrea
 }
 template <typename TX, typename TIO, bool VEC>
 cudaError_t backward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
+    if (threads_for(p.channels) <= 96) return backward_one<TX, TIO, VEC, 96>(p, sm_count, ctas, stream);
     if (threads_for(p.channels) <= 128) return backward_one<TX, TIO, VEC, 128>(p, sm_count, ctas, stream);
     if (threads_for(p.channels) <= 320) return backward_one<TX, TIO, VEC, 320>(p, sm_count, ctas, stream);
     return backward_one<TX, TIO, VEC, 512>(p, sm_count, ctas, stream);

@@ -6,7 +6,7 @@
 namespace regenvc {
 
 constexpr int kNormMaxChannels = 8192;   // sixteen columns per thread, at most 512 threads
-constexpr int kNormMaxCtas = 608;        // the backward pass's grid never exceeds this: it bounds the workspace
+constexpr int kNormMaxCtas = 760;        // the backward pass's grid never exceeds this: it bounds the workspace
 constexpr int kNormLayer = 1, kNormRms = 2;
 
 struct BlockNormParams {

@@ -69,7 +69,7 @@ def test_block_norm_backward_refusals(L):
     d = _norm_desc()
     need = B.regenvc_block_norm_workspace_bytes(4, 64)
     assert need == 4 * 9 * 64 * 4
-    assert B.regenvc_block_norm_workspace_bytes(10 ** 6, 64) == 608 * 9 * 64 * 4
+    assert B.regenvc_block_norm_workspace_bytes(10 ** 6, 64) == 760 * 9 * 64 * 4
     assert B.regenvc_block_norm_workspace_bytes(0, 64) == 0 and B.regenvc_block_norm_workspace_bytes(4, 8193) == 0
     assert _backward(L, d, size=need - 1) == B.ERR_WORKSPACE
     assert _backward(L, d, ws=A[15] + 8) == B.ERR_WORKSPACE
