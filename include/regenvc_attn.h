@@ -180,7 +180,8 @@ int regenvc_out_project(const void* attn_out, const void* w_o, const void* b_o, 
  * types are named per call, and a pointer needs the alignment of its elements only -- rows whose address, stride and
  * width allow 16-byte accesses take them, others go element by element.  Vectors of parameters are fp32.  Arithmetic
  * is fp32 with one rounding per result.  The calls allocate nothing, take scratch memory as arguments and are
- * asynchronous on `stream`; all can be captured into a CUDA graph (after one call of the library on the device).
+ * asynchronous on `stream`; all can be captured into a CUDA graph (after one call of the library on the device).  Calls
+ * that may overlap on the GPU need scratch memory of their own.
  */
 typedef enum { REGENVC_BF16 = 0, REGENVC_F16 = 1, REGENVC_F32 = 2 } regenvc_type;
 typedef enum { REGENVC_NORM_NONE = 0, REGENVC_NORM_LAYER = 1, REGENVC_NORM_RMS = 2 } regenvc_norm;
@@ -460,6 +461,8 @@ int regenvc_debug_set_phases(int mask);
  * REGENVC_ERR_TIMEOUT until regenvc_device_status() reads it.  Kernels of this
  * library that start while the word is set skip their work (their bounded
  * waits fall through) and leave `out` unspecified.  Nothing faults or hangs.
+ * (Kernels without such waits -- block norm, rotation, 4-bit conversion and the
+ * one-kernel form of the 4-bit product -- run as always.)
  */
 int regenvc_debug_expire_wait(int limit_us, void* stream);
 
