@@ -142,7 +142,7 @@ int mx_project_checks(const void* w, const void* bias, const void* y, int y_type
 }
 
 int mx_project(const void* x, const void* w, const void* bias, void* y, int y_type, int n, int features, int cols,
-               int sm_count, int* status, cudaStream_t stream) {
+               bool early, int sm_count, int* status, cudaStream_t stream) {
     const MxLayout lx(n, cols), lw(features, cols);
     const MxProjectPlan plan = plan_mxfp4_project(n, features, cols, sm_count);
     CUtensorMap mx, mxs, mw, mws, my;
@@ -167,7 +167,7 @@ int mx_project(const void* x, const void* w, const void* bias, void* y, int y_ty
     p.k_blocks = (int)(lx.cols_pad / 128);
     p.y_f16 = y_type == REGENVC_F16;
     p.status = status;
-    const cudaError_t e = launch_mxfp4_project(plan, mx, mxs, mw, mws, my, p, sm_count, stream);
+    const cudaError_t e = launch_mxfp4_project(plan, mx, mxs, mw, mws, my, p, early, sm_count, stream);
     return launch_done(e, "launch of the 4-bit product", e == cudaSuccess ? 1 : 0);
 }
 
@@ -434,7 +434,7 @@ int regenvc_mxfp4_project(const void* x_packed, const void* w_packed, const void
     if (mxfp4_rows_fits(n_tokens, out_features, MxLayout(n_tokens, in_features).cols_pad))
         return mx_rows(x_packed, REGENVC_BF16, -1, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count,
                        (cudaStream_t)stream);
-    return mx_project(x_packed, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count, status,
+    return mx_project(x_packed, w_packed, bias, y, y_type, n_tokens, out_features, in_features, false, sm_count, status,
                       (cudaStream_t)stream);
 }
 
@@ -467,7 +467,7 @@ int regenvc_mxfp4_linear(const void* x, int x_type, long long x_stride, const vo
                        (cudaStream_t)stream);
     rc = mx_convert(x, x_type, n_tokens, in_features, x_stride, scratch, true, (cudaStream_t)stream);
     if (rc != REGENVC_OK) return rc;
-    return mx_project(scratch, w_packed, bias, y, y_type, n_tokens, out_features, in_features, sm_count, status,
+    return mx_project(scratch, w_packed, bias, y, y_type, n_tokens, out_features, in_features, true, sm_count, status,
                       (cudaStream_t)stream);
 }
 

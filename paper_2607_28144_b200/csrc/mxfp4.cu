@@ -125,6 +125,8 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kMaxThreads) mxfp4_quantize_kernel(const MxConvertParams p, const int rows_per_block) {
     __shared__ alignas(16) float spread[VEC ? 1 : kMaxThreads / 32][VEC ? 4 : kSpread];
     constexpr int kAhead = !VEC ? 1 : (sizeof(T) == 4 ? 2 : 4);   // rows of loads in flight
+    // a product launched behind this may set itself up from here on (it starts once every block of this grid has)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const MxLayout lay(p.rows, p.cols);
     const unsigned groups = (unsigned)(lay.cols_pad / 128);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

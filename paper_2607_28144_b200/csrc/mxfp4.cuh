@@ -48,9 +48,11 @@ struct MxProjectPlan {
 };
 MxProjectPlan plan_mxfp4_project(int n_tokens, int features, int in_features, int sm_count);
 cudaError_t configure_mxfp4_project();
+// early: the launch before it on `stream` is launch_mxfp4_quantize() of this x, whose end the set-up may overlap (the kernel
+// waits for it before it reads x).
 cudaError_t launch_mxfp4_project(const MxProjectPlan& plan, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& w,
-                                 const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, int sm_count,
-                                 cudaStream_t stream);
+                                 const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, bool early,
+                                 int sm_count, cudaStream_t stream);
 
 // The product for a few tokens (mxfp4_rows.cu), from x of any type or packed.
 constexpr int kMxFewRows = 4;

@@ -174,6 +174,8 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
         if (elect_one()) {
             tma_prefetch_desc(&tmap_x);
             tma_prefetch_desc(&tmap_w);
+            // launched early behind the kernel that quantises x (launch_mxfp4_project): all set-up above ran beside its end
+            asm volatile("griddepcontrol.wait;" ::: "memory");
             int fill = 0;
             bool ok = true;
             for (int slice = slice0; ok && slice < n_slices; slice += slice_step) {
@@ -336,7 +338,7 @@ mxfp4_project_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
 
 template <int CG, int NT>
 cudaError_t launch_cfg(const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& w, const CUtensorMap& ws,
-                       const CUtensorMap& y, const MxProjectParams& p, int sm_count, cudaStream_t stream) {
+                       const CUtensorMap& y, const MxProjectParams& p, bool early, int sm_count, cudaStream_t stream) {
     const int n_tiles = (p.n_tokens + kTile - 1) / kTile;
     const long long n_slices = (long long)((n_tiles + CG - 1) / CG) * ((p.features + NT - 1) / NT);
     const int slots = sm_count / CG;
@@ -347,13 +349,20 @@ cudaError_t launch_cfg(const CUtensorMap& x, const CUtensorMap& xs, const CUtens
     cfg.blockDim = dim3(kThreadsMx);
     cfg.dynamicSmemBytes = mx_smem<CG, NT>();
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    int n_attr = 0;
+    if (CG == 2) {
+        attr[n_attr].id = cudaLaunchAttributeClusterDimension;
+        attr[n_attr].val.clusterDim.x = CG;
+        attr[n_attr].val.clusterDim.y = 1;
+        attr[n_attr++].val.clusterDim.z = 1;
+    }
+    if (early) {
+        attr[n_attr].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n_attr++].val.programmaticStreamSerializationAllowed = 1;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = CG == 2 ? 1 : 0;
+    cfg.numAttrs = n_attr;
     return cudaLaunchKernelEx(&cfg, mxfp4_project_kernel<CG, NT>, x, xs, w, ws, y, p);
 }
 
@@ -402,12 +411,12 @@ cudaError_t configure_mxfp4_project() {
 }
 
 cudaError_t launch_mxfp4_project(const MxProjectPlan& plan, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& w,
-                                 const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, int sm_count,
-                                 cudaStream_t stream) {
-    if (plan.pair && plan.tile_features == 256) return launch_cfg<2, 256>(x, xs, w, ws, y, p, sm_count, stream);
-    if (plan.pair) return launch_cfg<2, 192>(x, xs, w, ws, y, p, sm_count, stream);
-    if (plan.tile_features == 64) return launch_cfg<1, 64>(x, xs, w, ws, y, p, sm_count, stream);
-    return launch_cfg<1, 192>(x, xs, w, ws, y, p, sm_count, stream);
+                                 const CUtensorMap& ws, const CUtensorMap& y, const MxProjectParams& p, bool early,
+                                 int sm_count, cudaStream_t stream) {
+    if (plan.pair && plan.tile_features == 256) return launch_cfg<2, 256>(x, xs, w, ws, y, p, early, sm_count, stream);
+    if (plan.pair) return launch_cfg<2, 192>(x, xs, w, ws, y, p, early, sm_count, stream);
+    if (plan.tile_features == 64) return launch_cfg<1, 64>(x, xs, w, ws, y, p, early, sm_count, stream);
+    return launch_cfg<1, 192>(x, xs, w, ws, y, p, early, sm_count, stream);
 }
 
 }  // namespace regenvc
