@@ -327,8 +327,8 @@ def _new(shape, dtype, device, stream):
 
 def _like(t, stream):
     """A packed result of an operand's shape and type."""
-    if stream is None and t.is_contiguous():
-        return torch.empty_like(t)
+    if stream is None:
+        return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
     return _new(t.shape, t.dtype, t.device, stream)
 
 
@@ -353,6 +353,9 @@ def _rows(t, name: str, dtype, n: int, c: int) -> int:
     """Checks a matrix and returns the elements between its rows as the library takes them (0: packed)."""
     if t.dtype is not dtype or t.shape != (n, c):
         raise TypeError(f"{name} must be {dtype} [{n}, {c}]")
+    between, step = t.stride()
+    if n > 1 and between >= c and (step == 1 or c == 1):   # the ordinary case, without a second call
+        return between
     return _row_stride(t, name)
 
 
@@ -412,9 +415,12 @@ def regenvc_block_norm_forward(x, y=None, *, gate=None, post_norm: int = NORM_NO
         raise TypeError("h must be bf16, fp16 or fp32")
     x_stride = _row_stride(x, "x")
     y_stride = 0 if y is None else _rows(y, "y", io, n, c)
-    _vector(post_weight, "post_weight", c)
-    _vector(weight, "weight", c)
-    _vector(bias, "bias", c)
+    if post_weight is not None:
+        _vector(post_weight, "post_weight", c)
+    if weight is not None:
+        _vector(weight, "weight", c)
+    if bias is not None:
+        _vector(bias, "bias", c)
     per, _, mod_stride = _modulation(n, c, tokens_per_mod, gate, scale, shift)
     x_out_stride = h_stride = 0
     if x_out is not None:
@@ -441,9 +447,6 @@ def regenvc_block_norm_workspace_bytes(n_tokens: int, channels: int) -> int:
     return int(lib().regenvc_block_norm_workspace_bytes(n_tokens, channels))
 
 
-_NORM_GRADS = ("dx", "dy", "dgate", "dscale", "dshift", "dpost_weight", "dweight", "dbias")
-
-
 def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, post_norm: int = NORM_NONE, post_weight=None,
                                 post_eps: float = 1e-6, residual_scale: float = 1.0, norm: int = NORM_LAYER, weight=None,
                                 bias=None, eps: float = 1e-6, scale=None, shift=None, tokens_per_mod=None, dx=None,
@@ -464,33 +467,36 @@ def regenvc_block_norm_backward(dh, x_out, *, dx_out=None, y=None, gate=None, po
     x_stride = 0 if x_out is None else _rows(x_out, "x_out", like.dtype, n, c)
     h_stride = 0 if dh is None else _rows(dh, "dh", io, n, c)
     more_stride = 0 if dx_out is None else _rows(dx_out, "dx_out", like.dtype, n, c)
-    for t, name in ((post_weight, "post_weight"), (weight, "weight"), (bias, "bias")):
-        _vector(t, name, c)
-    per, rows, mod_stride = _modulation(n, c, tokens_per_mod, gate, scale, shift)
+    if post_weight is not None:
+        _vector(post_weight, "post_weight", c)
+    if weight is not None:
+        _vector(weight, "weight", c)
+    if bias is not None:
+        _vector(bias, "bias", c)
+    per, _, mod_stride = _modulation(n, c, tokens_per_mod, gate, scale, shift)
     if dx is None:
         dx, dx_stride = _like(like, stream), 0
     else:
         dx_stride = _rows(dx, "dx", like.dtype, n, c)
-    g = dict.fromkeys(_NORM_GRADS)
-    g["dx"], g["dy"] = dx, None if y is None else _like(y, stream)
-    # the parameters' gradients are parts of one allocation
-    wanted = [(k, rows) for t, k in ((gate, "dgate"), (scale, "dscale"), (shift, "dshift")) if t is not None]
-    wanted += [(k, 0) for t, k in ((post_weight, "dpost_weight"), (weight, "dweight"), (bias, "dbias")) if t is not None]
-    if wanted:
-        sizes = [(r or 1) * c for _, r in wanted]
-        parts = _new((sum(sizes),), torch.float32, like.device, stream).split_with_sizes(sizes)
-        for (k, r), part in zip(wanted, parts):
-            g[k] = part.view(r, c) if r else part
+    # every parameter's gradient has its shape, packed
+    dy = None if y is None else _like(y, stream)
+    dgate = None if gate is None else _like(gate, stream)
+    dscale = None if scale is None else _like(scale, stream)
+    dshift = None if shift is None else _like(shift, stream)
+    dpost = None if post_weight is None else _like(post_weight, stream)
+    dweight = None if weight is None else _like(weight, stream)
+    dbias = None if bias is None else _like(bias, stream)
     if workspace is None:
         workspace = _new((regenvc_block_norm_workspace_bytes(n, c),), torch.uint8, like.device, stream)
     d = _NORM_DESC.pack(n, c, per, TYPES[like.dtype], TYPES[io], norm, post_norm, eps, post_eps, residual_scale,
                         mod_stride, 0, y_stride, x_stride, h_stride, more_stride, dx_stride, 0)
     _check(lib().regenvc_block_norm_backward(
         d, _addr(x_out), _addr(y), _addr(gate), _addr(post_weight), _addr(weight), _addr(bias), _addr(scale),
-        _addr(dh), _addr(dx_out), dx.data_ptr(), _addr(g["dy"]), _addr(g["dgate"]), _addr(g["dpost_weight"]),
-        _addr(g["dweight"]), _addr(g["dbias"]), _addr(g["dscale"]), _addr(g["dshift"]), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _launch_stream(stream, index)))
-    return g
+        _addr(dh), _addr(dx_out), dx.data_ptr(), _addr(dy), _addr(dgate), _addr(dpost), _addr(dweight), _addr(dbias),
+        _addr(dscale), _addr(dshift), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _launch_stream(stream, index)))
+    return {"dx": dx, "dy": dy, "dgate": dgate, "dscale": dscale, "dshift": dshift, "dpost_weight": dpost,
+            "dweight": dweight, "dbias": dbias}
 
 
 def regenvc_rope_axes(q, k, positions, widths, *, rope_theta: float = 10000.0, halves: bool = False,
