@@ -33,7 +33,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC,-O2", "-shared",
+           "-Xcompiler", "-fPIC,-O2", "-shared", "--threads", "0",
            "-cudart", "static", "-I", INCLUDE, "-o", tmp] + sources()
     if verbose:
         cmd.insert(1, "-Xptxas")

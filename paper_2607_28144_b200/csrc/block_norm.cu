@@ -899,18 +899,21 @@ cudaError_t backward_one(BlockNormParams& p, int sm_count, int* ctas, cudaStream
     return cudaGetLastError();
 }
 // Builds by the registers and the shared memory that a row's threads leave: up to 1536 channels (gradients: five blocks
-// per SM instead of four), 2048, 5120, 8192.
+// per SM instead of four), 2048, 5120, 8192; rows read as images: 2048 and 8192.
 template <typename TX, typename TIO, bool VEC>
 cudaError_t forward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
     if (threads_for(p.channels) <= 128) return forward_one<TX, TIO, VEC, 128>(p, sm_count, ctas, stream);
-    if (threads_for(p.channels) <= 320) return forward_one<TX, TIO, VEC, 320>(p, sm_count, ctas, stream);
+    if constexpr (VEC)
+        if (threads_for(p.channels) <= 320) return forward_one<TX, TIO, VEC, 320>(p, sm_count, ctas, stream);
     return forward_one<TX, TIO, VEC, 512>(p, sm_count, ctas, stream);
 }
 template <typename TX, typename TIO, bool VEC>
 cudaError_t backward_sized(BlockNormParams& p, int sm_count, int* ctas, cudaStream_t stream) {
-    if (threads_for(p.channels) <= 96) return backward_one<TX, TIO, VEC, 96>(p, sm_count, ctas, stream);
+    if constexpr (VEC)
+        if (threads_for(p.channels) <= 96) return backward_one<TX, TIO, VEC, 96>(p, sm_count, ctas, stream);
     if (threads_for(p.channels) <= 128) return backward_one<TX, TIO, VEC, 128>(p, sm_count, ctas, stream);
-    if (threads_for(p.channels) <= 320) return backward_one<TX, TIO, VEC, 320>(p, sm_count, ctas, stream);
+    if constexpr (VEC)
+        if (threads_for(p.channels) <= 320) return backward_one<TX, TIO, VEC, 320>(p, sm_count, ctas, stream);
     return backward_one<TX, TIO, VEC, 512>(p, sm_count, ctas, stream);
 }
 
