@@ -843,6 +843,8 @@ __global__ void __launch_bounds__(32 * kJoinLanes, 2) block_norm_join_kernel(con
     }
 }
 
+constexpr uint32_t kMostShared = 228000;   // dynamic shared memory of a thread block, at most (plan_ring)
+
 int threads_for(int channels) { return (channels + 32 * kCols - 1) / (32 * kCols) * 32; }
 
 // A persistent grid: as many thread blocks as the device holds at a time (more would run as a second, mostly empty wave:
@@ -850,7 +852,9 @@ int threads_for(int channels) { return (channels + 32 * kCols - 1) / (32 * kCols
 template <typename K>
 cudaError_t plan(BlockNormParams* p, K kernel, int threads, size_t smem, int sm_count, int cap, int* ctas) {
     if (smem > 40000) {   // static and dynamic shared memory together past the default limit of 48 KB
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        // The limit belongs to the kernel, not to the call, and other host threads launch the same kernel at other widths:
+        // it is always set to the most that any width takes, so that no call lowers it under another one's launch.
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared);
         if (e != cudaSuccess) return e;
     }
     int most = p->n_tokens;
@@ -872,7 +876,7 @@ cudaError_t plan(BlockNormParams* p, K kernel, int threads, size_t smem, int sm_
 Ring plan_ring(uint32_t stage_bytes, uint32_t other_bytes, int threads, int threads_wanted) {
     const int blocks = threads_wanted / threads > 1 ? threads_wanted / threads : 1;
     int stages = (int)((224000u / blocks - other_bytes) / stage_bytes);
-    if (stages < 2) stages = 2 * stage_bytes + other_bytes <= 228000u ? 2 : 1;
+    if (stages < 2) stages = 2 * stage_bytes + other_bytes <= kMostShared ? 2 : 1;
     if (stages > 4) stages = 4;
     return Ring{stages, stage_bytes};
 }
