@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kHalfWarps = kThreads / 16;
+constexpr int kMostShared = 160 * 1024;   // dynamic shared memory of a thread block, at most
 struct Packed {};   // source type of x that is in 4-bit form already
 
 __device__ __forceinline__ float2 sum_pairs(const uint4& a, const uint4& b, const uint4& c, const uint4& d, const uint32_t* w) {
@@ -186,7 +187,8 @@ template <typename T, int MR, int FP>
 cudaError_t launch_one(const MxRowsParams& p, int sm_count, cudaStream_t stream) {
     const size_t smem = (size_t)MR * (p.cols_pad * 2 + p.cols_pad / 32);
     if (smem > 48000) {
-        const cudaError_t e = cudaFuncSetAttribute(mxfp4_rows_kernel<T, MR, FP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        // always the most that any call takes: the limit is the kernel's, and other host threads launch it at other sizes
+        const cudaError_t e = cudaFuncSetAttribute(mxfp4_rows_kernel<T, MR, FP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
         if (e != cudaSuccess) return e;
     }
     const int per_block = kHalfWarps * FP;
@@ -213,7 +215,7 @@ cudaError_t launch_typed(const MxRowsParams& p, int sm_count, cudaStream_t strea
 
 bool mxfp4_rows_fits(int n_tokens, int features, long long cols_pad) {
     if (n_tokens > kMxFewRows || (n_tokens > 1 && features * cols_pad >= 1ll << 24)) return false;
-    return (n_tokens == 1 ? 1 : 4) * (cols_pad * 2 + cols_pad / 32) <= 160 * 1024;
+    return (n_tokens == 1 ? 1 : 4) * (cols_pad * 2 + cols_pad / 32) <= kMostShared;
 }
 
 cudaError_t launch_mxfp4_rows(const MxRowsParams& p, int type, bool packed, int sm_count, cudaStream_t stream) {

@@ -38,6 +38,16 @@ def _norm_backward(c, xt, iot, stream, g):
     return B.lib().regenvc_block_norm_backward, args, (dx, dy, dw), (d, x, dx_out, y, dh, w, ws)
 
 
+def _linear(cols, tokens, _, stream, g):
+    f = 64
+    x, w = torch.randn(tokens, cols, generator=g, device=DEV), torch.randn(f, cols, generator=g, device=DEV)
+    wp = B.regenvc_mxfp4_quantize(w)
+    y = torch.empty((tokens, f), dtype=torch.bfloat16, device=DEV)
+    assert B.regenvc_mxfp4_linear_scratch_bytes(tokens, f, cols) == 0
+    args = (x.data_ptr(), B.TYPES[x.dtype], 0, wp.data_ptr(), None, y.data_ptr(), 0, tokens, f, cols, None, stream)
+    return B.lib().regenvc_mxfp4_linear, args, (y,), (x, wp)
+
+
 def _two_threads(make, a, b, first, second):
     """Both calls alternate freely on a stream each: every call succeeds, and the results are those of the call alone."""
     jobs, want = [], []
@@ -76,3 +86,8 @@ def _two_threads(make, a, b, first, second):
     (_norm_forward, 2056, 4096, "fp32", "fp32"), (_norm_forward, 6001, 8191, "fp16", "fp16")])
 def test_block_norm_of_two_widths(make, a, b, xt, iot):
     _two_threads(make, a, b, xt, iot)
+
+
+@pytest.mark.parametrize("tokens,a,b", [(1, 30080, 80640), (4, 8192, 20096)])
+def test_4_bit_product_of_few_tokens_of_two_inner_extents(tokens, a, b):
+    _two_threads(_linear, a, b, tokens, None)
