@@ -199,6 +199,8 @@ typedef enum { REGENVC_NORM_NONE = 0, REGENVC_NORM_LAYER = 1, REGENVC_NORM_RMS =
  *   x_out    : x' rounded to x_type; may be x itself (in place, same stride), or NULL; NULL if y is NULL
  *   h        : from x' before that rounding; NULL exactly if norm is REGENVC_NORM_NONE
  * Other overlaps of a result with an operand are refused (REGENVC_ERR_ALIASING); NaN and infinity stay in their rows.
+ * Statistics are fp32: a row whose sum of squares passes its range (magnitudes near 5e17 at 1536 channels) has an infinite
+ * deviation, normalises to 0 and lets no gradient through its norm.
  */
 typedef struct {
     int n_tokens, channels, tokens_per_mod;

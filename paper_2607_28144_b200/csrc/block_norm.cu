@@ -308,14 +308,15 @@ __device__ __forceinline__ BlockSum block_sum_init(float (*buf)[4][16]) {
     return BlockSum{buf, (int)(blockDim.x + 31) / 32, 0};
 }
 
-// s / channels, rounded as a division is: the product with the reciprocal alone would leave a constant row a mean that is
-// off by an ulp.
+// s / channels with one step of residual correction (Markstein's): exact where the quotient is an fp32 value, as a constant
+// row's mean is, which the product with the reciprocal alone may miss by an ulp.  An infinite s stays infinite (the residual
+// would be inf - inf): a row whose sum of squares passes fp32's range then has r = 0 and normalises to 0.
 struct Channels {
     float n, inverse;
     __device__ __forceinline__ explicit Channels(int channels) : n((float)channels), inverse(1.0f / (float)channels) {}
     __device__ __forceinline__ float mean(float s) const {
         const float q = s * inverse;
-        return fmaf(fmaf(-q, n, s), inverse, q);
+        return fabsf(q) < __uint_as_float(0x7F800000u) ? fmaf(fmaf(-q, n, s), inverse, q) : q;
     }
 };
 
@@ -653,8 +654,10 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
                     q[1] = join(tb);
                     sum.run<4>(q);
                     const float r = rsqrtf(ch.mean(q[3]) + p.eps);
-                    // dx' = r (d - m0 - xhat m1), xhat = r times the centred x'
-                    const f32x2 r2 = both(r), m0 = both(p.norm == kNormLayer ? -r * ch.mean(q[0]) : 0.0f), m1 = both(-(r * (r * (r * ch.mean(q[1])))));
+                    // dx' = r (d - m0 - xhat m1), xhat = r times the centred x' (r = 0: nothing comes through, even where
+                    // the sum against the centred x' is infinite)
+                    const f32x2 r2 = both(r), m0 = both(p.norm == kNormLayer ? -r * ch.mean(q[0]) : 0.0f),
+                                m1 = both(r == 0.0f ? 0.0f : -(r * (r * (r * ch.mean(q[1])))));
 #pragma unroll
                     for (int i = 0; i < kPairs; i += 2) {
                         f32x2 wi[2];
