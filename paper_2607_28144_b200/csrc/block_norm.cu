@@ -273,7 +273,10 @@ __device__ __forceinline__ void read_vector(const float* base, float absent, con
 }
 
 // Sums over the thread block, the same value in every thread, in a fixed order.  Two buffers used in turn make one
-// barrier per sum enough: a buffer is written again only behind the next sum's barrier.
+// barrier per sum enough: a buffer is written again only behind the next sum's barrier.  WARPS: the build's most; the
+// warps' parts are read back without a loop, all in flight (as a loop over the launched warps every value waited for shared
+// memory two or three times: 31200 x 5120 forward 358 us instead of 324, 12480 x 5120 gradients 340 instead of 279).
+template <int WARPS>
 struct BlockSum {
     float (*buf)[4][16];   // [2 buffers][4 values][warp]
     int warps, turn;
@@ -294,7 +297,8 @@ struct BlockSum {
         for (int n = 0; n < N; ++n) {
             const float4 q = *reinterpret_cast<const float4*>(&b[n][0]);
             float s = (q.x + q.y) + (q.z + q.w);
-            for (int w = 4; w < warps; w += 4) {
+#pragma unroll
+            for (int w = 4; w < WARPS; w += 4) {   // (no such warp: 0)
                 const float4 r = *reinterpret_cast<const float4*>(&b[n][w]);
                 s += (r.x + r.y) + (r.z + r.w);
             }
@@ -302,10 +306,11 @@ struct BlockSum {
         }
     }
 };
-__device__ __forceinline__ BlockSum block_sum_init(float (*buf)[4][16]) {
+template <int WARPS>
+__device__ __forceinline__ BlockSum<WARPS> block_sum_init(float (*buf)[4][16]) {
     for (int i = threadIdx.x; i < 128; i += blockDim.x) (&buf[0][0][0])[i] = 0.0f;   // entries past the last warp stay 0
     __syncthreads();
-    return BlockSum{buf, (int)(blockDim.x + 31) / 32, 0};
+    return BlockSum<WARPS>{buf, (int)(blockDim.x + 31) / 32, 0};
 }
 
 // s / channels with one step of residual correction (Markstein's): exact where the quotient is an fp32 value, as a constant
@@ -345,18 +350,33 @@ __device__ __forceinline__ void subtract(f32x2* v, float mean, const Place<VEC>&
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], at.masked(i, -mean));
 }
+// Layer norm's mean carries the rounding of its sum, up to 24 u of the row's magnitude, which counts where that magnitude is
+// far above the deviation (a constant fp32 row of 12345.678 came out as +-0.7 at eps 1e-6 instead of 0).  The centred values'
+// mean is that error: it goes out of the values, and its square out of their squares' mean.
+__device__ __forceinline__ float variance(float mean_squares, float error) {
+    const float v = fmaf(-error, error, mean_squares);
+    return v < 0.0f ? 0.0f : v;
+}
 // v -> normalised v
-template <bool VEC>
-__device__ __forceinline__ void normalise(f32x2* v, int kind, float eps, const Channels& ch, const Place<VEC>& at, BlockSum& sum) {
-    float s[1];
+template <bool VEC, typename SUM>
+__device__ __forceinline__ void normalise(f32x2* v, int kind, float eps, const Channels& ch, const Place<VEC>& at, SUM& sum) {
+    float s[2], var;
     if (kind == kNormLayer) {
         s[0] = total(v);
-        sum.run<1>(s);
+        sum.template run<1>(s);
         subtract<VEC>(v, ch.mean(s[0]), at);
+        s[0] = total_squares(v);
+        s[1] = total(v);
+        sum.template run<2>(s);
+        const float error = ch.mean(s[1]);
+        subtract<VEC>(v, error, at);
+        var = variance(ch.mean(s[0]), error);
+    } else {
+        s[0] = total_squares(v);
+        sum.template run<1>(s);
+        var = ch.mean(s[0]);
     }
-    s[0] = total_squares(v);
-    sum.run<1>(s);
-    const f32x2 r = both(rsqrtf(ch.mean(s[0]) + eps));
+    const f32x2 r = both(rsqrtf(var + eps));
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) v[i] = mul2(v[i], r);
 }
@@ -428,7 +448,7 @@ template <typename TX, typename TIO, bool VEC, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) block_norm_forward_kernel(const BlockNormParams p, const Ring ring) {
     __shared__ alignas(16) float buf[2][4][16];
     extern __shared__ uint4 ring_mem[];
-    BlockSum sum = block_sum_init(buf);
+    BlockSum<MAXT / 32> sum = block_sum_init<MAXT / 32>(buf);
     const Place<VEC> at(p.channels);
     const Channels ch(p.channels);
     const int row0 = blockIdx.x * p.rows_per_cta;
@@ -549,6 +569,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
     __shared__ alignas(16) float buf[2][4][16];
     extern __shared__ uint4 shared_mem[];
     constexpr bool kRegs = MAXT == 320;
+    // Rows of fp32 have the error of a layer norm's mean taken out (see variance()).  x's takes the place of y's squares in
+    // the second exchange: those go with the means or, where y has a mean itself, into an exchange of their own (12480 x
+    // 5120 with an fp32 stream: 279 us, 296 us with a fifth sum).  Rows of 16-bit types do without: a sum of values of one
+    // binade is exact in fp32, and values of several leave a deviation that such an error does not touch.
+    constexpr bool kSharpX = sizeof(TX) == 4, kSharpY = sizeof(TIO) == 4;
     Kept<MAXT, kRegs> w_kept, g_kept;
     uint4* ring_mem = shared_mem;
     if constexpr (!kRegs) {
@@ -556,7 +581,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
         g_kept.mem = w_kept.mem + kCols / 4 * MAXT;
         ring_mem += 2 * (kCols / 4) * MAXT;
     }
-    BlockSum sum = block_sum_init(buf);
+    BlockSum<MAXT / 32> sum = block_sum_init<MAXT / 32>(buf);
     const Place<VEC> at(p.channels);
     const Channels ch(p.channels);
     const int row0 = blockIdx.x * p.rows_per_cta;
@@ -621,24 +646,40 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
             if (normed || p.post_norm) {
                 // All sums of the row that do not need dx' take two barriers: the means, then the centred squares of x' and
                 // y and the sums of d = dh (1 + s) w and of d against the centred x' (one barrier where both are RMS norms).
+                const bool sharp = kSharpX && p.norm == kNormLayer;
+                const bool y_early = kSharpX && (sharp || p.post_norm == kNormLayer);   // y's squares before the second exchange
                 float m[2] = {0.0f, 0.0f}, q[4];
                 if (normed) xs.read(at, here, v);
                 if (p.norm == kNormLayer) m[0] = total(v);
                 if (p.post_norm == kNormLayer) {
                     ys.read(at, here, d);
                     m[1] = total(d);
+                } else if (sharp && p.post_norm) {
+                    ys.read(at, here, d);
+                    m[1] = total_squares(d);
                 }
-                if (p.norm == kNormLayer || p.post_norm == kNormLayer) sum.run<2>(m);
-                y_mean = ch.mean(m[1]);
+                if (p.norm == kNormLayer || p.post_norm == kNormLayer) sum.template run<2>(m);
+                if (!kSharpX || p.post_norm == kNormLayer) y_mean = ch.mean(m[1]);
+                float y_squares = m[1], y_error = 0.0f;
                 q[2] = 0.0f;
-                if (p.post_norm) {
+                if (p.post_norm && (!y_early || p.post_norm == kNormLayer)) {
                     ys.read(at, here, d);
                     if (p.post_norm == kNormLayer) subtract<VEC>(d, y_mean, at);
                     q[2] = total_squares(d);
                 }
+                if (kSharpX && p.post_norm == kNormLayer) {
+                    float e[2] = {q[2], kSharpY ? total(d) : 0.0f};
+                    sum.template run<kSharpY ? 2 : 1>(e);
+                    y_squares = e[0];
+                    if (kSharpY) {
+                        y_error = ch.mean(e[1]);
+                        y_mean += y_error;   // (the columns are read again below)
+                    }
+                }
                 if (normed) {
                     if (p.norm == kNormLayer) subtract<VEC>(v, ch.mean(m[0]), at);
                     q[3] = total_squares(v);
+                    if (sharp) q[2] = total(v);
                     hs.read(at, here, d);
                     f32x2 ta = 0ull, tb = 0ull;
 #pragma unroll
@@ -652,8 +693,16 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
                     }
                     q[0] = join(ta);
                     q[1] = join(tb);
-                    sum.run<4>(q);
-                    const float r = rsqrtf(ch.mean(q[3]) + p.eps);
+                    sum.template run<4>(q);
+                    float var = ch.mean(q[3]);
+                    if (kSharpX) {
+                        const float error = sharp ? ch.mean(q[2]) : 0.0f;
+                        var = variance(var, error);
+                        q[1] = fmaf(-error, q[0], q[1]);
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], both(-error));   // (dead columns are not used below)
+                    }
+                    const float r = rsqrtf(var + p.eps);
                     // dx' = r (d - m0 - xhat m1), xhat = r times the centred x' (r = 0: nothing comes through, even where
                     // the sum against the centred x' is infinite)
                     const f32x2 r2 = both(r), m0 = both(p.norm == kNormLayer ? -r * ch.mean(q[0]) : 0.0f),
@@ -669,10 +718,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
                             d[i + k] = fma2(v[i + k], m1, fma2(mul2(d[i + k], wi[k]), r2, m0));
                         }
                     }
-                } else {
-                    sum.run<1>(q + 2);
+                } else if (!y_early) {
+                    sum.template run<1>(q + 2);
                 }
-                if (p.post_norm) y_r = rsqrtf(ch.mean(q[2]) + p.post_eps);
+                if (!y_early) y_squares = q[2];
+                if (p.post_norm) y_r = rsqrtf((kSharpY ? variance(ch.mean(y_squares), y_error) : ch.mean(y_squares)) + p.post_eps);
             }
             if (!normed) {
 #pragma unroll
@@ -717,7 +767,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 96 ? 5 : (MAXT == 128 ? 4 : 1)) 
                         tb = fma2(d[i], v[i], tb);   // v is 0 there
                     }
                     float t[2] = {join(ta), join(tb)};
-                    sum.run<2>(t);
+                    sum.template run<2>(t);
                     const f32x2 m0 = both(p.post_norm == kNormLayer ? -y_r * ch.mean(t[0]) : 0.0f), m1 = both(-y_r * ch.mean(t[1])), r2 = both(y_r);
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) d[i] = fma2(v[i], m1, fma2(d[i], r2, m0));

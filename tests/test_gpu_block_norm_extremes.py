@@ -63,3 +63,73 @@ def test_an_infinity_beside_finite_values():
         others = torch.arange(c, device=DEV) != 7
         assert torch.isnan(h[1, 7]) and (h[1, others] == 0).all()
         _forward_check(x[[0, 2]], None, {}, 2, 0, 1.0, 2, None, h[[0, 2]])
+
+
+VALUES = [12345.678, 1000.1, 1e18, 3e-3, -77777.77, 0.1, 1e-20, 3.0]
+
+
+def _constant(c, dtype):
+    return torch.tensor(VALUES, device=DEV).to(dtype)[:, None].expand(-1, c).contiguous()
+
+
+@pytest.mark.parametrize("c", [7, 96, 200, 1000, 1531, 1536, 2056, 5120, 8191])
+@pytest.mark.parametrize("xt,iot", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16"), ("fp16", "fp16")])
+def test_rows_of_one_value_normalise_to_zero(c, xt, iot):
+    """Layer norm of a row whose fp32 sum is not exact: the mean's error is known after the centred values' sum and goes
+    out again, so the result is 0 and not that error times 1 / sqrt(eps)."""
+    n = len(VALUES)
+    x = _constant(c, T[xt])
+    x[~torch.isfinite(x)] = 3.0                                    # (fp16's range)
+    _, h = B.regenvc_block_norm_forward(x, norm=1, eps=EPS)
+    assert (h == 0).all()
+    # x' of one value: a product and a sum with all of fp32's bits, whatever the types
+    y, gate = torch.full((n, c), 0.3, device=DEV).to(T[iot]), torch.full((1, c), 1.7, device=DEV)
+    _, h = B.regenvc_block_norm_forward(x, y, gate=gate, norm=1, eps=EPS)
+    assert (h == 0).all()
+    # as the branch's own norm
+    yc = _constant(c, T[iot])
+    yc[~torch.isfinite(yc)] = 3.0
+    z = torch.randn(n, c, device=DEV, generator=torch.Generator(device=DEV).manual_seed(c)).to(T[xt])
+    x_out, _ = B.regenvc_block_norm_forward(z, yc, norm=0, post_norm=1, post_eps=EPS)
+    assert torch.equal(x_out, z)
+
+
+@pytest.mark.parametrize("c", [7, 200, 1531, 1536, 5120, 8191])
+@pytest.mark.parametrize("xt,iot", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16")])
+def test_gradients_of_rows_of_one_value(c, xt, iot):
+    """xhat = 0: no gradient of the weights, and d - mean(d) times 1 / sqrt(eps) for the row itself."""
+    r, p = _parts(c, c)
+    n, x, yc = len(VALUES), _constant(c, T[xt]), _constant(c, T[iot])
+    dh, more = r(n, c).to(T[iot]), r(n, c).to(T[xt])
+    p = {"weight": p["weight"], "scale": p["scale"], "shift": p["shift"]}
+    got = B.regenvc_block_norm_backward(dh, x, **p, norm=1, eps=EPS)
+    assert (got["dweight"] == 0).all() and (got["dscale"] == 0).all()
+    d = dh.double() * p["weight"].double() * (1 + p["scale"].double())
+    ref, top = (d - d.mean(1, keepdim=True)) / EPS ** 0.5, d.abs().amax(1, keepdim=True) / EPS ** 0.5
+    _check(got["dx"], ref, half_step(T[xt]) * ref.abs() + 64 * U * top * 4, "dx")
+    pw, gate = 1 + 0.2 * r(c), r(1, c)
+    got = B.regenvc_block_norm_backward(None, None, dx_out=more, y=yc, gate=gate, post_weight=pw, norm=0, post_norm=1, post_eps=EPS)
+    assert (got["dgate"] == 0).all() and (got["dpost_weight"] == 0).all()
+    d = more.double() * gate.double() * pw.double()
+    ref, top = (d - d.mean(1, keepdim=True)) / EPS ** 0.5, d.abs().amax(1, keepdim=True) / EPS ** 0.5
+    _check(got["dy"], ref, half_step(T[iot]) * ref.abs() + 64 * U * top * 4, "dy")
+
+
+@pytest.mark.parametrize("c", [200, 1531, 1536, 5120])
+def test_rows_that_differ_by_single_bits(c):
+    """Values of 12345.678 and up to two units in the last place around.  Centred values are exact; the mean's first error is
+    at most 24 u of the mean, 18 ulp, against a deviation of 1.4 ulp, so r loses 14 u (1 + 18^2 / 2), and the rest is the
+    ordinary 64 u T with T = 2 max|v - mean| r."""
+    g = torch.Generator(device=DEV).manual_seed(c)
+    x = torch.full((5, c), 12345.678, device=DEV) + 2.0 ** -10 * torch.randint(-2, 3, (5, c), generator=g, device=DEV)
+    _, h = B.regenvc_block_norm_forward(x, norm=1, eps=0.0)
+    d = x.double() - x.double().mean(1, keepdim=True)
+    ref = d * torch.rsqrt((d * d).mean(1, keepdim=True))
+    t = 2 * ref.abs().amax(1, keepdim=True)
+    _check(h, ref, (64 + 14 * 163) * U * t, "h")
+    # gradient: dx = r (dh - mean(dh) - xhat mean(dh xhat)), the same loss in r and xhat
+    dh = torch.randn(5, c, generator=g, device=DEV)
+    got = B.regenvc_block_norm_backward(dh, x, norm=1, eps=0.0)["dx"]
+    r, dd = torch.rsqrt((d * d).mean(1, keepdim=True)), dh.double()
+    want = r * (dd - dd.mean(1, keepdim=True) - ref * (dd * ref).mean(1, keepdim=True))
+    _check(got, want, (64 + 14 * 163) * U * dd.abs().amax(1, keepdim=True) * r * (2 + t) ** 2, "dx")
