@@ -189,7 +189,7 @@ typedef enum { REGENVC_NORM_NONE = 0, REGENVC_NORM_LAYER = 1, REGENVC_NORM_RMS =
 /*
  * Norms before and after a block, fused with the block's gate and residual scale (backbone by reference, Sec. 3.2 /
  * 3.4: every branch reads a normalised and modulated copy of the residual stream and is added back through a gate):
- *     z  = N2(y) post_weight            (post_norm; N2 absent: z = y)
+ *     z  = N2(y) post_weight            (post_norm; without one N2(y) is y: z = y post_weight, a scale per channel)
  *     x' = residual_scale x + gate z    (y == NULL: x' = x, nothing is added or scaled)
  *     h  = (N1(x') weight + bias) (1 + scale) + shift
  * N is layer norm (v - mean) / sqrt(var + eps) or RMS norm v / sqrt(mean v^2 + eps) over `channels` (1 .. 8192).

@@ -401,8 +401,8 @@ def regenvc_block_norm_forward(x, y=None, *, gate=None, post_norm: int = NORM_NO
                                post_eps: float = 1e-6, residual_scale: float = 1.0, norm: int = NORM_LAYER, weight=None,
                                bias=None, eps: float = 1e-6, scale=None, shift=None, tokens_per_mod=None, h_dtype=None,
                                x_out=None, h=None, stream=None):
-    """x' = residual_scale x + gate N2(y) and h = (N1(x') weight + bias) (1 + scale) + shift in one pass; returns
-    (x' or None where y is None, h or None where norm is NORM_NONE).  x [tokens, C]: bf16, fp16 or fp32; y and h: the
+    """x' = residual_scale x + gate N2(y) post_weight and h = (N1(x') weight + bias) (1 + scale) + shift in one pass (N2(y)
+    is y where post_norm is NORM_NONE); returns (x' or None where y is None, h or None where norm is NORM_NONE).  x [tokens, C]: bf16, fp16 or fp32; y and h: the
     same type, or any of them where x is fp32 (h: ``h_dtype``, else y's, else x's).  gate, scale, shift: fp32 [rows, C],
     one row per ``tokens_per_mod`` tokens (None: one for all); post_weight, weight, bias: fp32 [C].  x may be given as
     ``x_out`` (in place)."""

@@ -1,6 +1,6 @@
 // Norms before and after a transformer block, fused with the block's gate and residual scale, and their gradients.
 //
-//     z  = N2(y) pw  (or y)          x' = a x + g z          h = (N1(x') w + b) (1 + s) + t
+//     z  = N2(y) pw  (or y pw)       x' = a x + g z          h = (N1(x') w + b) (1 + s) + t
 //
 // N is layer norm ((v - mean) r, r = 1 / sqrt(var + eps)) or RMS norm (v r, r = 1 / sqrt(mean v^2 + eps)); g, s, t are
 // rows of a modulation table shared by tokens_per_mod consecutive tokens.  With xhat = N1(x'), yhat = N2(y):

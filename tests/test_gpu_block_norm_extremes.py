@@ -3,9 +3,9 @@ exact.  Bounds as in the norm's own tests."""
 import pytest
 import torch
 
-from block_ops_util import U, half_step
+from block_ops_util import U, half_step, rows_of
 from paper_2607_28144_b200 import binding as B
-from test_gpu_block_norm import DEV, EPS, T, _check, _forward_check
+from test_gpu_block_norm import DEV, EPS, T, _backward_check, _check, _forward_check, _grads, _inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,21 @@ def test_rows_that_differ_by_single_bits(c):
     r, dd = torch.rsqrt((d * d).mean(1, keepdim=True)), dh.double()
     want = r * (dd - dd.mean(1, keepdim=True) - ref * (dd * ref).mean(1, keepdim=True))
     _check(got, want, (64 + 14 * 163) * U * dd.abs().amax(1, keepdim=True) * r * (2 + t) ** 2, "dx")
+
+
+@pytest.mark.parametrize("n,c,per", [(50, 256, 20), (33, 1531, 33), (300, 1536, 1)])
+@pytest.mark.parametrize("xt,iot", [("bf16", "bf16"), ("fp32", "fp16")])
+def test_a_weight_of_the_branch_without_a_norm_of_it(n, c, per, xt, iot):
+    """z = y post_weight, a scale per channel, and its gradients."""
+    x, y, p, r = _inputs(n, c, per, n + c, T[xt], T[iot], True, True, 0, True, True)
+    p["post_weight"] = 1 + 0.2 * r(c)
+    x_out, h = B.regenvc_block_norm_forward(x, y, **p, norm=1, eps=EPS, residual_scale=0.5, tokens_per_mod=per)
+    _forward_check(x, y, p, 1, 0, 0.5, per, x_out, h)
+    dh, more = r(n, c).to(T[iot]), r(n, c).to(T[xt])
+    got = _grads(x_out, y, dh, more, p, 1, 0, 0.5, per)
+    _backward_check(x_out, y, dh, more, p, 1, 0, 0.5, per, got)
+    # dpost_weight (not among those checks without a norm): the sum of gate dx' y.  dx' is dx / 0.5 and carries its rounding;
+    # 256 + n additions and two products
+    dx, g = got["dx"].double() / 0.5, rows_of(p["gate"].double(), per, n)
+    terms = (g * dx * y.double()).abs().sum(0)
+    _check(got["dpost_weight"], (g * dx * y.double()).sum(0), (half_step(T[xt]) + (n + 256 + 4) * U) * terms, "dpost_weight")
