@@ -43,4 +43,12 @@ __device__ __forceinline__ void mx_values8(uint32_t codes, uint32_t* h2) {
         : "r"(codes));
 }
 
+// Eight values -> the e2m1 values nearest to them, as four packed fp16 pairs; by all lanes of a warp.  The two conversions
+// must not meet in one thread's registers: ptxas 12.9 from -O1 on makes zeros of mx_values8(mx_codes8(v)) (the same PTX is
+// right at ptxas -O0, an empty asm statement between the two changes nothing).  An exchange of each lane with itself keeps
+// them apart.
+__device__ __forceinline__ void mx_round8(const float* v, uint32_t* h2) {
+    mx_values8(__shfl_sync(0xffffffffu, mx_codes8(v), threadIdx.x & 31), h2);
+}
+
 }  // namespace regenvc

@@ -113,8 +113,7 @@ __global__ void __launch_bounds__(kThreads) mxfp4_rows_kernel(const MxRowsParams
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = byte == 255u ? 0.0f : v[k] * inv;
             uint32_t h2[4];
-            // (through an exchange with itself: without one the two conversions back to back gave zeros, nvcc 12.9)
-            mx_values8(__shfl_sync(0xffffffffu, mx_codes8(v), threadIdx.x & 31), h2);
+            mx_round8(v, h2);
             if (i < total) {
                 xv[(m * 4 + piece) * blocks + b] = make_uint4(h2[0], h2[1], h2[2], h2[3]);
                 if (piece == 0) xscale[m * blocks + b] = (uint8_t)byte;

@@ -214,3 +214,22 @@ def test_refusals_of_the_binding():
     with pytest.raises(B.RegenvcError) as e:
         B.regenvc_mxfp4_linear(x, w, 12)
     assert e.value.code == B.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_values_of_few_tokens_one_by_one(n, dtype):
+    """Weights with a single 1 per feature give back x as it was taken to 4 bits, exactly: every code, tie and sign, of each
+    token, from x itself and from its packed form."""
+    k = 160
+    x = torch.zeros((n, k), device=DEV)
+    steps = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.2, 0.3, 0.7, 0.8, 4.9, 5.1, 7.5], device=DEV)
+    for b in range(k // 32):
+        x[:, 32 * b] = 7.0                            # fixes the block's scale
+        x[:, 32 * b + 1: 32 * b + 1 + 22] = steps * (-1.0) ** b * 2.0 ** (0 if b < 2 else -3 * b)
+        x[:, 32 * b] *= 2.0 ** (0 if b < 2 else -3 * b)
+    x = (x * torch.exp2(torch.arange(n, device=DEV))[:, None]).to(T[dtype])
+    want = _quantised64(x)
+    w = B.regenvc_mxfp4_quantize(torch.eye(k, device=DEV))
+    assert torch.equal(B.regenvc_mxfp4_linear(x, w, k).double(), want)
+    assert torch.equal(B.regenvc_mxfp4_project(B.regenvc_mxfp4_quantize(x), w, n, k, k).double(), want)
