@@ -225,8 +225,8 @@ int regenvc_block_norm_forward(const regenvc_block_norm_desc* desc, const void* 
  *            dweight, dbias, dscale, dshift need dh
  *   workspace : regenvc_block_norm_workspace_bytes(n_tokens, channels) bytes, 16-byte aligned; calls that may overlap on
  *            the GPU (and graphs that may be replayed at a time) need one each
- * Sums over tokens run in fp32 in an order that depends on the shape and the kind of GPU only: two calls give the same
- * bits.
+ * Sums over tokens run in fp32 in an order that depends on the shape, on whether rows allow 16-byte accesses and on the
+ * kind of GPU only: two calls on the same tensors give the same bits.
  */
 size_t regenvc_block_norm_workspace_bytes(int n_tokens, int channels);
 int regenvc_block_norm_backward(const regenvc_block_norm_desc* desc, const void* x_out, const void* y, const void* gate,

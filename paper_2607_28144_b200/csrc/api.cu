@@ -952,7 +952,7 @@ const char* regenvc_status_string(int status) {
         case REGENVC_ERR_NULL_POINTER: return "null pointer";
         case REGENVC_ERR_BAD_SHAPE: return "bad shape";
         case REGENVC_ERR_UNSUPPORTED: return "unsupported setting (attention: head_dim must be 128, theta > 0; other operators: types and widths as the header lists them; device sm_100)";
-        case REGENVC_ERR_MISALIGNED: return "device pointer not 16-byte aligned";
+        case REGENVC_ERR_MISALIGNED: return "device pointer not aligned as the call needs it (attention: 16 bytes; other operators: as the header lists them)";
         case REGENVC_ERR_ALIASING: return "out overlaps an input";
         case REGENVC_ERR_CUDA: return "CUDA call failed";
         case REGENVC_ERR_TIMEOUT: return "device-side bounded wait expired";

@@ -21,9 +21,10 @@
 // Hence sixteen columns per thread, which halves the share of the sums' exchanges, arithmetic on pairs (f32x2), and
 // asynchronous copies of the rows ahead into a ring in shared memory, which takes no registers: 16-bit rows by the thread
 // that reads them (no barrier), fp32 rows by its warp, rows of odd width or address as images of 16-byte words by the block.
-// Measured: 10920 x 1536 bf16 with residual, gate and modulation 28.5 us (4.7 TB/s of 6.45 measured), 31200 x 5120 with an
-// fp32 stream and RMS norms on both sides 358 us (5.4 TB/s); gradients 49.6 us (4.1 TB/s) and, at 12480 x 5120, 321 us
-// (3.6 TB/s): there the three sums per column take the registers that more rows in flight would need.
+// Measured: 10920 x 1536 bf16 with residual, gate and modulation 28.7 us (4.7 TB/s of 6.45 measured), 31200 x 5120 with an
+// fp32 stream and RMS norms on both sides 324 us in bursts and 331 under the power cap (5.9 and 5.8 TB/s); gradients
+// 49.1 us (4.1 TB/s) and, at 12480 x 5120, 279 us (4.1 TB/s): there the three sums per column take the registers that more
+// rows in flight would need.
 #include "block_norm.cuh"
 #include "row_io.cuh"
 
@@ -925,7 +926,8 @@ cudaError_t plan(BlockNormParams* p, K kernel, int threads, size_t smem, int sm_
 }
 
 // Stages: as many as fit a share of the SM's shared memory (for about `threads_wanted` threads on it), two to four; one
-// where two rows do not fit an SM (fp32 gradients of more than 7000 channels).
+// where two rows do not fit an SM: gradients with an fp32 stream from 5128 channels on (rows read as images: from 5073, or
+// 6761 with 16-bit branches).  Every row then waits for its copies in full.
 Ring plan_ring(uint32_t stage_bytes, uint32_t other_bytes, int threads, int threads_wanted) {
     const int blocks = threads_wanted / threads > 1 ? threads_wanted / threads : 1;
     int stages = (int)((224000u / blocks - other_bytes) / stage_bytes);

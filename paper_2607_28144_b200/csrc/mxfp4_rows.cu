@@ -3,7 +3,7 @@
 // launch.
 //
 // Bound: the weights' bytes from HBM (17 / 32 byte per weight), and at small sizes the launch itself.  For more than one
-// token and 2^24 weights or more the tensor-core product takes over, although it computes 128 rows (2 x 5120 -> 15360: 23
+// token and 2^24 weights or more the tensor-core product takes over, although it computes 128 rows (2 x 5120 -> 15360: 20.5
 // against 46 us; 4 x 5120 -> 5120: 19 against 21 us).  Every thread block first takes all of x to e2m1 values (as fp16,
 // which holds them) in shared memory, while its first weights are on their way.  A half warp then walks over groups of FP
 // output features: a lane reads 16 bytes = one block of 32 weights per feature, up to eight of them in flight at a time.  Sixteen products are summed in packed fp16 -- exactly:

@@ -8,8 +8,9 @@
 // Bound: HBM (every element is read and written once).  The angles of a token are shared by all heads of q and k, so a
 // thread block computes them once per token into shared memory (a few 64-bit operations per pair against heads * 2
 // elements) and then walks over its (token, head) vectors.  A thread keeps its place within a head; four vectors per
-// thread are loaded before the first is used.  Measured: 31200 tokens x 80 heads x 128 bf16 207 us (6.2 TB/s of 6.45
-// measured), 4097 x 48 heads x 128 fp16 in half pairs 22.7 us (4.4 TB/s, one round of blocks).
+// thread are loaded before the first is used.  Measured: 31200 tokens x 80 heads x 128 bf16 207 us in a burst (6.2 TB/s of
+// 6.45 measured), 215 to 219 us call after call, when the power cap takes the SM clock from 1965 to 1807 MHz (5.8 TB/s);
+// 4097 x 48 heads x 128 fp16 in half pairs 22.6 us (4.5 TB/s, one round of blocks).
 #include "rope_axes.cuh"
 #include "row_io.cuh"
 
