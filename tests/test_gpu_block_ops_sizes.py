@@ -74,3 +74,18 @@ def test_rotation(n, hq, hk, halves, dtype):
         for x, y in zip((q, k), got):
             ref, mag = rope64(x.double(), pos, [44, 42, 42] if not halves else [32, 48, 48], 1e4, halves, False, inverse)
             assert ((y.double() - ref).abs() <= half_step(T[dtype]) * ref.abs() + 2.0 ** -21 * mag + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("norm", [0, 1, 2])
+@pytest.mark.parametrize("post", [0, 1, 2])
+@pytest.mark.parametrize("xt,iot", [("bf16", "bf16"), ("fp32", "bf16"), ("fp32", "fp32")])
+def test_gradients_of_every_pair_of_norms(norm, post, xt, iot):
+    """Which sums share an exchange depends on both norms and on the types; rows of one warp, of several, and as images."""
+    for n, c, per in ((700, 200, 300), (900, 1536, 900), (300, 5120, 77), (400, 1531, 133)):
+        x, y, p, r = _inputs(n, c, per, n + c, T[xt], T[iot], True, True, post, norm > 0, norm > 0)
+        dh, more = (r(n, c).to(T[iot]) if norm else None), r(n, c).to(T[xt])
+        got = _grads(x, y, dh, more, p, norm, post, 0.5, per)
+        _backward_check(x, y, dh, more, p, norm, post, 0.5, per, got)
+        xo, h = B.regenvc_block_norm_forward(x, y, **p, norm=norm, post_norm=post, residual_scale=0.5, eps=EPS, post_eps=EPS,
+                                             tokens_per_mod=per)
+        _forward_check(x, y, p, norm, post, 0.5, per, xo, h)
