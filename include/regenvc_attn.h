@@ -263,6 +263,109 @@ int regenvc_rope_axes(const regenvc_rope_axes_desc* desc, const void* q, const v
                       void* q_out, void* k_out, void* stream);
 
 /*
+ * Queries and keys of every head normalised and rotated in one pass: y = R(position) (x / sqrt(mean(x^2) + eps) * weight),
+ * the mean over the head_dim elements of one head, R as in regenvc_rope_axes().  Nothing is rounded between norm and rotation.
+ *   q, k : type, strided as in regenvc_rope_axes(); either may be absent (0 heads, NULL).  A result may be its operand (in
+ *          place, same strides); views of one fused tensor may interleave; other overlaps are refused
+ *   q_weight, k_weight : fp32 [head_dim] or NULL (ones), shared by the heads
+ *   positions, n_axes, widths, halves, whole_ladder, pos_float, rope_theta : as there; n_axes 0 (and positions NULL): no
+ *          rotation
+ * A row whose sum of squares passes fp32's range normalises to 0.
+ * The gradients take the operands again (no statistics are kept): dq_out, dk_out with the strides of q_out, k_out; dq and dk
+ * may be them in place; dq_weight, dk_weight: fp32 [head_dim], NULL where not wanted, need q_weight, k_weight and `workspace`
+ * (regenvc_qk_norm_rope_workspace_bytes(), 16-byte aligned, one for each of the calls that may overlap on the GPU; else
+ * NULL).  Sums have a fixed order: two calls on the same tensors give the same bits.
+ */
+typedef struct {
+    int n_tokens, n_q_heads, n_k_heads, head_dim;   /* head_dim even, 2 .. 256 */
+    int type;                   /* regenvc_type */
+    int n_axes, widths[4];
+    float rope_theta;
+    int halves, whole_ladder, pos_float;
+    float eps;                  /* >= 0 */
+    long long pos_stride;       /* strides in elements, 0: packed */
+    long long q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+    long long q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+    long long dq_token_stride, dq_head_stride, dk_token_stride, dk_head_stride;   /* gradients only */
+} regenvc_qk_norm_rope_desc;
+int regenvc_qk_norm_rope_forward(const regenvc_qk_norm_rope_desc* desc, const void* q, const void* k, const void* q_weight,
+                                 const void* k_weight, const void* positions, void* q_out, void* k_out, void* stream);
+size_t regenvc_qk_norm_rope_workspace_bytes(int head_dim);
+int regenvc_qk_norm_rope_backward(const regenvc_qk_norm_rope_desc* desc, const void* dq_out, const void* dk_out, const void* q,
+                                  const void* k, const void* q_weight, const void* k_weight, const void* positions, void* dq,
+                                  void* dk, void* dq_weight, void* dk_weight, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/*
+ * Keys and values of earlier windows kept on the GPU, so that the tokens of a new window (a latent frame, a single token)
+ * attend to them: a paged cache for any number of streams, and attention over it.
+ *
+ * The cache is two tensors of pages, keys and values: element (page, slot, head, i) at page * page_stride + slot *
+ * slot_stride + head * head_stride + i, in any order of the strides (0: packed [pages][slots][heads][head_dim]).  Token t of
+ * sequence s lies in slot t % page_size of page block_table[s * table_stride + t / page_size].
+ *   row_starts : int32 [n_sequences + 1], ascending; rows row_starts[s] .. row_starts[s + 1] - 1 of the call's tensors are
+ *                sequence s's new tokens (none: equal); rows behind the last sequence (a padded batch) are left as they were
+ *   lengths    : int32 [n_sequences], cached tokens of each sequence with the new ones, which are the last of them
+ *   block_table: int32; entries behind a sequence's last page are not read
+ * All three are read on the device when the call runs, so a captured call follows them.  Where they contradict the sizes in
+ * the description (a page outside 0 .. n_pages - 1, more tokens than the table holds, fewer than the new ones in an append,
+ * descending starts), nothing outside the tensors is touched, regenvc_device_status() reports REGENVC_ERR_RANGE (until
+ * then later attention calls skip their work) and the results of the call are unspecified.  1 <= n_sequences <= 4096.
+ *
+ * regenvc_paged_append(): k (normalised per head where norm is REGENVC_NORM_RMS, rotated where n_axes > 0, as in
+ *   regenvc_qk_norm_rope_forward()) and v (as it is) of the call's tokens into their slots, and, where given, q -> q_out in
+ *   the same way (q may be q_out).  positions: [n_axes][n_tokens], of the call's rows.  cache elements have k's type.
+ * regenvc_paged_attn_forward(): out = softmax(scale q k^T) v over the cached tokens that a row sees.
+ *   q, out : bf16 or fp16 like the caches [n_tokens][n_q_heads][head_dim], head_dim 64 or 128; n_q_heads a multiple of
+ *            n_k_heads, query head a reads head a / (n_q_heads / n_k_heads) of the cache
+ *   group  : 0: every row of a sequence sees all its cached tokens.  b >= 1: the token at position p (of its sequence) sees
+ *            the tokens of its own group of b and of those before it: t / b <= p / b.  1 is the causal mask, the tokens of a
+ *            latent frame make it causal by frames
+ *   window : 0, or (with group >= 1) the number of groups seen, its own among them: t / b > p / b - window; pages of tokens
+ *            that no new token sees need not exist any more
+ *   scale  : > 0, or 0 for 1 / sqrt(head_dim)
+ *   lse    : fp32 [n_tokens][n_q_heads] or NULL: natural logarithm of the sum of the exponentials of a row's scores
+ *   A row that sees nothing gives zeros (lse -inf).  What lies in unseen slots (behind a length, before the window of all
+ *   of a call's rows, in unused pages) does not matter; tokens that any new token of their sequence sees must be finite.
+ *   page_size: a multiple of 8 (REGENVC_ERR_UNSUPPORTED); rows of q, out and the caches allow 16-byte accesses
+ *   (REGENVC_ERR_MISALIGNED).  Probabilities are rounded to the cache's type, everything else is fp32.
+ *   workspace : regenvc_paged_attn_workspace_bytes() bytes (0 for invalid arguments), 16-byte aligned, its content of no
+ *            matter; calls that may overlap on the GPU (and graphs that may be replayed at a time) need one each
+ *   Waits inside are bounded as in the other attention kernels.  The same call on the same lengths gives the same bits.
+ */
+typedef struct {
+    int n_tokens, n_q_heads, n_k_heads, head_dim;   /* n_q_heads 0: no q */
+    int type;
+    int n_axes, widths[4];      /* n_axes 0: no rotation */
+    float rope_theta;
+    int halves, whole_ladder, pos_float;
+    float eps;
+    int norm;                   /* REGENVC_NORM_NONE or REGENVC_NORM_RMS */
+    int n_sequences, page_size, n_pages, pages_per_sequence;
+    long long pos_stride;       /* strides in elements, 0: packed */
+    long long q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    long long q_out_token_stride, q_out_head_stride, table_stride;
+    long long k_page_stride, k_slot_stride, k_cache_head_stride, v_page_stride, v_slot_stride, v_cache_head_stride;
+} regenvc_paged_append_desc;
+int regenvc_paged_append(const regenvc_paged_append_desc* desc, const void* q, const void* k, const void* v,
+                         const void* q_weight, const void* k_weight, const void* positions, const void* row_starts,
+                         const void* lengths, const void* block_table, void* q_out, void* k_cache, void* v_cache, void* stream);
+
+typedef struct {
+    int n_tokens, n_q_heads, n_k_heads, head_dim;
+    int type;                   /* REGENVC_BF16 or REGENVC_F16 */
+    int n_sequences, page_size, n_pages, pages_per_sequence;
+    int group, window;
+    float scale;
+    long long q_token_stride, q_head_stride, out_token_stride, out_head_stride, table_stride;   /* elements, 0: packed */
+    long long k_page_stride, k_slot_stride, k_head_stride, v_page_stride, v_slot_stride, v_head_stride;
+} regenvc_paged_attn_desc;
+size_t regenvc_paged_attn_workspace_bytes(int n_q_heads, int n_k_heads, int head_dim);
+int regenvc_paged_attn_forward(const regenvc_paged_attn_desc* desc, const void* q, const void* k_cache, const void* v_cache,
+                               const void* row_starts, const void* lengths, const void* block_table, void* out, void* lse,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Microscaled 4-bit floating point (OCP MX: e2m1 elements, one e8m0 scale per 32 columns of a row): the projections
  * with a quarter of the operand bytes and up to four times the tensor rate of bf16.
  *
@@ -464,8 +567,9 @@ int regenvc_debug_set_phases(int mask);
  * REGENVC_ERR_TIMEOUT until regenvc_device_status() reads it.  Kernels of this
  * library that start while the word is set skip their work (their bounded
  * waits fall through) and leave `out` unspecified.  Nothing faults or hangs.
- * (Kernels without such waits -- block norm, rotation, 4-bit conversion and the
- * one-kernel form of the 4-bit product -- run as always.)
+ * (Kernels without such waits -- block norm, rotation, the norm of queries and
+ * keys, the append to a paged cache, 4-bit conversion and the one-kernel form of
+ * the 4-bit product -- run as always.)
  */
 int regenvc_debug_expire_wait(int limit_us, void* stream);
 

@@ -34,6 +34,8 @@ EXPORTS = [
     "regenvc_block_norm_forward", "regenvc_block_norm_backward", "regenvc_block_norm_workspace_bytes",
     "regenvc_rope_axes", "regenvc_mxfp4_bytes", "regenvc_mxfp4_quantize", "regenvc_mxfp4_dequantize",
     "regenvc_mxfp4_project", "regenvc_mxfp4_linear", "regenvc_mxfp4_linear_scratch_bytes",
+    "regenvc_qk_norm_rope_forward", "regenvc_qk_norm_rope_backward", "regenvc_qk_norm_rope_workspace_bytes",
+    "regenvc_paged_append", "regenvc_paged_attn_forward", "regenvc_paged_attn_workspace_bytes",
 ]
 
 
@@ -54,6 +56,39 @@ class RopeAxesDesc(ctypes.Structure):
                [(n, ctypes.c_longlong) for n in ("pos_stride", "q_token_stride", "q_head_stride", "k_token_stride",
                                                  "k_head_stride", "q_out_token_stride", "q_out_head_stride",
                                                  "k_out_token_stride", "k_out_head_stride")]
+
+
+def _rotation_fields(extra, strides):
+    return [(n, ctypes.c_int) for n in ("n_tokens", "n_q_heads", "n_k_heads", "head_dim", "type", "n_axes")] + \
+           [("widths", ctypes.c_int * 4), ("rope_theta", ctypes.c_float)] + \
+           [(n, ctypes.c_int) for n in ("halves", "whole_ladder", "pos_float")] + [("eps", ctypes.c_float)] + \
+           [(n, ctypes.c_int) for n in extra] + [(n, ctypes.c_longlong) for n in strides]
+
+
+class QkNormRopeDesc(ctypes.Structure):
+    """``regenvc_qk_norm_rope_desc``."""
+    _fields_ = _rotation_fields((), ("pos_stride", "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                     "q_out_token_stride", "q_out_head_stride", "k_out_token_stride", "k_out_head_stride",
+                                     "dq_token_stride", "dq_head_stride", "dk_token_stride", "dk_head_stride"))
+
+
+class PagedAppendDesc(ctypes.Structure):
+    """``regenvc_paged_append_desc``."""
+    _fields_ = _rotation_fields(("norm", "n_sequences", "page_size", "n_pages", "pages_per_sequence"),
+                                ("pos_stride", "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                 "v_token_stride", "v_head_stride", "q_out_token_stride", "q_out_head_stride", "table_stride",
+                                 "k_page_stride", "k_slot_stride", "k_cache_head_stride", "v_page_stride", "v_slot_stride",
+                                 "v_cache_head_stride"))
+
+
+class PagedAttnDesc(ctypes.Structure):
+    """``regenvc_paged_attn_desc``."""
+    _fields_ = [(n, ctypes.c_int) for n in ("n_tokens", "n_q_heads", "n_k_heads", "head_dim", "type", "n_sequences",
+                                            "page_size", "n_pages", "pages_per_sequence", "group", "window")] + \
+               [("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_longlong) for n in ("q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride",
+                                                 "table_stride", "k_page_stride", "k_slot_stride", "k_head_stride",
+                                                 "v_page_stride", "v_slot_stride", "v_head_stride")]
 
 
 _lib = None
@@ -127,6 +162,18 @@ def lib() -> ctypes.CDLL:
     L.regenvc_mxfp4_project.restype = i32
     L.regenvc_mxfp4_linear.argtypes = [vp, i32, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp]
     L.regenvc_mxfp4_linear.restype = i32
+    L.regenvc_qk_norm_rope_forward.argtypes = [vp] * 9
+    L.regenvc_qk_norm_rope_forward.restype = i32
+    L.regenvc_qk_norm_rope_workspace_bytes.argtypes = [i32]
+    L.regenvc_qk_norm_rope_workspace_bytes.restype = sz
+    L.regenvc_qk_norm_rope_backward.argtypes = [vp] * 13 + [sz, vp]
+    L.regenvc_qk_norm_rope_backward.restype = i32
+    L.regenvc_paged_append.argtypes = [vp] * 14
+    L.regenvc_paged_append.restype = i32
+    L.regenvc_paged_attn_workspace_bytes.argtypes = [i32, i32, i32]
+    L.regenvc_paged_attn_workspace_bytes.restype = sz
+    L.regenvc_paged_attn_forward.argtypes = [vp] * 10 + [sz, vp]
+    L.regenvc_paged_attn_forward.restype = i32
     L.regenvc_workspace_bytes.argtypes = [i32, i32, i32]
     L.regenvc_workspace_bytes.restype = sz
     L.regenvc_set_workspace.argtypes = [vp, sz]
@@ -646,6 +693,226 @@ def regenvc_mxfp4_linear(x, w_packed, out_features: int, bias=None, *, y_dtype=t
                                       y.data_ptr(), TYPES[y.dtype], n, out_features, cols, _addr(scratch),
                                       _launch_stream(stream, index)))
     return y
+
+
+# ------------------------------------------------------------------------------------- attention over cached windows
+_QKNORM_DESC, _APPEND_DESC, _PAGED_DESC = struct.Struct("@10if3if13q"), struct.Struct("@10if3if5i16q"), struct.Struct("@11if11q")
+assert _QKNORM_DESC.size == ctypes.sizeof(QkNormRopeDesc) and _APPEND_DESC.size == ctypes.sizeof(PagedAppendDesc) \
+    and _PAGED_DESC.size == ctypes.sizeof(PagedAttnDesc)
+
+
+def _head_strides(t, name: str, dtype, n: int, heads: int, d: int):
+    """(token, head) strides of [tokens, heads, head_dim] vectors as the library takes them (0, 0: packed)."""
+    if t is None:
+        return 0, 0
+    if t.dtype is not dtype or t.shape != (n, heads, d):
+        raise TypeError(f"{name} must be {dtype} [{n}, {heads}, {d}]")
+    if t.is_contiguous():
+        return 0, 0
+    token, head, step = t.stride()
+    if d > 1 and step != 1:
+        raise TypeError(f"{name} must have neighbouring elements of a head")
+    if (n > 1 and token < d) or (heads > 1 and head < d):
+        raise ValueError(f"{name} has vectors that overlap (an expanded tensor?)")
+    head = head if heads > 1 else d       # the stride of an axis with one entry is never used: name the packed one
+    return (token if n > 1 else heads * head), head
+
+
+def _rotation(positions, widths, n: int):
+    """(axes, four widths, fp32 positions, stride between axes) of an optional rotation."""
+    if positions is None:
+        if widths is not None and len(widths):
+            raise ValueError("widths need positions")
+        return 0, (0, 0, 0, 0), False, 0
+    widths = list(widths)
+    if positions.dtype not in (torch.int32, torch.float32) or positions.shape != (len(widths), n) or \
+            (n > 1 and positions.stride(1) != 1) or (len(widths) > 1 and positions.stride(0) < n):
+        raise TypeError(f"positions must be int32 or fp32 [{len(widths)}, {n}] with neighbouring tokens")
+    if not 1 <= len(widths) <= 4:
+        raise RegenvcError(ERR_BAD_SHAPE, status_string(ERR_BAD_SHAPE))
+    return len(widths), (widths + [0, 0, 0])[:4], positions.dtype is torch.float32, \
+        positions.stride(0) if len(widths) > 1 else 0
+
+
+def _heads_of(q, k):
+    """(tokens, query heads, key heads, head_dim, type) of q and k, either of which may be None."""
+    like = q if q is not None else k
+    if like is None or like.dim() != 3 or like.dtype not in TYPES:
+        raise TypeError("q and k must be [tokens, heads, head_dim] in bf16, fp16 or fp32")
+    if q is not None and k is not None and (k.dtype != q.dtype or k.dim() != 3 or k.shape[0] != q.shape[0] or
+                                            k.shape[2] != q.shape[2]):
+        raise TypeError("k must be [tokens, heads, head_dim] of q's type")
+    return like.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], like.shape[2], like.dtype
+
+
+def regenvc_qk_norm_rope_forward(q, k, positions=None, widths=None, *, q_weight=None, k_weight=None, eps: float = 1e-6,
+                                 rope_theta: float = 10000.0, halves: bool = False, whole_ladder: bool = False, q_out=None,
+                                 k_out=None, stream=None):
+    """Every head of q and k [tokens, heads, head_dim] (either may be None) divided by its root mean square, times the gains
+    q_weight / k_weight (fp32 [head_dim], None: ones), and rotated by ``positions`` as in regenvc_rope_axes (None: not);
+    returns (q_out, k_out).  Strided views are taken as they are; q / k given as q_out / k_out are replaced in place."""
+    n, hq, hk, d, dtype = _heads_of(q, k)
+    index = _place(q if q is not None else k, k, positions, q_weight, k_weight, q_out, k_out)
+    axes, four, as_float, between = _rotation(positions, widths, n)
+    _vector(q_weight, "q_weight", d)
+    _vector(k_weight, "k_weight", d)
+    if (q is None and (q_out is not None or q_weight is not None)) or (k is None and (k_out is not None or k_weight is not None)):
+        raise ValueError("a result and gains need their operand")
+    if q is not None and q_out is None:
+        q_out = _like(q, stream)
+    if k is not None and k_out is None:
+        k_out = _like(k, stream)
+    desc = _QKNORM_DESC.pack(n, hq, hk, d, TYPES[dtype], axes, *four, rope_theta, bool(halves), bool(whole_ladder), as_float, eps,
+                             between, *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(k, "k", dtype, n, hk, d),
+                             *_head_strides(q_out, "q_out", dtype, n, hq, d), *_head_strides(k_out, "k_out", dtype, n, hk, d),
+                             0, 0, 0, 0)
+    _check(lib().regenvc_qk_norm_rope_forward(desc, _addr(q), _addr(k), _addr(q_weight), _addr(k_weight), _addr(positions),
+                                              _addr(q_out), _addr(k_out), _launch_stream(stream, index)))
+    return q_out, k_out
+
+
+def regenvc_qk_norm_rope_workspace_bytes(head_dim: int) -> int:
+    return int(lib().regenvc_qk_norm_rope_workspace_bytes(head_dim))
+
+
+def regenvc_qk_norm_rope_backward(dq_out, dk_out, q, k, positions=None, widths=None, *, q_weight=None, k_weight=None,
+                                  eps: float = 1e-6, rope_theta: float = 10000.0, halves: bool = False,
+                                  whole_ladder: bool = False, dq=None, dk=None, workspace=None, stream=None):
+    """Gradients of regenvc_qk_norm_rope_forward at its operands q and k, from those of its results.  Returns a dict: dq, dk,
+    dq_weight, dk_weight, each None where its operand is.  ``dq`` / ``dk`` may be dq_out / dk_out (in place)."""
+    n, hq, hk, d, dtype = _heads_of(q, k)
+    index = _place(q if q is not None else k, k, dq_out, dk_out, positions, q_weight, k_weight, dq, dk, workspace)
+    if (q is None) != (dq_out is None) or (k is None) != (dk_out is None) or (q is None and (dq is not None or q_weight is not None)) \
+            or (k is None and (dk is not None or k_weight is not None)):
+        raise ValueError("q and k need the gradients of their results, and those need them")
+    axes, four, as_float, between = _rotation(positions, widths, n)
+    _vector(q_weight, "q_weight", d)
+    _vector(k_weight, "k_weight", d)
+    if q is not None and dq is None:
+        dq = _like(q, stream)
+    if k is not None and dk is None:
+        dk = _like(k, stream)
+    dqw = None if q_weight is None else _new((d,), torch.float32, q.device, stream)
+    dkw = None if k_weight is None else _new((d,), torch.float32, k.device, stream)
+    if workspace is None and (dqw is not None or dkw is not None):
+        workspace = _new((regenvc_qk_norm_rope_workspace_bytes(d),), torch.uint8, (q if q is not None else k).device, stream)
+    desc = _QKNORM_DESC.pack(n, hq, hk, d, TYPES[dtype], axes, *four, rope_theta, bool(halves), bool(whole_ladder), as_float, eps,
+                             between, *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(k, "k", dtype, n, hk, d),
+                             *_head_strides(dq_out, "dq_out", dtype, n, hq, d), *_head_strides(dk_out, "dk_out", dtype, n, hk, d),
+                             *_head_strides(dq, "dq", dtype, n, hq, d), *_head_strides(dk, "dk", dtype, n, hk, d))
+    _check(lib().regenvc_qk_norm_rope_backward(
+        desc, _addr(dq_out), _addr(dk_out), _addr(q), _addr(k), _addr(q_weight), _addr(k_weight), _addr(positions), _addr(dq),
+        _addr(dk), _addr(dqw), _addr(dkw), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _launch_stream(stream, index)))
+    return {"dq": dq, "dk": dk, "dq_weight": dqw, "dk_weight": dkw}
+
+
+def _cache(t, name: str, dtype, like=None):
+    """(page, slot, head) strides of a cache [pages, slots, heads, head_dim], as the library takes them (0: packed)."""
+    if t.dim() != 4 or t.dtype is not dtype or (like is not None and t.shape != like.shape):
+        raise TypeError(f"{name} must be {dtype} [pages, slots of a page, heads, head_dim], both caches alike")
+    if t.is_contiguous():
+        return 0, 0, 0
+    if t.stride(3) != 1 and t.shape[3] > 1:
+        raise TypeError(f"{name} must have neighbouring elements of a head")
+    pages, slots, heads, d = t.shape
+    strides = list(t.stride()[:3])
+    for i, count in enumerate((pages, slots, heads)):
+        if count == 1:                     # never used: behind everything else
+            strides[i] = 0
+        elif strides[i] < d:
+            raise ValueError(f"{name} has vectors that overlap (an expanded tensor?)")
+    top = max([d] + [s * c for s, c in zip(strides, (pages, slots, heads))])
+    return tuple(s or -(-top // 8) * 8 for s in strides)
+
+
+def _paged_lists(block_table, lengths, row_starts):
+    """(sequences, pages per sequence, table stride)."""
+    if block_table.dim() != 2 or block_table.dtype is not torch.int32 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise TypeError("block_table must be int32 [sequences, pages] with neighbouring pages")
+    s, wide = block_table.shape
+    if lengths.dtype is not torch.int32 or lengths.shape != (s,) or not lengths.is_contiguous():
+        raise TypeError(f"lengths must be a contiguous int32 tensor of {s} elements")
+    if row_starts.dtype is not torch.int32 or row_starts.shape != (s + 1,) or not row_starts.is_contiguous():
+        raise TypeError(f"row_starts must be a contiguous int32 tensor of {s + 1} elements")
+    stride = block_table.stride(0) if s > 1 else 0
+    if s > 1 and stride < wide:
+        raise ValueError("block_table has rows that overlap (an expanded tensor?)")
+    return s, wide, stride
+
+
+def regenvc_paged_append(k, v, k_cache, v_cache, block_table, lengths, row_starts, *, q=None, positions=None, widths=None,
+                         norm: int = NORM_NONE, q_weight=None, k_weight=None, eps: float = 1e-6, rope_theta: float = 10000.0,
+                         halves: bool = False, whole_ladder: bool = False, q_out=None, stream=None):
+    """New tokens' k and v [tokens, heads, head_dim] into a paged cache [pages, slots of a page, heads, head_dim] (any order of
+    strides), k normalised (``norm`` NORM_RMS, gains k_weight) and rotated by ``positions`` (None: not) on the way; returns
+    q_out, q taken the same way (None without q; q given as q_out is replaced in place).  ``row_starts`` int32
+    [sequences + 1]: the rows of each sequence's new tokens; ``lengths`` int32 [sequences]: its cached tokens with the new
+    ones, which are the last; ``block_table`` int32 [sequences, pages]."""
+    n, hq, hk, d, dtype = _heads_of(q, k)
+    if k is None or k.dim() != 3:
+        raise TypeError("k must be [tokens, heads, head_dim]")
+    index = _place(k, v, q, k_cache, v_cache, block_table, lengths, row_starts, positions, q_weight, k_weight, q_out)
+    axes, four, as_float, between = _rotation(positions, widths, n)
+    _vector(q_weight, "q_weight", d)
+    _vector(k_weight, "k_weight", d)
+    if q is None and (q_out is not None or q_weight is not None):
+        raise ValueError("q_out and q_weight need q")
+    if norm == NORM_NONE and (q_weight is not None or k_weight is not None):
+        raise ValueError("gains need a norm")
+    seqs, wide, table_stride = _paged_lists(block_table, lengths, row_starts)
+    k_strides, v_strides = _cache(k_cache, "k_cache", dtype), _cache(v_cache, "v_cache", dtype, k_cache)
+    if k_cache.shape[2:] != (hk, d):
+        raise TypeError(f"the caches must hold {hk} heads of {d}")
+    if q is not None and q_out is None:
+        q_out = _like(q, stream)
+    desc = _APPEND_DESC.pack(n, hq, hk, d, TYPES[dtype], axes, *four, rope_theta, bool(halves), bool(whole_ladder), as_float, eps,
+                             norm, seqs, k_cache.shape[1], k_cache.shape[0], wide, between,
+                             *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(k, "k", dtype, n, hk, d),
+                             *_head_strides(v, "v", dtype, n, hk, d), *_head_strides(q_out, "q_out", dtype, n, hq, d),
+                             table_stride, *k_strides, *v_strides)
+    _check(lib().regenvc_paged_append(desc, _addr(q), k.data_ptr(), v.data_ptr(), _addr(q_weight), _addr(k_weight),
+                                      _addr(positions), row_starts.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
+                                      _addr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _launch_stream(stream, index)))
+    return q_out
+
+
+def regenvc_paged_attn_workspace_bytes(n_q_heads: int, n_k_heads: int, head_dim: int) -> int:
+    return int(lib().regenvc_paged_attn_workspace_bytes(n_q_heads, n_k_heads, head_dim))
+
+
+def regenvc_paged_attn_forward(q, k_cache, v_cache, block_table, lengths, row_starts, *, group: int = 0, window: int = 0,
+                               scale=None, out=None, lse=None, workspace=None, stream=None):
+    """Attention of each sequence's new tokens q [tokens, heads, head_dim] (rows ``row_starts``) over its cached tokens, the new
+    ones (already appended) among them; returns (out, lse).  ``group`` 0: every row sees them all; 1: causal; b: causal by
+    groups of b tokens (a latent frame), ``window`` of them at most (0: all).  ``lse``: None, or True or an fp32 tensor
+    [tokens, heads] for the logarithms of the rows' sums.  ``workspace``: uint8, regenvc_paged_attn_workspace_bytes() long."""
+    if q.dim() != 3 or q.dtype not in TYPES:
+        raise TypeError("q must be [tokens, heads, head_dim] in bf16 or fp16")
+    n, hq, d = q.shape
+    dtype = q.dtype
+    seqs, wide, table_stride = _paged_lists(block_table, lengths, row_starts)
+    k_strides, v_strides = _cache(k_cache, "k_cache", dtype), _cache(v_cache, "v_cache", dtype, k_cache)
+    pages, slots, hk, dc = k_cache.shape
+    if dc != d:
+        raise TypeError(f"the caches must hold heads of {d}")
+    if lse is True:
+        lse = _new((n, hq), torch.float32, q.device, stream)
+    elif lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, hq) or not lse.is_contiguous()):
+        raise TypeError(f"lse must be a contiguous fp32 tensor [{n}, {hq}]")
+    index = _place(q, k_cache, v_cache, block_table, lengths, row_starts, out, lse, workspace)
+    if out is None:
+        out = _like(q, stream)
+    if workspace is None:
+        workspace = _new((max(regenvc_paged_attn_workspace_bytes(hq, hk, d), 1),), torch.uint8, q.device, stream)
+    desc = _PAGED_DESC.pack(n, hq, hk, d, TYPES[dtype], seqs, slots, pages, wide, group, window, 0.0 if scale is None else scale,
+                            *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(out, "out", dtype, n, hq, d), table_stride,
+                            *k_strides, *v_strides)
+    _check(lib().regenvc_paged_attn_forward(desc, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), row_starts.data_ptr(),
+                                            lengths.data_ptr(), block_table.data_ptr(), out.data_ptr(), _addr(lse),
+                                            workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                            _launch_stream(stream, index)))
+    return out, lse
 
 
 def regenvc_cross_attn_forward_static(q, k, v, out, stream=None):

@@ -13,6 +13,7 @@
 #include "../../include/regenvc_attn.h"
 #include "common.cuh"
 #include "mxfp4.cuh"
+#include "paged_attn.cuh"
 
 
 namespace {
@@ -131,6 +132,7 @@ int device_state(int* dev_out, DeviceState** st_out) {
             CUDA_TRY(configure_out_project());
             CUDA_TRY(configure_attn_persistent());
             CUDA_TRY(configure_mxfp4_project());
+            CUDA_TRY(configure_paged_attn());
             CUDA_TRY(cudaMalloc(&st.status, sizeof(int)));
             CUDA_TRY(cudaMemset(st.status, 0, sizeof(int)));
         }
@@ -531,6 +533,21 @@ int encode_map(CUtensorMap* m, CUtensorMapDataType type, void* base, uint64_t in
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r == CUDA_SUCCESS) return REGENVC_OK;
     tl_cuda_error = "cuTensorMapEncodeTiled failed with CUresult " + std::to_string((int)r);
+    return REGENVC_ERR_CUDA;
+}
+int encode_map_4d(CUtensorMap* m, CUtensorMapDataType type, void* base, const uint64_t* extent, const uint64_t* stride_bytes,
+                  const uint32_t* box, CUtensorMapSwizzle swizzle) {
+    const cuuint64_t gdim[4] = {extent[0], extent[1], extent[2], extent[3]};
+    const cuuint64_t gstride[3] = {stride_bytes[0], stride_bytes[1], stride_bytes[2]};
+    const cuuint32_t boxes[4] = {box[0], box[1], box[2], box[3]};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    const CUresult r = g_encode(m, type, 4, base, gdim, gstride, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return REGENVC_OK;
+    try {
+        tl_cuda_error = "cuTensorMapEncodeTiled failed with CUresult " + std::to_string((int)r);
+    } catch (...) {   // out of host memory: no exception leaves a C entry point
+    }
     return REGENVC_ERR_CUDA;
 }
 }  // namespace regenvc

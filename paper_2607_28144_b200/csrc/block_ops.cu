@@ -1,41 +1,13 @@
 // Entry points of the operators around a block's attention: norms fused with gate and residual scale, rotation by
 // explicit positions, microscaled 4-bit matrices.  Arguments are checked before any CUDA call; nothing is allocated.
-#include <cmath>
-
-#include "../../include/regenvc_attn.h"
 #include "block_norm.cuh"
-#include "common.cuh"
 #include "mxfp4.cuh"
+#include "op_checks.cuh"
 #include "rope_axes.cuh"
 
 namespace {
 
 using namespace regenvc;
-
-bool type_ok(int t) { return t == REGENVC_BF16 || t == REGENVC_F16 || t == REGENVC_F32; }
-size_t type_size(int t) { return t == REGENVC_F32 ? 4 : 2; }
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
-// Bytes from an operand's first to its last element, for overlap tests.
-struct Span {
-    const void* p;
-    size_t bytes;
-};
-Span rows_span(const void* p, long long rows, long long stride, long long width, size_t size) {
-    return Span{p, p ? ((size_t)(rows - 1) * (size_t)stride + (size_t)width) * size : 0};
-}
-bool meet(const Span& a, const Span& b) {
-    if (!a.p || !b.p) return false;
-    const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-    return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
-}
-// An element's index times its size stays far inside 64 bits.
-constexpr long long kMaxStride = 1ll << 31;
-
-int launch_done(cudaError_t e, const char* what, int launches) {
-    for (int i = 0; i < launches; ++i) count_launch();
-    return e == cudaSuccess ? REGENVC_OK : record_cuda_failure(e, what);
-}
 
 // ------------------------------------------------------------------------------------------------ block norm
 struct NormArgs {
@@ -386,20 +358,7 @@ int regenvc_rope_axes(const regenvc_rope_axes_desc* d, const void* q, const void
         if (!(same[0] && apart(2, 1)) && meet(span[2], span[1])) return REGENVC_ERR_ALIASING;
         if (!(same[1] && apart(3, 0)) && meet(span[3], span[0])) return REGENVC_ERR_ALIASING;
     }
-    // Frequencies as turns per unit of position: powers of one ratio per ladder, multiplied up in extended precision (64
-    // factors add up to 2^-58) and rounded to 64 bits.
-    const long double turn = 1.0L / 6.283185307179586476925286766559L;
-    int j = 0;
-    for (int a = 0; a < d->n_axes; ++a) {
-        const int pairs = d->widths[a] / 2;
-        if (a == 0 || !d->whole_ladder) {
-            p.turns[j] = (double)turn;
-            const long double ratio = std::pow((long double)d->rope_theta, -1.0L / (d->whole_ladder ? p.n_pairs : pairs));
-            long double f = turn;
-            for (int i = 1; i < (d->whole_ladder ? p.n_pairs : pairs); ++i) p.turns[j + i] = (double)(f *= ratio);
-        }
-        j += pairs;
-    }
+    rope_turns(d->widths, d->n_axes, p.n_pairs, d->whole_ladder != 0, d->rope_theta, p.turns);
     int sm_count = 0, *status = nullptr;
     const int rc = op_device(&sm_count, &status);
     if (rc != REGENVC_OK) return rc;

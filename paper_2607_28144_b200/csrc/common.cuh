@@ -142,10 +142,12 @@ cudaError_t launch_expire_wait(int* status, unsigned long long limit_ns, cudaStr
 // runtime's error state and maps to REGENVC_ERR_CUDA.
 void count_launch();
 // Device checks of the entry points outside api.cu (the first call on a device sets it up): REGENVC_OK, the SM count and
-// the status word; and the encoder of two-dimensional tensor maps (box of box_inner x box_outer elements).
+// the status word; and the encoders of tensor maps of two (box of box_inner x box_outer elements) and four dimensions.
 int op_device(int* sm_count, int** status);
 int encode_map(CUtensorMap* m, CUtensorMapDataType type, void* base, uint64_t inner, uint64_t outer, uint64_t row_bytes,
                uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swizzle);
+int encode_map_4d(CUtensorMap* m, CUtensorMapDataType type, void* base, const uint64_t* extent, const uint64_t* stride_bytes,
+                  const uint32_t* box, CUtensorMapSwizzle swizzle);
 int record_cuda_failure(cudaError_t e, const char* what);
 
 // Launchers (each returns the launch error, enqueues on `stream`).

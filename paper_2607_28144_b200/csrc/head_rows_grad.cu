@@ -1,0 +1,304 @@
+// Gradients of the norm and rotation of queries and keys, from the operands themselves: nothing is kept between the passes.
+//
+//     x the operand, n = x r, r = 1 / sqrt(mean(x^2) + eps), y = R (n w)
+//     g = R^T dy,   dw = sum over tokens and heads of g n,   dx = r (g w - n mean(g w n))
+//
+// Bound: HBM, x and dy are read once and dx is written once.  Both sums over a head, of x^2 and of g w x, run side by side.
+// The sums of dw have a fixed order: a thread adds up what its own vectors give, a block joins its threads, a second kernel
+// joins the blocks, each over the same vectors in every call of a shape; no atomics.
+#include "head_rows_core.cuh"
+
+namespace regenvc {
+namespace {
+
+constexpr int kBatch = 2;
+constexpr int kMaxTokens = 16;
+
+template <typename T>
+struct Vector {
+    const T *x, *dy;
+    T* dx;
+};
+template <typename T>
+__device__ __forceinline__ Vector<T> locate(const HeadRowsParams& p, int token, int h, int& w) {
+    w = h < p.heads[0] ? 0 : 1;
+    const long long n = token, hh = w ? h - p.heads[0] : h;
+    return {reinterpret_cast<const T*>(p.in[w]) + n * p.in_token[w] + hh * p.in_head[w],
+            reinterpret_cast<const T*>(p.grad[w]) + n * p.grad_token[w] + hh * p.grad_head[w],
+            reinterpret_cast<T*>(p.out[w]) + n * p.out_token[w] + hh * p.out_head[w]};
+}
+
+template <typename T, bool HALVES>
+__global__ void __launch_bounds__(kHeadThreads) head_rows_grad_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
+    extern __shared__ float4 table_raw[];
+    float2* table = reinterpret_cast<float2*>(table_raw);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the join sets itself up and waits for this grid
+    const int pitch = table_pitch(p), chunks = p.head_dim / 8;
+    const int c = threadIdx.x & (width - 1), group = threadIdx.x / width, groups = blockDim.x / width;
+    const bool active = c < chunks;
+    const int all = p.heads[0] + p.heads[1];
+    const float inv_d = 1.0f / (float)p.head_dim;
+    const bool sums = p.partial != nullptr;
+    float gq[8], gk[8], dw[2][8];
+    load_gains(p.weight[0], c, active, gq);
+    load_gains(p.weight[1], c, active, gk);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.0f;
+
+    for (long long token0 = (long long)blockIdx.x * p.tokens_per_cta; token0 < p.n_tokens; token0 += (long long)gridDim.x * p.tokens_per_cta) {
+        const int tokens = (int)min((long long)p.tokens_per_cta, p.n_tokens - token0);
+        if (p.n_axes) {
+            __syncthreads();                                // the last group's table has been read
+            fill_table<HALVES ? kHalfChunks : kAdjacentChunks>(p, table, pitch, (int)token0, tokens, true);
+            __syncthreads();
+        }
+        const int total = tokens * all;
+        int t = 0, h = group;
+        while (h >= all) h -= all, ++t;
+        for (int base = 0; base < total; base += groups * kBatch) {   // the same rounds for all lanes
+            Raw8<T> rx[kBatch], ry[kBatch];
+            T* to[kBatch];
+            int of[kBatch], at[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                of[i] = -1;
+                at[i] = 0;
+                rx[i] = ry[i] = Raw8<T>{};
+                if (t < tokens) {
+                    const Vector<T> u = locate<T>(p, (int)token0 + t, h, of[i]);
+                    at[i] = t;
+                    to[i] = u.dx;
+                    if (active) {
+                        rx[i] = load_raw8(u.x + 8 * c);
+                        ry[i] = load_raw8(u.dy + 8 * c);
+                    }
+                    h += groups;
+                    while (h >= all) h -= all, ++t;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                float x[8], g[8];
+                widen8(rx[i], x);
+                widen8(ry[i], g);
+                if (p.n_axes) turn_chunk<HALVES>(g, table + at[i] * pitch, p, active ? c : 0, chunks);
+                if (!active) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[e] = 0.0f;
+                }
+                float sq = 0.0f, hx = 0.0f, hw[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    hw[e] = g[e] * (of[i] == 1 ? gk[e] : gq[e]);
+                    sq += x[e] * x[e];
+                    hx += hw[e] * x[e];
+                }
+                sq = head_sum(sq, width);
+                hx = head_sum(hx, width);
+                const float r = rsqrtf(sq * inv_d + p.eps);
+                const float m = hx * inv_d * r * r;         // x m is n mean(g w n)
+                if (of[i] >= 0 && active) {
+                    float o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        o[e] = r * (hw[e] - x[e] * m);
+                        const float s = g[e] * x[e] * r;
+                        if (of[i]) dw[1][e] += s;
+                        else dw[0][e] += s;
+                    }
+                    store8(to[i] + 8 * c, o);
+                }
+            }
+        }
+    }
+    if (!sums) return;
+    // the block's sums: lanes of one warp that hold the same chunk by shuffles, warps in turn through shared memory
+    __shared__ float part[kHeadThreads / 32][2][kRopeMaxPairs * 2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float s = dw[w][e];
+            if (width <= 16) s += __shfl_xor_sync(0xffffffffu, s, 16);
+            if (width <= 8) s += __shfl_xor_sync(0xffffffffu, s, 8);
+            if ((threadIdx.x & 31) < width && active) part[threadIdx.x >> 5][w][8 * c + e] = s;
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.head_dim; i += blockDim.x) {
+        const int w = i >= p.head_dim, col = w ? i - p.head_dim : i;
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kHeadThreads / 32; ++j) s += part[j][w][col];
+        p.partial[(size_t)blockIdx.x * 2 * p.head_dim + i] = s;
+    }
+}
+
+// Element form: a warp holds a head, as in the forward pass.
+template <typename T>
+__global__ void __launch_bounds__(kHeadThreads) head_rows_grad_element_kernel(const __grid_constant__ HeadRowsParams p) {
+    extern __shared__ float4 table_raw[];
+    float2* table = reinterpret_cast<float2*>(table_raw);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int pitch = table_pitch(p), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int all = p.heads[0] + p.heads[1], units = p.head_dim - p.n_pairs;
+    float da[2][kUnits], db[2][kUnits];
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) da[0][k] = da[1][k] = db[0][k] = db[1][k] = 0.0f;
+    for (long long token0 = (long long)blockIdx.x * p.tokens_per_cta; token0 < p.n_tokens; token0 += (long long)gridDim.x * p.tokens_per_cta) {
+        const int tokens = (int)min((long long)p.tokens_per_cta, p.n_tokens - token0);
+        if (p.n_axes) {
+            __syncthreads();
+            fill_table<kPlain>(p, table, pitch, (int)token0, tokens, true);
+            __syncthreads();
+        }
+        for (int i = warp; i < tokens * all; i += blockDim.x >> 5) {
+            const int t = i / all;
+            int w;
+            const Vector<T> at = locate<T>(p, (int)token0 + t, i - t * all, w);
+            const float* gain = p.weight[w];
+            float xa[kUnits], xb[kUnits], ga[kUnits], gb[kUnits], sq = 0.0f, hx = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const int u = lane + 32 * k;
+                xa[k] = xb[k] = ga[k] = gb[k] = 0.0f;
+                if (u >= units) continue;
+                const int first = unit_first(u, p);
+                xa[k] = to_f32(at.x[first]);
+                ga[k] = to_f32(at.dy[first]);
+                sq += xa[k] * xa[k];
+                if (u < p.n_pairs) {
+                    const int second = unit_second(u, p);
+                    xb[k] = to_f32(at.x[second]);
+                    const float d = to_f32(at.dy[second]);
+                    const float2 cs = table[t * pitch + u];
+                    gb[k] = d * cs.x + ga[k] * cs.y;
+                    ga[k] = ga[k] * cs.x - d * cs.y;
+                    sq += xb[k] * xb[k];
+                    hx += gb[k] * (gain ? gain[second] : 1.0f) * xb[k];
+                }
+                hx += ga[k] * (gain ? gain[first] : 1.0f) * xa[k];
+            }
+            sq = head_sum(sq, 32) / (float)p.head_dim;
+            hx = head_sum(hx, 32) / (float)p.head_dim;
+            const float r = rsqrtf(sq + p.eps), m = hx * r * r;
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const int u = lane + 32 * k;
+                if (u >= units) continue;
+                const int first = unit_first(u, p);
+                from_f32(r * (ga[k] * (gain ? gain[first] : 1.0f) - xa[k] * m), at.dx[first]);
+                const float sa = ga[k] * xa[k] * r, sb = gb[k] * xb[k] * r;
+                if (w) da[1][k] += sa, db[1][k] += sb;
+                else da[0][k] += sa, db[0][k] += sb;
+                if (u < p.n_pairs) {
+                    const int second = unit_second(u, p);
+                    from_f32(r * (gb[k] * (gain ? gain[second] : 1.0f) - xb[k] * m), at.dx[second]);
+                }
+            }
+        }
+    }
+    if (!p.partial) return;
+    __shared__ float part[kHeadThreads / 32][2][kRopeMaxPairs * 2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            const int u = lane + 32 * k;
+            if (u >= units) continue;
+            part[warp][w][unit_first(u, p)] = da[w][k];
+            if (u < p.n_pairs) part[warp][w][unit_second(u, p)] = db[w][k];
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.head_dim; i += blockDim.x) {
+        const int w = i >= p.head_dim, col = w ? i - p.head_dim : i;
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kHeadThreads / 32; ++j) s += part[j][w][col];
+        p.partial[(size_t)blockIdx.x * 2 * p.head_dim + i] = s;
+    }
+}
+
+// Sums of the blocks' partial sums: eight columns per block, 32 threads to a column.
+__global__ void __launch_bounds__(256) head_rows_join_kernel(const float* partial, int blocks, int head_dim, float* dq, float* dk) {
+    __shared__ float part[32][8];
+    const int col = blockIdx.x * 8 + (threadIdx.x & 7), row = threadIdx.x >> 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    float s = 0.0f;
+    if (col < 2 * head_dim)
+#pragma unroll 4
+        for (int i = row; i < blocks; i += 32) s += partial[(size_t)i * 2 * head_dim + col];
+    part[row][threadIdx.x & 7] = s;
+    __syncthreads();
+    if (threadIdx.x < 8 && col < 2 * head_dim) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum += part[i][threadIdx.x];
+        float* to = col < head_dim ? dq : dk;
+        if (to) to[col < head_dim ? col : col - head_dim] = sum;
+    }
+}
+
+template <typename K>
+cudaError_t plan_grad(K kernel, HeadRowsParams& p, int groups, int sm_count, int* blocks, size_t* smem) {
+    const int all = p.heads[0] + p.heads[1];
+    int tokens = 8 * groups / all;
+    if (tokens > kMaxTokens) tokens = kMaxTokens;
+    const size_t per_token = (size_t)table_pitch(p) * sizeof(float2);
+    int per_sm = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, (tokens < 1 ? 1 : tokens) * per_token);
+    if (e != cudaSuccess) return e;
+    long long room = (long long)(per_sm > 0 ? per_sm : 1) * sm_count;
+    if (room > kHeadGradMaxBlocks) room = kHeadGradMaxBlocks;
+    const long long even = (p.n_tokens + room - 1) / room;
+    if (tokens > even) tokens = (int)even;
+    if (tokens < 1) tokens = 1;
+    p.tokens_per_cta = tokens;
+    const long long rounds = ((long long)p.n_tokens + tokens - 1) / tokens;
+    *blocks = (int)(rounds < room ? rounds : room);
+    *smem = tokens * per_token;
+    return cudaSuccess;
+}
+
+template <typename T>
+cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, int* blocks, cudaStream_t stream) {
+    size_t smem = 0;
+    if (!vec || p.head_dim % 8 != 0 || (p.halves && p.n_pairs % 8 != 0)) {
+        const cudaError_t e = plan_grad(head_rows_grad_element_kernel<T>, p, kHeadThreads / 32, sm_count, blocks, &smem);
+        if (e != cudaSuccess) return e;
+        head_rows_grad_element_kernel<T><<<*blocks, kHeadThreads, smem, stream>>>(p);
+        return cudaGetLastError();
+    }
+    const int width = p.head_dim <= 64 ? 8 : (p.head_dim <= 128 ? 16 : 32);
+    auto kernel = p.halves ? head_rows_grad_kernel<T, true> : head_rows_grad_kernel<T, false>;
+    const cudaError_t e = plan_grad(kernel, p, kHeadThreads / width, sm_count, blocks, &smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<*blocks, kHeadThreads, smem, stream>>>(p, width);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_head_rows_grad(HeadRowsParams p, int type, bool vec, int sm_count, int* launches, cudaStream_t stream) {
+    int blocks = 0;
+    *launches = 0;
+    cudaError_t e = type == kTypeBf16  ? launch_typed<__nv_bfloat16>(p, vec, sm_count, &blocks, stream)
+                    : type == kTypeF16 ? launch_typed<__half>(p, vec, sm_count, &blocks, stream)
+                                       : launch_typed<float>(p, vec, sm_count, &blocks, stream);
+    if (e != cudaSuccess) return e;
+    *launches = 1;
+    if (!p.partial) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((2 * p.head_dim + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, head_rows_join_kernel, (const float*)p.partial, blocks, p.head_dim, p.dweight[0], p.dweight[1]);
+    if (e == cudaSuccess) *launches = 2;
+    return e;
+}
+
+}  // namespace regenvc

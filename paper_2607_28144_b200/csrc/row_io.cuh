@@ -31,6 +31,11 @@ __device__ __forceinline__ Raw8<T> load_raw8(const T* p) {
     for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = reinterpret_cast<const uint4*>(p)[i];
     return r;
 }
+template <typename T>
+__device__ __forceinline__ void store_raw8(T* p, const Raw8<T>& r) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(p)[i] = r.w[i];
+}
 __device__ __forceinline__ void widen2(uint32_t w, float& a, float& b, const __nv_bfloat16*) {
     a = __uint_as_float(w << 16);
     b = __uint_as_float(w & 0xFFFF0000u);

@@ -1,0 +1,138 @@
+"""Queries and keys normalised per head and rotated, into rows and into a paged cache, and the gradients, against their 64-bit
+forms."""
+import pytest
+import torch
+
+from block_ops_util import U, floor_step, half_step
+from cache_ops_util import head64, head_grads64, scatter_pages, slots_of
+from paper_2607_28144_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, FP, F32 = torch.bfloat16, torch.float16, torch.float32
+
+CASES = [
+    # tokens, hq, hk, d, type, widths, halves, whole ladder, float positions, gains
+    (1, 12, 12, 128, BF, (44, 42, 42), False, False, False, True),
+    (700, 12, 12, 128, BF, (44, 42, 42), False, False, False, True),
+    (333, 8, 2, 128, FP, (32, 48, 48), True, True, True, True),
+    (65, 5, 1, 64, F32, (24, 20, 20), True, False, False, True),
+    (50, 3, 3, 256, BF, (256,), False, True, False, False),
+    (40, 2, 4, 96, FP, (32, 32), True, False, True, True),
+    (77, 7, 1, 80, BF, (20, 12), False, True, False, True),
+    (31, 3, 0, 66, BF, (22, 22, 22), False, False, False, True),
+    (29, 2, 2, 6, F32, (4,), True, False, False, True),
+    (20, 2, 1, 250, FP, (100, 50), True, True, False, True),
+    (90, 4, 4, 128, F32, (), False, False, False, True),
+    (5000, 1, 1, 8, BF, (8,), True, True, False, True),
+]
+
+
+def operands(case, seed=0):
+    n, hq, hk, d, dtype, widths, halves, whole, as_float, gains = case
+    g = torch.Generator().manual_seed(seed)
+    wide = 1 + 4 * torch.rand(d, generator=g) ** 4
+    q, k = ((torch.randn(n, h, d, generator=g) * wide).to(dtype).to(DEV) if h else None for h in (hq, hk))
+    pos = torch.randint(0, 5000, (len(widths), n), generator=g, dtype=torch.int32) if widths else None
+    if pos is not None and as_float:
+        pos = pos.float() * 0.125
+    w = [(1 + 0.3 * torch.randn(d, generator=g)).to(DEV) if gains and h else None for h in (hq, hk)]
+    how = dict(q_weight=w[0], k_weight=w[1], halves=halves, whole_ladder=whole)
+    return q, k, None if pos is None else pos.to(DEV), list(widths) or None, how
+
+
+def reference(x, w, pos, widths, how, eps=1e-6):
+    return head64(x.double(), None if w is None else w.double(), pos, widths, 10000.0, how["halves"], how["whole_ladder"], eps)
+
+
+def forward_bound(ref, mag, dtype, d):
+    # sum of squares (d terms), rsqrt (2 steps), two products, cosine and sine of an angle rounded to a fraction of a turn
+    # (its 32-bit fraction is off by up to pi 2^-24 of a turn's radians, cos and sin by two steps more), two products, a sum
+    return half_step(dtype) * ref.abs() + (d / 2 + 24) * U * mag + floor_step(dtype)
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_forward(case):
+    q, k, pos, widths, how = operands(case)
+    qo, ko = B.regenvc_qk_norm_rope_forward(q, k, pos, widths, **how)
+    for x, y, w in ((q, qo, how["q_weight"]), (k, ko, how["k_weight"])):
+        if x is None:
+            assert y is None
+            continue
+        ref, mag = reference(x, w, pos, widths, how)
+        assert ((y.double() - ref).abs() <= forward_bound(ref, mag, x.dtype, x.shape[2])).all()
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_gradients_of_the_formula(case):
+    q, k, pos, widths, how = operands(case)
+    g = torch.Generator().manual_seed(9)
+    dqo, dko = (None if x is None else torch.randn(x.shape, generator=g).to(x.dtype).to(DEV) for x in (q, k))
+    got = B.regenvc_qk_norm_rope_backward(dqo, dko, q, k, pos, widths, **how)
+    again = B.regenvc_qk_norm_rope_backward(dqo, dko, q, k, pos, widths, **how)
+    for x, dy, name in ((q, dqo, "q"), (k, dko, "k")):
+        if x is None:
+            assert got["d" + name] is None
+            continue
+        w, d = how[name + "_weight"], x.shape[2]
+        dx, mag, dw, dwm = head_grads64(x.double(), None if w is None else w.double(), dy.double(), pos, widths, 10000.0,
+                                        how["halves"], how["whole_ladder"], 1e-6)
+        err = (got["d" + name].double() - dx).abs()
+        assert (err <= half_step(x.dtype) * dx.abs() + (2 * d + 48) * U * mag + floor_step(x.dtype)).all()
+        assert torch.equal(got["d" + name], again["d" + name])
+        if w is not None:
+            # a thread adds up at most all tokens and heads; blocks and threads are joined in some dozen steps
+            terms = x.shape[0] * x.shape[1]
+            err = (got[f"d{name}_weight"].double() - dw).abs()
+            assert (err <= (d + 64 + min(terms, 4096)) * U * dwm).all()
+            assert torch.equal(got[f"d{name}_weight"], again[f"d{name}_weight"])
+
+
+APPEND = [
+    # new tokens, cached tokens with them, hq, hk, d, page, type, widths, halves, norm, order
+    ([1], [1], 2, 2, 128, 16, BF, (44, 42, 42), False, True, "tokens"),
+    ([1, 1, 0, 1], [17, 500, 33, 48], 8, 2, 128, 16, FP, (128,), True, True, "heads"),
+    ([130, 7], [1000, 7], 12, 12, 128, 1560, BF, (44, 42, 42), False, True, "tokens"),
+    ([64, 3, 20], [64, 900, 21], 0, 3, 64, 24, F32, (20, 20), True, True, "tokens"),
+    ([9, 5], [9, 40], 3, 1, 66, 5, BF, (22, 22, 22), False, True, "heads"),
+    ([40], [50], 2, 2, 80, 1, FP, (), False, False, "tokens"),
+]
+
+
+@pytest.mark.parametrize("new,keys,hq,hk,d,page,dtype,widths,halves,norm,order", APPEND)
+def test_append(new, keys, hq, hk, d, page, dtype, widths, halves, norm, order):
+    g = torch.Generator().manual_seed(page)
+    table, pages = scatter_pages(keys, page, order, g)
+    n = sum(new)
+    rows = torch.randn(n + 4, hq + 2 * hk, d, generator=g).to(dtype).to(DEV)      # four rows behind the last sequence
+    q, k, v = rows[:, :hq] if hq else None, rows[:, hq:hq + hk], rows[:, hq + hk:]
+    shape = (pages, page, hk, d) if order == "tokens" else (pages, hk, page, d)
+    kc, vc = (torch.randn(shape, generator=g).to(dtype).to(DEV) for _ in range(2))
+    if order == "heads":
+        kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
+    k_want, v_want = kc.double(), vc.double()
+    k_bound = torch.zeros_like(k_want)
+    pos = torch.randint(0, 9000, (len(widths), n + 4), generator=g, dtype=torch.int32).to(DEV) if widths else None
+    w = [(1 + 0.3 * torch.randn(d, generator=g)).to(DEV) if norm else None for _ in range(2)]
+    starts = [sum(new[:i]) for i in range(len(new) + 1)]
+    q_out = torch.full((n + 4, hq, d), 7.0, dtype=dtype, device=DEV) if hq else None
+    how = dict(halves=halves, whole_ladder=False)
+    B.regenvc_paged_append(k, v, kc, vc, table.to(DEV), torch.tensor(keys, dtype=torch.int32, device=DEV),
+                           torch.tensor(starts, dtype=torch.int32, device=DEV), q=q, positions=pos, widths=list(widths) or None,
+                           norm=B.NORM_RMS if norm else B.NORM_NONE, q_weight=w[0] if hq else None, k_weight=w[1], q_out=q_out, **how)
+    assert B.regenvc_device_status() == B.OK
+    kr, km = head64(k.double(), None if w[1] is None else w[1].double(), pos, widths, 10000.0, halves, False, 1e-6, norm)
+    for s, (m, total) in enumerate(zip(new, keys)):
+        if not m:
+            continue
+        page_at, slot_at = slots_of(table, s, total, page)
+        at = page_at[total - m:].to(DEV), slot_at[total - m:].to(DEV)
+        part = slice(starts[s], starts[s] + m)
+        k_want[at], v_want[at] = kr[part], v[part].double()
+        k_bound[at] = forward_bound(kr[part], km[part], dtype, d)
+    assert torch.equal(vc.double(), v_want)
+    assert ((kc.double() - k_want).abs() <= k_bound).all()                        # other slots: as they were
+    if hq:
+        qr, qm = head64(q.double(), None if w[0] is None else w[0].double(), pos, widths, 10000.0, halves, False, 1e-6, norm)
+        assert ((q_out.double() - qr).abs()[:n] <= forward_bound(qr, qm, dtype, d)[:n]).all()
+        assert (q_out[n:] == 7.0).all()
