@@ -418,10 +418,10 @@ int regenvc_paged_attn_forward(const regenvc_paged_attn_desc* d, const void* q, 
     p.box_rows = 128;
     while (d->page_size % p.box_rows != 0) p.box_rows /= 2;
     p.one_page_box = p.box_rows < 128 && d->page_size >= 128;
-    // Whole items in rounds where several tiles of rows can share a head's keys; calls of few rows per sequence have
-    // nothing to share.
+    // Whole items in rounds where several tiles of rows share a head's keys and there can be more items than thread blocks;
+    // calls of few rows per sequence have nothing to share.
     const long long rows = (long long)d->n_tokens * p.share;
-    p.rounds = rows >= 2 * kPagedRows && rows >= 64ll * d->n_sequences;
+    p.rounds = rows >= 64ll * d->n_sequences && (rows / kPagedRows + d->n_sequences) * d->n_k_heads >= kPagedRoundsFrom;
     char* w = reinterpret_cast<char*>(workspace);
     p.part_o = reinterpret_cast<float4*>(w);
     w += (size_t)kPagedMaxGrid * 2 * kPagedRows * d->head_dim * sizeof(float);

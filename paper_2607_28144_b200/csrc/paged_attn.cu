@@ -9,6 +9,7 @@
 //                   sum in registers, probabilities back to tensor memory
 //   warp  8         issues the products (one thread) and owns the tensor memory
 //   warp  9         copies: looks the pages up (a lane per box) and fetches K and V tiles into a ring by TMA
+//   warp  10        walks over this thread block's work and hands it to the others, stretch by stretch
 // More than 128 rows: each stream has 128 rows of its own and both take every tile of keys.  At most 128 rows (single
 // tokens): both streams have the same rows and take every other tile of keys, and their results are joined in tensor memory
 // at the end.  Either way one stream's products run under the other's exponentials.
@@ -17,8 +18,10 @@
 // K comes as [keys][64 columns] blocks with the 128-byte swizzle, which is a K-major operand of Q K^T, V in the same form,
 // which is an MN-major operand of P V: neither is rewritten.
 //
-// Softmax: a row's reference is its maximum at the time it was last set, and is set again only when a later tile's maximum
-// lies more than 8 log2 units above it (probabilities up to 2^8, in range of either type); then the row's O is rescaled.
+// Softmax: a row's reference is its maximum over the first tile in which it sees a key.  No later maximum is taken: a
+// tile's probabilities are formed against the reference, and only if their sum leaves the range of the probabilities' type
+// (65504) or 2^32 (bf16, whose range is fp32's) the reference is raised, O rescaled and the tile done again.  A larger
+// probability costs no precision, it has as many bits as one below 1.
 // Scores, sums, O are fp32; probabilities are rounded to the cache's type, which the product P V takes both operands in
 // (half a step of 2^-9 or 2^-12 each, independent from key to key).  Keys that no row of the item sees (behind the length,
 // before the window) are zeroed in V's tile, so that what lies there does not reach a sum as 0 * NaN.
@@ -34,31 +37,46 @@
 namespace regenvc {
 namespace {
 
-constexpr int kPgThreads = 384, kPgSoftmax = 256;
+constexpr int kPgSoftmax = 256, kPgThreads = kPgSoftmax + 128;
 constexpr int kPgLaunchRegs = 168, kPgControlRegs = 64;
 constexpr int kPgSoftmaxRegs = ((kPgLaunchRegs * kPgThreads - kPgControlRegs * 128) / kPgSoftmax) / 8 * 8;
 static_assert(kPgSoftmaxRegs * kPgSoftmax + kPgControlRegs * 128 <= kPgLaunchRegs * kPgThreads, "register budget");
-constexpr int kPgMmaWarp = 8, kPgTmaWarp = 9;
+constexpr int kPgMmaWarp = 8, kPgKeyWarp = 9, kPgWalkWarp = 10, kPgValueWarp = 11;
+constexpr int kSegments = 4;      // stretches of work handed to the warps ahead
 constexpr int kMaxRounds = 64;
-constexpr float kRaise = 8.0f;
+// Sums of 128 probabilities from which on a row's reference is set anew: far inside what the probabilities' type holds.
+template <bool F16>
+__device__ constexpr float raise_at() { return F16 ? 65504.0f : 4294967296.0f; }
 
 template <int D>
 struct Shape {
     static constexpr int kTileB = 128 * D * 2;               // one tile of Q, K or V
-    static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int kRing = kStages * kTileB;
+    static constexpr int kKeySlots = D == 128 ? 3 : 5, kValueSlots = D == 128 ? 2 : 5;   // rings of K and of V tiles
+    static constexpr int kRing = (kKeySlots + kValueSlots) * kTileB;
     static constexpr int kBlocks = D / 64;                    // 64-column blocks of a tile, 16 KB each
 };
 
-struct Control {
-    uint64_t kv_full[10], kv_empty[10], q_full, s_full[2], p_full[2], o_full[2];
-    uint32_t tmem_base;
-    int abort_flag;
-    // this thread block's part of the work
-    int rounds, seq, head, tile, off;
-    long long left;
-    int item_seq[kMaxRounds], item_head[kMaxRounds], item_tile[kMaxRounds];
-    long long warp_units[12], warp_items[12];
+// The bounded wait of ptx.cuh with its clock out of line: the kernel waits in some twenty places, and its loops have to stay
+// in the instruction cache (at 175 KB of code, everything inlined, the window's attention took 5.9 ms).
+__device__ __noinline__ uint64_t wait_clock(volatile int* abort_flag, int* status, uint64_t since) {
+    if (*abort_flag) return 0;
+    const uint64_t now = global_timer_ns();
+    if (since == 1) return now;
+    if (now - since <= kWaitLimitNs) return since;
+    *abort_flag = 1;
+    atomicCAS(status, 0, kStatusTimeout);
+    return 0;
+}
+struct Waiter {
+    volatile int* abort_flag;
+    int* status;
+    __device__ __forceinline__ bool operator()(const uint64_t* bar, uint32_t parity) const {
+        const uint32_t addr = smem_u32(bar);
+        uint64_t since = 1;                                  // 1: the clock has not been read yet
+        for (uint32_t spins = 1; !mbar_try_wait(addr, parity & 1); ++spins)
+            if ((spins & 255u) == 0 && (since = wait_clock(abort_flag, status, since)) == 0) return false;
+        return true;
+    }
 };
 
 // ------------------------------------------------------------------------------------------------------ the work
@@ -66,7 +84,7 @@ struct Seq {
     int row0, tokens, keys;
 };
 // Lengths and row starts as far as the buffers go: whatever they hold, no access leaves them.
-__device__ __forceinline__ Seq load_seq(const PagedAttnParams& p, int s) {
+__device__ __noinline__ Seq load_seq(const PagedAttnParams& p, int s) {
     Seq q;
     q.row0 = min(max(p.row_starts[s], 0), p.n_tokens);
     q.tokens = min(max(p.row_starts[s + 1], q.row0), p.n_tokens) - q.row0;
@@ -87,7 +105,7 @@ struct Item {
     int rows, lo, hi, first_tile, n_tiles;
 };
 __device__ __forceinline__ int item_tiles(const PagedAttnParams& p, const Seq& q) { return (q.tokens * p.share + kPagedRows - 1) / kPagedRows; }
-__device__ __forceinline__ Item load_item(const PagedAttnParams& p, const Seq& q, int tile) {
+__device__ __noinline__ Item load_item(const PagedAttnParams& p, const Seq& q, int tile) {
     Item it;
     const int r0 = tile * kPagedRows;
     it.rows = min(kPagedRows, q.tokens * p.share - r0);
@@ -104,242 +122,327 @@ __device__ __forceinline__ Item load_item(const PagedAttnParams& p, const Seq& q
 struct Segment {
     Seq q;
     int seq, tile, head, rows, lo, hi, kt0, n;   // key tiles kt0 .. kt0 + n - 1
-    bool starts, ends;
+    int starts, ends;                       // n = 0: no more work
 };
-struct Walk {
-    int round, rounds, seq, head, tile, off;
-    long long left;
-    Seq q;
-    int loaded;   // sequence that q holds
-    __device__ __forceinline__ Walk(const Control& c) : round(0), rounds(c.rounds), seq(c.seq), head(c.head), tile(c.tile), off(c.off),
-                                                        left(c.left), loaded(-1) {}
-    __device__ __forceinline__ bool next(const PagedAttnParams& p, const Control& c, Segment& g) {
-        int s, take;
-        if (round < rounds) {
-            s = c.item_seq[round];
-            g.head = c.item_head[round];
-            g.tile = c.item_tile[round];
-            ++round;
-            if (s != loaded) q = load_seq(p, loaded = s);
-            const Item it = load_item(p, q, g.tile);
-            g.q = q, g.seq = s;
-            g.rows = it.rows, g.lo = it.lo, g.hi = it.hi, g.kt0 = it.first_tile, g.n = it.n_tiles;
-            g.starts = g.ends = true;
-            return true;
-        }
-        if (left <= 0) return false;
-        if (seq != loaded) q = load_seq(p, loaded = seq);
-        const Item it = load_item(p, q, tile);
-        take = (int)min((long long)(it.n_tiles - off), left);
-        if (take < 1) return false;                          // (cannot be: the part was cut from the same lengths)
-        g.q = q, g.seq = seq;
-        g.head = head, g.tile = tile, g.rows = it.rows, g.lo = it.lo, g.hi = it.hi;
-        g.kt0 = it.first_tile + off, g.n = take;
-        g.starts = off == 0;
-        g.ends = off + take == it.n_tiles;
-        left -= take;
-        off += take;
-        if (g.ends) {
-            off = 0;
-            if (++tile >= item_tiles(p, q)) {
-                tile = 0;
-                if (++head >= p.n_k_heads) {
-                    head = 0;
-                    if (left > 0) {
-                        do {
-                            if (++seq >= p.n_sequences) {
-                                left = 0;
-                                break;
-                            }
-                            q = load_seq(p, loaded = seq);
-                        } while (q.tokens == 0);
-                    }
-                }
-            }
-        }
-        return true;
-    }
+struct Control {
+    uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, s_full[2], p_full[2], o_full[2], stagger;
+    uint64_t seg_full[kSegments], seg_empty[kSegments], together;
+    uint32_t tmem_base;
+    int abort_flag;
+    Segment seg[kSegments];
+    // this thread block's part of the work: whole items of the rounds, then a stretch of the line
+    int rounds;
+    long long start, left;
+    int item_seq[kMaxRounds], item_head[kMaxRounds], item_tile[kMaxRounds];
+    // the plan's sums
+    long long warp_cost[kPgThreads / 32], taken, before;
+    int warp_items[kPgThreads / 32], most;
 };
-
-// Number of ring entries before V(j) and K(j) of a segment: the copies come as K(0) .. K(ahead - 1), then V(j), K(j + ahead)
-// in turn, in the order in which the products want them.
-__device__ __forceinline__ int ring_of_v(int j, int n, int ahead) { return ahead + j + min(j, n - ahead); }
-__device__ __forceinline__ int ring_of_k(int j, int ahead) { return j < ahead ? j : 2 * j - ahead + 1; }
 
 __device__ __forceinline__ void plan_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kPgThreads) : "memory"); }
 
-// Exclusive prefix over the thread block of two sums.
-__device__ __forceinline__ void block_scan(Control& c, long long& units, long long& items, long long& all_units, long long& all_items) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long u0 = units, i0 = items;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, units, o), i = __shfl_up_sync(0xffffffffu, items, o);
-        if (lane >= o) units += u, items += i;
+// The line of work: sequences, in them heads of the cache, in them tiles of rows, in them tiles of keys.  A tile of keys
+// counts two for an item of two tiles of rows, one for an item of one, which is about what they take.
+__device__ __forceinline__ int weight(const Item& it) { return it.rows > 128 ? 2 : 1; }
+// Where part i of n begins on a line of `all`.
+__device__ __forceinline__ long long bound(long long all, int n, int i) {
+    return i >= n ? all : (long long)((double)all * (double)__fdividef((float)i, (float)n));
+}
+// Parts: one per item or per four units, whichever are more, as far as there are thread blocks.
+__device__ __forceinline__ int parts_of(long long all, int items) {
+    const long long most = max((long long)items, (all + 3) / 4);
+    return (int)min((long long)gridDim.x, max(most, 1ll));
+}
+
+struct Walk {
+    int round, seq, head, tile;
+    long long at, left;                     // on the line: place within the item, what is still to be done
+    Seq q;
+    int loaded;                             // sequence that q holds
+    __device__ __forceinline__ bool next(const PagedAttnParams& p, const Control& c, Segment& g) {
+#pragma unroll 1
+        while (true) {
+            const bool whole = round < c.rounds;
+            if (!whole && left <= 0) return false;
+            const int s = whole ? c.item_seq[round] : seq;
+            if (s != loaded) q = load_seq(p, loaded = s);
+            g.q = q, g.seq = s;
+            g.head = whole ? c.item_head[round] : head;
+            g.tile = whole ? c.item_tile[round] : tile;
+            const Item it = load_item(p, q, g.tile);
+            g.rows = it.rows, g.lo = it.lo, g.hi = it.hi;
+            if (whole) {
+                ++round;
+                g.kt0 = it.first_tile, g.n = it.n_tiles;
+                g.starts = g.ends = 1;
+                return true;
+            }
+            const int w = weight(it), cost = it.n_tiles * w;
+            const int from = (int)at, to = (int)min((long long)cost, at + left);
+            const int a = (from + w - 1) / w, b = (to + w - 1) / w;
+            left -= to - from;
+            at = to;
+            if (to == cost) {
+                at = 0;
+                if (++tile >= item_tiles(p, q)) {
+                    tile = 0;
+                    if (++head >= p.n_k_heads) {
+                        head = 0;
+#pragma unroll 1
+                        while (left > 0 && ++seq < p.n_sequences) {
+                            q = load_seq(p, loaded = seq);
+                            if (q.tokens > 0) break;
+                        }
+                        if (seq >= p.n_sequences) left = 0;
+                    }
+                }
+            }
+            g.kt0 = it.first_tile + a, g.n = b - a;
+            g.starts = a == 0, g.ends = b == it.n_tiles;
+            if (b > a) return true;
+        }
     }
-    plan_barrier();
-    if (lane == 31) c.warp_units[warp] = units, c.warp_items[warp] = items;
-    plan_barrier();
-    units -= u0, items -= i0;
-    all_units = all_items = 0;
-#pragma unroll
-    for (int w = 0; w < kPgThreads / 32; ++w) {
-        if (w < warp) units += c.warp_units[w], items += c.warp_items[w];
-        all_units += c.warp_units[w], all_items += c.warp_items[w];
+};
+
+// Cost of a sequence's items of one head, a sequence per lane; `most`: the largest item's.  Lanes with many items are helped
+// by the whole warp.
+__device__ __noinline__ long long cost_of(const PagedAttnParams& p, const Seq& q, int tiles, int& most) {
+    const int lane = threadIdx.x & 31;
+    long long cost = 0;
+    most = 0;
+    const bool alike = p.group == 0 && tiles > 2;            // all items but the last are alike
+    const int mine = alike ? 2 : (tiles <= 8 ? tiles : 0);
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        const Item it = load_item(p, q, alike && i == 1 ? tiles - 1 : i);
+        const int c = it.n_tiles * weight(it);
+        cost += alike && i == 0 ? (long long)c * (tiles - 1) : c;
+        most = max(most, c);
+    }
+    uint32_t many = __ballot_sync(0xffffffffu, tiles > 0 && mine == 0);
+#pragma unroll 1
+    while (many) {
+        const int l = __ffs(many) - 1;
+        many &= many - 1;
+        Seq o;
+        o.row0 = __shfl_sync(0xffffffffu, q.row0, l);
+        o.tokens = __shfl_sync(0xffffffffu, q.tokens, l);
+        o.keys = __shfl_sync(0xffffffffu, q.keys, l);
+        const int n = __shfl_sync(0xffffffffu, tiles, l);
+        long long sum = 0;
+        int top = 0;
+#pragma unroll 1
+        for (int i = lane; i < n; i += 32) {
+            const Item it = load_item(p, o, i);
+            const int c = it.n_tiles * weight(it);
+            sum += c;
+            top = max(top, c);
+        }
+#pragma unroll 1
+        for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == l) cost = sum, most = top;
+    }
+    return cost;
+}
+
+__device__ __forceinline__ void check_seq(const PagedAttnParams& p, int s) {
+    const bool good = p.row_starts[s] >= 0 && p.row_starts[s + 1] >= p.row_starts[s] && p.row_starts[s + 1] <= p.n_tokens &&
+                      p.lengths[s] >= 0 && p.lengths[s] <= (long long)p.pages_per_sequence * p.page_size;
+    if (!good) atomicCAS(p.status, 0, kStatusRange);
+}
+
+// Sum over the lanes before this one; `all`: over the warp.
+__device__ __forceinline__ long long lanes_before(long long v, long long& all) {
+    const int lane = threadIdx.x & 31;
+    long long sum = v;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += u;
+    }
+    all = __shfl_sync(0xffffffffu, sum, 31);
+    return sum - v;
+}
+
+// Where `rest` units into a sequence lie: head, tile of rows, place in the item.  One warp.
+__device__ __forceinline__ void place(const PagedAttnParams& p, Walk& w, long long rest) {
+    const int lane = threadIdx.x & 31, tiles = item_tiles(p, w.q);
+    w.head = w.tile = 0;
+    w.at = rest;
+    if (tiles == 1 && p.n_k_heads == 1) return;
+    long long each = 0;                                      // of one head
+    bool found = false;
+#pragma unroll 1
+    for (int pass = 0; pass < 2 && !found; ++pass) {
+        if (pass == 1) {
+            w.head = (int)((float)rest / (float)each);       // a quotient below 2^16: off by one at most
+            if ((long long)w.head * each > rest) --w.head;
+            else if ((long long)(w.head + 1) * each <= rest) ++w.head;
+            rest -= w.head * each;
+        }
+#pragma unroll 1
+        for (int t0 = 0; t0 < tiles; t0 += 32) {
+            long long c = 0;
+            if (t0 + lane < tiles) {
+                const Item it = load_item(p, w.q, t0 + lane);
+                c = it.n_tiles * weight(it);
+            }
+            long long all;
+            const long long before = lanes_before(c, all);
+            if (pass == 0) {
+                each += all;
+                continue;
+            }
+            const uint32_t here = __ballot_sync(0xffffffffu, before <= rest && rest < before + c);
+            if (here) {
+                const int l = __ffs(here) - 1;
+                w.tile = t0 + l;
+                w.at = rest - __shfl_sync(0xffffffffu, before, l);
+                found = true;
+                break;
+            }
+            rest -= all;
+        }
     }
 }
 
-// This thread block's part of the work.  scratch: at least 16 bytes per sequence + 2 KB of shared memory.
-__device__ void plan_work(const PagedAttnParams& p, Control& c, uint8_t* scratch) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_seq = p.n_sequences;
-    long long* unit0 = reinterpret_cast<long long*>(scratch);        // [n_seq + 1] units of a sequence, then before it
-    int* item0 = reinterpret_cast<int*>(scratch + (size_t)(n_seq + 1) * 8);   // [n_seq + 1] tiles of rows, then items before it
-    for (int s = tid; s < n_seq; s += kPgThreads) {
-        const Seq q = load_seq(p, s);
-        const int tiles = item_tiles(p, q);
-        long long units = 0;
-        if (p.group == 0) units = tiles ? (long long)tiles * load_item(p, q, 0).n_tiles : 0;
-        else if (tiles <= 8)
-            for (int t = 0; t < tiles; ++t) units += load_item(p, q, t).n_tiles;
-        else units = -1;                                     // the warps below
-        unit0[s] = units;
-        item0[s] = tiles;
-        if (blockIdx.x == 0) {
-            const bool good = p.row_starts[s] >= 0 && p.row_starts[s + 1] >= p.row_starts[s] && p.row_starts[s + 1] <= p.n_tokens &&
-                              p.lengths[s] >= 0 && p.lengths[s] <= (long long)p.pages_per_sequence * p.page_size;
-            if (!good) atomicCAS(p.status, 0, kStatusRange);
+// At most 32 sequences and no rounds: the walking warp finds this thread block's part alone, a lane per sequence (a call of
+// a few tokens would wait longer for barriers than for its keys).
+__device__ __noinline__ void plan_few(const PagedAttnParams& p, Control& c, Walk& w) {
+    const int lane = threadIdx.x & 31;
+    Seq q{0, 0, 0};
+    int tiles = 0, most;
+    if (lane < p.n_sequences) {
+        q = load_seq(p, lane);
+        tiles = item_tiles(p, q);
+        if (blockIdx.x == 0) check_seq(p, lane);
+    }
+    const long long mine = cost_of(p, q, tiles, most) * p.n_k_heads;
+    long long all;
+    const long long before = lanes_before(mine, all);
+    const int items = __reduce_add_sync(0xffffffffu, tiles) * p.n_k_heads;
+    const int parts = parts_of(all, items), me = blockIdx.x;
+    const long long start = bound(all, parts, me);
+    w.left = me < parts ? bound(all, parts, me + 1) - start : 0;
+    const uint32_t at = __ballot_sync(0xffffffffu, mine > 0 && before <= start);
+    w.seq = at ? 31 - __clz(at) : 0;                         // the last sequence with work that starts at or before it
+    w.loaded = w.seq;
+    w.q.row0 = __shfl_sync(0xffffffffu, q.row0, w.seq);
+    w.q.tokens = __shfl_sync(0xffffffffu, q.tokens, w.seq);
+    w.q.keys = __shfl_sync(0xffffffffu, q.keys, w.seq);
+    if (lane == 0) c.rounds = 0;
+    const long long rest = start - __shfl_sync(0xffffffffu, before, w.seq);
+    __syncwarp();
+    if (w.left > 0) place(p, w, rest);
+}
+
+// Any number: all threads, a thread per sequence.  line: units before each sequence, first_item: items before each.
+__device__ __noinline__ void plan_many(const PagedAttnParams& p, Control& c, long long* line, int* first_item) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_seq = p.n_sequences, grid = gridDim.x, me = blockIdx.x;
+    long long all = 0;
+    int items = 0, most = 0;
+    if (tid == 0) c.most = 0, c.taken = c.before = 0;
+#pragma unroll 1
+    for (int s0 = 0; s0 < n_seq; s0 += kPgThreads) {
+        const int s = s0 + tid;
+        Seq q{0, 0, 0};
+        int tiles = 0, top;
+        if (s < n_seq) {
+            q = load_seq(p, s);
+            tiles = item_tiles(p, q);
+            if (me == 0) check_seq(p, s);
         }
+        const long long cost = cost_of(p, q, tiles, top) * p.n_k_heads;
+        most = max(most, top);
+        long long warp_cost, warp_items;
+        long long before = lanes_before(cost, warp_cost);
+        int items_before = (int)lanes_before((long long)tiles * p.n_k_heads, warp_items);
+        if (lane == 0) c.warp_cost[warp] = warp_cost, c.warp_items[warp] = (int)warp_items;
+        plan_barrier();
+        before += all, items_before += items;
+#pragma unroll 1
+        for (int w = 0; w < kPgThreads / 32; ++w) {
+            if (w < warp) before += c.warp_cost[w], items_before += c.warp_items[w];
+            all += c.warp_cost[w], items += c.warp_items[w];
+        }
+        if (s < n_seq) line[s] = before, first_item[s] = items_before;
+        plan_barrier();
     }
-    plan_barrier();
-    for (int s = warp; s < n_seq; s += kPgThreads / 32) {
-        if (unit0[s] >= 0) continue;
-        const Seq q = load_seq(p, s);
-        long long units = 0;
-        for (int t = lane; t < item0[s]; t += 32) units += load_item(p, q, t).n_tiles;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) units += __shfl_xor_sync(0xffffffffu, units, o);
-        __syncwarp();
-        if (lane == 0) unit0[s] = units;
-    }
-    plan_barrier();
-    // prefixes over the sequences, a stretch of them per thread
-    const int per = (n_seq + kPgThreads - 1) / kPgThreads, s0 = min(n_seq, tid * per), s1 = min(n_seq, s0 + per);
-    long long units = 0, items = 0, all_units, all_items;
-    for (int s = s0; s < s1; ++s) units += unit0[s] * p.n_k_heads, items += (long long)item0[s] * p.n_k_heads;
-    block_scan(c, units, items, all_units, all_items);
-    for (int s = s0; s < s1; ++s) {
-        const long long u = unit0[s] * p.n_k_heads;
-        const int i = item0[s] * p.n_k_heads;
-        unit0[s] = units;
-        item0[s] = (int)items;
-        units += u, items += i;
-    }
-    if (tid == 0) unit0[n_seq] = all_units, item0[n_seq] = (int)all_items;
-    plan_barrier();
-    // parts: one per item or per four units, whichever are more
-    const int grid = gridDim.x;
-    const long long wanted = max(all_items, (all_units + 3) / 4);
-    const int parts = (int)min((long long)grid, max(wanted, 1ll));
+    const int parts = parts_of(all, items);
     int rounds = 0;
-    long long start, count;
-    const int me = blockIdx.x;
-    if (p.rounds && parts == grid) {
-        const long long fair = all_units / grid;
+    long long start = bound(all, parts, me), count = me < parts ? bound(all, parts, me + 1) - start : 0;
+    if (p.rounds && items >= grid) {
+        // whole items in rounds, as many as no part can be too small for
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) atomicMax(&c.most, most);
+        plan_barrier();
+        const long long fair = bound(all, grid, 1) - 2 - (all >> 20);
+        rounds = (int)min((long long)min(kMaxRounds, items / grid), (long long)((float)fair / (float)c.most * 0.9999f));
+        rounds = max(rounds, 0);
         long long mine = 0;
-        while (rounds < kMaxRounds && (long long)(rounds + 1) * grid <= all_items) {
-            int tiles = 0, s = 0, head = 0, tile = 0;
-            if (tid < grid) {
-                const int item = rounds * grid + tid;
+        if (tid < grid) {
+#pragma unroll 1
+            for (int r = 0; r < rounds; ++r) {
+                const int item = r * grid + tid;
                 int lo = 0, hi = n_seq;                      // the last sequence whose items start at or before it
+#pragma unroll 1
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) >> 1;
-                    if (item0[mid] <= item) lo = mid;
+                    if (first_item[mid] <= item) lo = mid;
                     else hi = mid;
                 }
-                s = lo;
-                const Seq q = load_seq(p, s);
-                const int each = item_tiles(p, q);
-                head = (item - item0[s]) / each;
-                tile = item - item0[s] - head * each;
-                tiles = load_item(p, q, tile).n_tiles;
+                const Seq q = load_seq(p, lo);
+                const int each = item_tiles(p, q), head = (item - first_item[lo]) / each, tile = item - first_item[lo] - head * each;
+                const Item it = load_item(p, q, tile);
+                mine += it.n_tiles * weight(it);
+                if (tid == me) c.item_seq[r] = lo, c.item_head[r] = head, c.item_tile[r] = tile;
             }
-            int over;
-            asm volatile(
-                "{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbar.red.or.pred b, 1, %2, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
-                : "=r"(over)
-                : "r"((uint32_t)(tid < grid && mine + tiles > fair)), "n"(kPgThreads)
-                : "memory");
-            if (over) break;
-            mine += tiles;
-            if (tid == me) c.item_seq[rounds] = s, c.item_head[rounds] = head, c.item_tile[rounds] = tile;
-            ++rounds;
-        }
-        // the rest is cut so that every thread block has the same in all
-        long long share = tid < grid ? (tid + 1) * all_units / grid - tid * all_units / grid - mine : 0;
-        const long long own = share;
-        long long done = mine, all_share, all_done;
-        block_scan(c, share, done, all_share, all_done);
-        if (tid == me) {
-            c.left = own;
-            unit0[n_seq] = all_done + share;                 // where the part starts on the line
+            // the rest of the line is cut so that every thread block has the same in all
+            const long long share = bound(all, grid, tid + 1) - bound(all, grid, tid) - mine;
+            atomicAdd(reinterpret_cast<unsigned long long*>(&c.taken), (unsigned long long)mine);
+            if (tid < me) atomicAdd(reinterpret_cast<unsigned long long*>(&c.before), (unsigned long long)share);
+            if (tid == me) c.left = share;
         }
         plan_barrier();
-        start = unit0[n_seq];
+        start = c.taken + c.before;
         count = c.left;
-    } else {
-        start = me < parts ? me * all_units / parts : 0;
-        count = me < parts ? (me + 1) * all_units / parts - start : 0;
     }
-    if (warp == 0) {
-        int lo = 0, hi = n_seq;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (unit0[mid] <= start) lo = mid;
-            else hi = mid;
-        }
-        int head = 0, tile = 0, off = 0;
-        if (count > 0) {
-            const Seq q = load_seq(p, lo);
-            const int tiles = item_tiles(p, q);
-            long long rest = start - unit0[lo];
-            long long each = 0;                              // units of one head
-            for (int t0 = 0; t0 < tiles; t0 += 32) each += __reduce_add_sync(0xffffffffu, t0 + lane < tiles ? load_item(p, q, t0 + lane).n_tiles : 0);
-            head = (int)(rest / each);
-            rest -= head * each;
-            for (int t0 = 0; t0 < tiles; t0 += 32) {
-                const int n = t0 + lane < tiles ? load_item(p, q, t0 + lane).n_tiles : 0;
-                int before = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int u = __shfl_up_sync(0xffffffffu, before, o);
-                    if (lane >= o) before += u;
-                }
-                const int all = __shfl_sync(0xffffffffu, before, 31);
-                if (rest < all) {
-                    const uint32_t here = __ballot_sync(0xffffffffu, rest < before);
-                    const int at = __ffs(here) - 1;          // the first tile that ends behind the start
-                    tile = t0 + at;
-                    off = (int)rest - __shfl_sync(0xffffffffu, before - n, at);
-                    break;
-                }
-                rest -= all;
-            }
-        }
-        if (lane == 0) {
-            c.rounds = rounds;
-            c.seq = lo, c.head = head, c.tile = tile, c.off = off;
-            c.left = count;
-        }
+    if (tid == kPgWalkWarp * 32) c.rounds = rounds, c.start = start, c.left = count;
+}
+// ... and where it begins, by the walking warp.
+__device__ __noinline__ void plan_start(const PagedAttnParams& p, const Control& c, const long long* line, Walk& w) {
+    int lo = 0, hi = p.n_sequences;
+#pragma unroll 1
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (line[mid] <= c.start) lo = mid;
+        else hi = mid;
     }
+    w.seq = w.loaded = lo;
+    w.q = load_seq(p, lo);
+    w.left = c.left;
+    if (w.left > 0) place(p, w, c.start - line[lo]);
 }
 
 // ------------------------------------------------------------------------------------------------------ small pieces
-__device__ __forceinline__ void streams_barrier() { asm volatile("bar.sync 2, %0;" ::"n"(kPgSoftmax) : "memory"); }
-
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* map, int x, int slot, int head, int page, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
         "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ bool wait_segment(const Control& c, uint32_t segment, const Waiter& wait) {
+    return wait(&c.seg_full[segment % kSegments], (segment / kSegments) & 1);
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
         : "memory");
 }
 
@@ -408,7 +511,7 @@ constexpr uint32_t paged_smem() {
     return 2 * Shape<D>::kTileB + Shape<D>::kRing + 1024 + (uint32_t)((sizeof(Control) + 127) / 128 * 128);
 }
 static_assert(paged_smem<128>() <= 232448 && paged_smem<64>() <= 232448, "shared memory");
-static_assert((kPagedMaxSequences + 1) * 12 <= Shape<128>::kRing && (kPagedMaxSequences + 1) * 12 <= Shape<64>::kRing, "plan's scratch");
+static_assert(kPagedMaxSequences * 12 <= Shape<128>::kRing && kPagedMaxSequences * 12 <= Shape<64>::kRing, "plan's scratch");
 static_assert(kPagedMaxGrid <= kPgThreads, "a thread per part in the plan");
 
 // ------------------------------------------------------------------------------------------------------ the kernel
@@ -424,17 +527,28 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     uint8_t* ring = base + 2 * S::kTileB;
     Control* c = reinterpret_cast<Control*>(ring + S::kRing);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const WaitCtl ctl{&c->abort_flag, p.status, kStatusTimeout, kWaitLimitNs};
+    const Waiter wait{&c->abort_flag, p.status};
 
-    if (tid == 0) {
-        for (int i = 0; i < S::kStages; ++i) {
-            mbar_init(smem_u32(&c->kv_full[i]), 1);
-            mbar_init(smem_u32(&c->kv_empty[i]), 1);
+    if (tid == kPgValueWarp * 32) {
+#pragma unroll 1
+        for (int i = 0; i < 5; ++i) {
+            mbar_init(smem_u32(&c->k_full[i]), 1);
+            mbar_init(smem_u32(&c->k_empty[i]), 1);
+            mbar_init(smem_u32(&c->v_full[i]), 1);
+            mbar_init(smem_u32(&c->v_empty[i]), 1);
         }
-        mbar_init(smem_u32(&c->q_full), kPgSoftmax);
+        mbar_init(smem_u32(&c->q_full), kPgSoftmax / 32);
+        mbar_init(smem_u32(&c->together), kPgSoftmax / 32);
+#pragma unroll 1
+        for (int i = 0; i < kSegments; ++i) {
+            mbar_init(smem_u32(&c->seg_full[i]), 1);
+            mbar_init(smem_u32(&c->seg_empty[i]), 3 + kPgSoftmax / 32);   // both copying warps, products, softmax warps
+        }
+        mbar_init(smem_u32(&c->stagger), 4);
+#pragma unroll 1
         for (int t = 0; t < 2; ++t) {
             mbar_init(smem_u32(&c->s_full[t]), 1);
-            mbar_init(smem_u32(&c->p_full[t]), 128);
+            mbar_init(smem_u32(&c->p_full[t]), 4);
             mbar_init(smem_u32(&c->o_full[t]), 1);
         }
         c->abort_flag = (*reinterpret_cast<volatile int*>(p.status) != 0) ? 1 : 0;
@@ -446,7 +560,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         tmem_alloc(smem_u32(&c->tmem_base), 512);
         tmem_relinquish();
     }
-    if (warp == kPgTmaWarp && lane == 0) {
+    if (warp == kPgKeyWarp && lane == 0) {
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
         if (p.one_page_box) {
@@ -455,8 +569,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
     }
     __syncwarp();
-    plan_work(p, *c, ring);
-    fence_proxy_async_smem();                                // the plan's scratch is the copies' ring
+    const bool few = p.n_sequences <= 32 && !p.rounds;
+    long long* line = reinterpret_cast<long long*>(ring);
+    if (!few) {
+        plan_many(p, *c, line, reinterpret_cast<int*>(line + p.n_sequences));
+        fence_proxy_async_smem();                            // the plan's scratch is the copies' ring
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -465,53 +583,80 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
     if (warp >= kPgMmaWarp) {
         setmaxnreg_dec<kPgControlRegs>();
-        if (warp == kPgTmaWarp) {
+        if (warp == kPgKeyWarp || warp == kPgValueWarp) {
             // ------------------------------------------------------------------------------------- copies
-            Walk walk(*c);
-            Segment g;
-            bool ok = true;
-            uint32_t slot = 0, phase = 1;                    // ring slot; the parity of its last release (none in the first round)
-            bool first_round = true;
-            while (ok && walk.next(p, *c, g)) {
-                const int ahead = min(g.rows > 128 ? 1 : 2, g.n), pairs = 2 * (g.n - ahead);
-                const int* pages = p.table + g.seq * p.table_stride;
-                for (int i = 0; i < 2 * g.n; ++i) {
-                    // entry i: a K tile for i < ahead, then V and K in turn while K tiles are left, then V tiles
-                    const int b = i - ahead;
-                    const bool is_v = b >= 0 && (b >= pairs || (b & 1) == 0);
-                    const int j = b < 0 ? i : (b >= pairs ? b - (g.n - ahead) : (b >> 1) + (is_v ? 0 : ahead));
-                    const int key0 = (g.kt0 + j) * 128;
-                    const bool whole = p.one_page_box && key0 / p.page_size == (key0 + 127) / p.page_size;
-                    const int rows = whole ? 128 : p.box_rows, key = key0 + lane * rows;
-                    const bool mine = lane * rows < 128 && key < g.hi && key + rows > g.lo;
-                    int page = -1, at = 0;
-                    if (mine) {
-                        const int n = key / p.page_size;
-                        at = key - n * p.page_size;
-                        page = pages[n];
-                        if (page < 0 || page >= p.n_pages) {   // not there: its rows arrive as zeros
-                            page = -1;
-                            atomicCAS(p.status, 0, kStatusRange);
+            // One warp for the keys, one for the values.  A lane looks up the page of its box of a tile, a tile ahead; the
+            // copies are issued by one lane, box by box, with operands that are the same in the whole warp (a copy per lane
+            // costs a turn of the warp each).
+            const bool values = warp == kPgValueWarp;
+            const CUtensorMap *map = values ? &map_v : &map_k, *page_map = values ? &map_v_page : &map_k_page;
+            uint64_t *full = values ? c->v_full : c->k_full, *empty = values ? c->v_empty : c->k_empty;
+            const uint32_t slots = values ? S::kValueSlots : S::kKeySlots;
+            const uint32_t ring_addr = smem_u32(ring) + (values ? S::kKeySlots * S::kTileB : 0);
+            const uint32_t elected = elect_one();
+            bool ok = true, first_round = true;              // (of the ring: nothing to wait for)
+            uint32_t slot = 0, phase = 1;                    // the parity of the slot's last release
+#pragma unroll 1
+            for (uint32_t segment = 0; ok; ++segment) {
+                ok = __all_sync(0xffffffffu, wait_segment(*c, segment, wait));
+                if (!ok) break;
+                const Segment* g = &c->seg[segment % kSegments];
+                const int n = g->n, head = g->head, lo = g->lo, hi = g->hi, kt0 = g->kt0;
+                const int* pages = p.table + g->seq * p.table_stride;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c->seg_empty[segment % kSegments]));
+                if (n == 0) break;
+                // this lane's box of the next tile to look up; and the tile as a whole, where it lies within a page
+                int key = kt0 * 128 + lane * p.box_rows;
+                int entry0 = kt0 * 128 / p.page_size, at0 = kt0 * 128 - entry0 * p.page_size;
+                int entry = key / p.page_size, at = key - entry * p.page_size;
+                int page, page_at;
+                uint32_t which, whole;
+                auto look_up = [&]() {
+                    whole = p.one_page_box && at0 + 128 <= p.page_size;
+                    const bool mine = whole ? lane == 0 : lane * p.box_rows < 128 && key < hi && key + p.box_rows > lo;
+                    page = mine ? pages[whole ? entry0 : entry] : 0;
+                    page_at = whole ? at0 : at;
+                    which = __ballot_sync(0xffffffffu, mine);
+                    key += 128, at0 += 128, at += 128;
+#pragma unroll 1
+                    while (at0 >= p.page_size) at0 -= p.page_size, ++entry0;
+#pragma unroll 1
+                    while (at >= p.page_size) at -= p.page_size, ++entry;
+                };
+                look_up();
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
+                    int my_page = page;
+                    const int my_at = page_at;
+                    uint32_t left = which;
+                    const int rows = whole ? 128 : p.box_rows;
+                    const CUtensorMap* m = whole ? page_map : map;
+                    if (j + 1 < n) look_up();
+                    if (!first_round) ok = __all_sync(0xffffffffu, wait(&empty[slot], phase));
+                    if (!ok) break;
+                    if (my_page < 0 || my_page >= p.n_pages) {   // not there: its rows arrive as zeros
+                        my_page = -1;
+                        atomicCAS(p.status, 0, kStatusRange);
+                    }
+                    const uint32_t bar = smem_u32(&full[slot]), dst = ring_addr + slot * S::kTileB;
+                    if (elected) {
+                        if (left) mbar_expect_tx(bar, (uint32_t)(__popc(left) * rows * D * 2));
+                        else mbar_arrive(bar);
+                    }
+                    __syncwarp();
+#pragma unroll 1
+                    while (left) {
+                        const int b = __ffs(left) - 1;
+                        left &= left - 1;
+                        const int box_page = __shfl_sync(0xffffffffu, my_page, b), box_at = __shfl_sync(0xffffffffu, my_at, b);
+                        if (elected) {
+#pragma unroll
+                            for (int x = 0; x < S::kBlocks; ++x) tma_load_4d(dst + b * rows * 128 + x * 16384, m, x * 64, box_at, head, box_page, bar);
                         }
                     }
-                    const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
-                    if (!first_round) ok = mbar_wait(smem_u32(&c->kv_empty[slot]), phase, ctl);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    const uint32_t full = smem_u32(&c->kv_full[slot]);
-                    if (lane == 0) {
-                        if (boxes) mbar_expect_tx(full, (uint32_t)(boxes * rows * D * 2));
-                        else mbar_arrive(full);
-                    }
                     __syncwarp();
-                    if (mine) {
-                        const void* map = is_v ? (whole ? &map_v_page : &map_v) : (whole ? &map_k_page : &map_k);
-                        const uint32_t dst = smem_u32(ring) + slot * S::kTileB + lane * rows * 128;
-#pragma unroll
-                        for (int x = 0; x < S::kBlocks; ++x) tma_load_4d(dst + x * 16384, map, x * 64, at, g.head, page, full);
-                    }
-                    __syncwarp();
-                    if (++slot == S::kStages) {
+                    if (++slot == slots) {
                         slot = 0;
                         phase ^= 1;
                         first_round = false;
@@ -521,55 +666,122 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         } else if (warp == kPgMmaWarp) {
             // ------------------------------------------------------------------------------------- products
             if (elect_one()) {
-                Walk walk(*c);
-                Segment g;
                 bool ok = true;
-                uint32_t entry = 0, segment = 0, visit[2] = {0, 0};
                 const uint32_t q_addr = smem_u32(sQ), ring_addr = smem_u32(ring);
-                auto wait_full = [&](uint32_t e) {
-                    return mbar_wait(smem_u32(&c->kv_full[e % S::kStages]), (e / S::kStages) & 1, ctl);
+                uint32_t k_next = 0, k_phase = 0, v_next = 0, v_phase = 0, visit0 = 0, visit1 = 0, staggered = 0;
+                auto take_k = [&](uint32_t& mine) {
+                    mine = k_next;
+                    const bool got = wait(&c->k_full[k_next], k_phase);
+                    if (++k_next == S::kKeySlots) k_next = 0, k_phase ^= 1;
+                    return got;
                 };
-                auto tile_at = [&](uint32_t e) { return ring_addr + (e % S::kStages) * S::kTileB; };
-                auto release = [&](uint32_t e) { umma_commit(smem_u32(&c->kv_empty[e % S::kStages])); };
-                while (ok && walk.next(p, *c, g)) {
-                    const bool two = g.rows > 128;
-                    const int ahead = min(two ? 1 : 2, g.n);
-                    ok = mbar_wait(smem_u32(&c->q_full), segment & 1, ctl);
-                    ++segment;
-                    for (int j = 0; ok && j < ahead; ++j) {
-                        const uint32_t ek = entry + ring_of_k(j, ahead);
-                        ok = wait_full(ek);
+                auto take_v = [&](uint32_t& mine) {
+                    mine = v_next;
+                    const bool got = wait(&c->v_full[v_next], v_phase);
+                    if (++v_next == S::kValueSlots) v_next = 0, v_phase ^= 1;
+                    return got;
+                };
+                auto scores = [&](int t, uint32_t q, uint32_t k_slot) {
+                    products_qk<D, F16>(tmem_base + t * 128, q, ring_addr + k_slot * S::kTileB);
+                    umma_commit(smem_u32(&c->s_full[t]));
+                };
+                auto output = [&](int t, uint32_t v_slot, uint32_t& visit, bool accumulate) {
+                    const uint32_t o_t = tmem_base + 256 + t * 128, s_t = tmem_base + t * 128, v = ring_addr + (S::kKeySlots + v_slot) * S::kTileB;
+                    if (!wait(&c->p_full[t], visit)) return false;
+                    ++visit;
+                    tc_fence_after();
+                    products_pv<D, F16>(o_t, s_t, v, accumulate);
+                    umma_commit(smem_u32(&c->o_full[t]));
+                    return true;
+                };
+                auto release_k = [&](uint32_t e) { umma_commit(smem_u32(&c->k_empty[e])); };
+                auto release_v = [&](uint32_t e) { umma_commit(smem_u32(&c->v_empty[e])); };
+#pragma unroll 1
+                for (uint32_t segment = 0; ok; ++segment) {
+                    ok = wait_segment(*c, segment, wait);
+                    if (!ok) break;
+                    const Segment* at = &c->seg[segment % kSegments];
+                    const bool two = at->rows > 128;
+                    const int n = at->n;
+                    mbar_arrive(smem_u32(&c->seg_empty[segment % kSegments]));
+                    if (n == 0) break;
+                    uint32_t k, v;
+                    ok = wait(&c->q_full, segment) && take_k(k);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (two) {                               // both streams take every tile
+                        scores(0, q_addr, k);
+                        // stream 1 starts half a period behind stream 0, when that is in the middle of its first exponentials:
+                        // started together, the streams stay one product's time apart and share the exponentials' pipe
+                        // (a period of 3600 cycles instead of 2900)
+                        ok = wait(&c->stagger, staggered++);
                         if (!ok) break;
-                        tc_fence_after();
-                        for (int t = two ? 0 : j; t < (two ? 2 : j + 1); ++t) {
-                            products_qk<D, F16>(tmem_base + t * 128, q_addr + (two ? t * S::kTileB : 0), tile_at(ek));
-                            umma_commit(smem_u32(&c->s_full[t]));
+                        scores(1, q_addr + S::kTileB, k);
+                        release_k(k);
+#pragma unroll 1
+                        for (int j = 0; j < n; ++j) {
+                            const bool more = j + 1 < n;
+                            ok = take_v(v) && (!more || take_k(k)) && output(0, v, visit0, j > 0);
+                            if (!ok) break;
+                            if (more) scores(0, q_addr, k);
+                            ok = output(1, v, visit1, j > 0);
+                            if (!ok) break;
+                            release_v(v);
+                            if (more) {
+                                scores(1, q_addr + S::kTileB, k);
+                                release_k(k);
+                            }
                         }
-                        release(ek);
-                    }
-                    for (int j = 0; ok && j < g.n; ++j) {
-                        const uint32_t ev = entry + ring_of_v(j, g.n, ahead);
-                        const bool more = j + ahead < g.n;
-                        const uint32_t ek = entry + ring_of_k(j + ahead, ahead);
-                        ok = wait_full(ev);
-                        for (int t = two ? 0 : (j & 1); ok && t < (two ? 2 : (j & 1) + 1); ++t) {
-                            ok = mbar_wait(smem_u32(&c->p_full[t]), visit[t] & 1, ctl);
-                            ++visit[t];
+                    } else {                                 // the streams take every other tile
+                        scores(0, q_addr, k);
+                        release_k(k);
+                        if (n > 1) {
+                            ok = take_k(k);
                             if (!ok) break;
                             tc_fence_after();
-                            products_pv<D, F16>(tmem_base + 256 + t * 128, tmem_base + t * 128, tile_at(ev), two ? j > 0 : j > 1);
-                            umma_commit(smem_u32(&c->o_full[t]));
-                            if (t == 1 || !two) release(ev);
-                            if (more) {
-                                ok = wait_full(ek);
+                            scores(1, q_addr, k);
+                            release_k(k);
+                        }
+#pragma unroll 1
+                        for (int j = 0; j < n; ++j) {
+                            const int t = j & 1;
+                            ok = take_v(v) && output(t, v, t ? visit1 : visit0, j > 1);
+                            if (!ok) break;
+                            release_v(v);
+                            if (j + 2 < n) {
+                                ok = take_k(k);
                                 if (!ok) break;
-                                products_qk<D, F16>(tmem_base + t * 128, q_addr + (two ? t * S::kTileB : 0), tile_at(ek));
-                                umma_commit(smem_u32(&c->s_full[t]));
-                                if (t == 1 || !two) release(ek);
+                                scores(t, q_addr, k);
+                                release_k(k);
                             }
                         }
                     }
-                    entry += 2 * g.n;
+                }
+            }
+        } else if (warp == kPgWalkWarp) {
+            // ------------------------------------------------------------------------------------- the work, stretch by stretch
+            Walk walk;
+            walk.round = walk.head = walk.tile = 0;
+            walk.at = 0;
+            if (few) {
+                plan_few(p, *c, walk);
+            } else {
+                plan_start(p, *c, line, walk);
+                fence_proxy_async_smem();
+                __syncwarp();
+            }
+            if (lane == 0) {
+                bool more = true, ok = true;
+#pragma unroll 1
+                for (uint32_t segment = 0; ok && more; ++segment) {
+                    Segment g;
+                    more = walk.next(p, *c, g);
+                    if (!more) g.n = 0;
+                    const uint32_t slot = segment % kSegments, round = segment / kSegments;
+                    if (round > 0) ok = wait(&c->seg_empty[slot], round - 1);
+                    if (!ok) break;
+                    c->seg[slot] = g;
+                    mbar_arrive(smem_u32(&c->seg_full[slot]));
                 }
             }
         }
@@ -581,126 +793,175 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         const uint32_t t_S = lane_base + t * 128, t_O = lane_base + 256 + t * 128;
         const float scale = p.scale_log2;
         const uint64_t scale2 = pack2(scale, scale);
-        Walk walk(*c);
-        Segment g;
-        bool ok = true;                                      // false once a wait ran out: barriers go on, work does not
-        uint32_t entry = 0, visit = 0;
-        while (walk.next(p, *c, g)) {
+        uint32_t entry = 0, visit = 0, met = 0;
+        // all softmax warps have come here (with a limit, like every wait: a wait that runs out ends the warp's work)
+        auto meet_all = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&c->together));
+            return __all_sync(0xffffffffu, wait(&c->together, met++ & 1));
+        };
+        bool ok = true;
+#pragma unroll 1
+        for (uint32_t segment = 0; ok; ++segment) {
+            ok = __all_sync(0xffffffffu, wait_segment(*c, segment, wait));
+            if (!ok) break;
+            const Segment& g = c->seg[segment % kSegments];
+            const int n = g.n;
+            if (n == 0) break;
             const bool two = g.rows > 128;
-            const int ahead = min(two ? 1 : 2, g.n), first = two ? t * 128 : 0;
-            streams_barrier();                               // the last segment's queries and tensor memory are done with
+            const int first = two ? t * 128 : 0;
+            ok = meet_all();                                 // the last segment's queries and tensor memory are done with
+            if (!ok) break;
             {
-                const int loaders = two ? 128 : 256, id = two ? (tid & 127) : tid;
-                uint8_t* dst = sQ + (two ? t * S::kTileB : 0);
-                const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + g.q.row0 * p.q_token;
-#pragma unroll 8
-                for (int i = id; i < 128 * (D / 8); i += loaders) {
-                    const int r = i / (D / 8), ch = i % (D / 8), in_seq = g.tile * kPagedRows + first + r;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (first + r < g.rows) {
-                        const int token = in_seq / p.share, h = g.head * p.share + in_seq - token * p.share;
-                        v = *reinterpret_cast<const uint4*>(q + token * p.q_token + h * p.q_head + ch * 8);
-                    }
-                    *reinterpret_cast<uint4*>(dst + (ch >> 3) * 16384 + sw128_offset(r, ch & 7)) = v;
+                // a thread has one 16-byte piece of every kStep-th row, and loads them all before it stores the first
+                constexpr int kPer = D / 8, kRowsAtOnce = 128 / kPer, kMost = 128 / kRowsAtOnce;
+                const int step = two ? kRowsAtOnce : 2 * kRowsAtOnce, mine = two ? kMost : kMost / 2;
+                const int id = two ? (tid & 127) : tid, ch = id % kPer, r0 = id / kPer;
+                uint8_t* dst = sQ + (two ? t * S::kTileB : 0) + (ch >> 3) * 16384;
+                const int in_seq = g.tile * kPagedRows + first + r0;
+                int token = in_seq / p.share, h = in_seq - token * p.share;
+                const int step_token = step / p.share, step_h = step - step_token * p.share;
+                const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q) + g.q.row0 * p.q_token + g.head * p.share * p.q_head + ch * 8;
+                const int rows = g.rows - first;
+                uint4 v[kMost];
+#pragma unroll
+                for (int i = 0; i < kMost; ++i) {
+                    v[i] = make_uint4(0, 0, 0, 0);
+                    if (i < mine && r0 + i * step < rows) v[i] = *reinterpret_cast<const uint4*>(q + token * p.q_token + h * p.q_head);
+                    token += step_token, h += step_h;
+                    if (h >= p.share) h -= p.share, ++token;
                 }
+#pragma unroll
+                for (int i = 0; i < kMost; ++i)
+                    if (i < mine) *reinterpret_cast<uint4*>(dst + sw128_offset(r0 + i * step, ch & 7)) = v[i];
                 fence_proxy_async_smem();
-                mbar_arrive(smem_u32(&c->q_full));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c->q_full));
             }
             const int in_seq = g.tile * kPagedRows + first + row, token = in_seq / p.share;
             const bool valid = first + row < g.rows, busy = first + (warp & 3) * 32 < g.rows;   // busy: any row of the warp
-            int lo = 0, hi = 1 << 30;                        // keys that this row sees
+            const int key_first = g.kt0 * 128, all_lo = g.lo - key_first, all_hi = g.hi - key_first;
+            int lo = all_lo, hi = all_hi;                    // keys that this row sees, from key_first on (not a row: any)
             if (valid) {
                 const int pos = g.q.keys - g.q.tokens + token;
-                lo = sees_begin(p, pos);
-                hi = sees_end(p, g.q.keys, pos);
+                lo = sees_begin(p, pos) - key_first;
+                hi = sees_end(p, g.q.keys, pos) - key_first;
             }
+            // tiles that all rows of the warp see whole
+            const int open0 = (__reduce_max_sync(0xffffffffu, max(lo, 0)) + 127) / 128, open1 = __reduce_min_sync(0xffffffffu, max(hi, 0)) / 128;
             float m = -INFINITY, l = 0.0f;
+            bool fresh = true;                               // some row of the warp has not seen a key yet
             int done = 0;                                    // tiles of this stream
-            for (int j = two ? 0 : t; j < g.n; j += two ? 1 : 2) {
-                const int key0 = (g.kt0 + j) * 128;
-                if (ok) ok = mbar_wait(smem_u32(&c->s_full[t]), visit & 1, ctl);
-                ok = __all_sync(0xffffffffu, ok);
+#pragma unroll 1
+            for (int j = two ? 0 : t; j < n; j += two ? 1 : 2) {
+                ok = __all_sync(0xffffffffu, wait(&c->s_full[t], visit & 1));
+                if (!ok) break;
                 tc_fence_after();
-                if (ok && busy) {
-                    uint32_t s[128];
+                const int from = lo - 128 * j, to = hi - 128 * j;
+                const bool masked = j < open0 || j >= open1;
+                if (masked) {
+                    if ((128 * j < all_lo || 128 * j + 128 > all_hi) && (!two || t == 0)) {
+                        // rows of V that no row of the item sees; with two tiles of rows stream 0 does it for both (its products
+                        // are issued first)
+                        const uint32_t e = entry + j;
+                        ok = __all_sync(0xffffffffu, wait(&c->v_full[e % S::kValueSlots], e / S::kValueSlots));
+                        if (!ok) break;
+                        const int key = 128 * j + row;
+                        if (key < all_lo || key >= all_hi) {
+                            uint8_t* v = ring + (S::kKeySlots + e % S::kValueSlots) * S::kTileB + row * 128;
+#pragma unroll
+                            for (int x = 0; x < S::kBlocks; ++x)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(v + x * 16384 + ((i + row) & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                    }
+                }
+                uint32_t s[128];
+                if (busy) {
 #pragma unroll
                     for (int b = 0; b < 4; ++b) tmem_ld32(t_S + 32 * b, s + 32 * b);
                     tmem_wait_ld();
-                    const int from = lo - key0, to = hi - key0;
-                    if (__any_sync(0xffffffffu, from > 0 || to < 128)) {
+                    if (masked) {
 #pragma unroll
                         for (int i = 0; i < 128; ++i)
                             if (i < from || i >= to) s[i] = 0xff800000u;   // -inf, whatever was there
                     }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    auto highest = [&]() {
+                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 128; i += 8)
+                        for (int i = 0; i < 128; i += 8)
 #pragma unroll
-                        for (int b = 0; b < 4; ++b) mx[b] = max3(mx[b], __uint_as_float(s[i + 2 * b]), __uint_as_float(s[i + 2 * b + 1]));
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                    const bool raise = top > m + kRaise;     // (m is -inf until the row has seen a key)
-                    if (__any_sync(0xffffffffu, raise)) {
-                        const float alpha = raise ? ex2_approx(m - top) : 1.0f;
-                        if (raise) m = top;
-                        l *= alpha;
-                        if (done > 0) {
-                            ok = mbar_wait(smem_u32(&c->o_full[t]), (visit - 1) & 1, ctl);
-                            ok = __all_sync(0xffffffffu, ok);
-                            tc_fence_after();
-                            if (ok) {
+                            for (int b = 0; b < 4; ++b) mx[b] = max3(mx[b], __uint_as_float(s[i + 2 * b]), __uint_as_float(s[i + 2 * b + 1]));
+                        return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+                    };
+                    // rows that have not seen a key yet take the tile's maximum for their reference
+                    bool again, redo = false;
+                    if (fresh) {
+                        const float top = highest();
+                        if (m == -INFINITY) m = top;
+                        fresh = __any_sync(0xffffffffu, m == -INFINITY);
+                    }
+                    float sum;
 #pragma unroll 1
-                                for (int b = 0; b < D / 32; ++b) {
-                                    uint32_t o[32];
-                                    tmem_ld32(t_O + b * 32, o);
-                                    tmem_wait_ld();
+                    while (true) {
+                        const float ref = m == -INFINITY ? 0.0f : m;
+                        uint64_t sum_a = 0, sum_b = 0;
 #pragma unroll
-                                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                    tmem_st32(t_O + b * 32, o);
-                                }
+                        for (int b = 0; b < 4; ++b) {
+                            uint32_t pr[16];
+                            probabilities<F16>(s + 32 * b, scale2, pack2(-ref, -ref), pr, sum_a, sum_b);
+                            tmem_st16(t_S + 16 * b, pr);
+                            if (b == 1 && two && t == 0 && j == 0 && !redo) {
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(smem_u32(&c->stagger));
+                            }
+                        }
+                        float s0, s1;
+                        unpack2(add2(sum_a, sum_b), s0, s1);
+                        sum = s0 + s1;
+                        again = !(sum < raise_at<F16>());
+                        if (!__any_sync(0xffffffffu, again)) break;
+                        // Rare: scores far above the reference.  The products so far are waited for, O and the sum are
+                        // brought to the new reference, and the tile is done again.
+                        const float top = highest();
+                        again = again && top > m;            // (a NaN among the scores stays one)
+                        if (!__any_sync(0xffffffffu, again)) break;
+                        const float alpha = again ? ex2_approx(ref - top) : 1.0f;
+                        if (again) m = top;
+                        l *= alpha;
+                        redo = true;
+                        if (done > 0) {
+                            ok = __all_sync(0xffffffffu, wait(&c->o_full[t], visit - 1));
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int b = 0; ok && b < D; b += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(t_O + b, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st16(t_O + b, o);
                             }
                         }
                     }
-                    const float ref = m == -INFINITY ? 0.0f : m;
-                    const uint64_t negm2 = pack2(-ref, -ref);
-                    uint64_t sum_a = 0, sum_b = 0;
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        uint32_t pr[16];
-                        probabilities<F16>(s + 32 * b, scale2, negm2, pr, sum_a, sum_b);
-                        tmem_st16(t_S + 16 * b, pr);
-                    }
-                    float s0, s1;
-                    unpack2(add2(sum_a, sum_b), s0, s1);
-                    l += s0 + s1;
+                    l += sum;
+                    tmem_wait_st();
                 }
-                if ((key0 < g.lo || key0 + 128 > g.hi) && (!two || t == 0)) {
-                    // rows of V that no row of the item sees; with two tiles of rows stream 0 does it for both (its products
-                    // are issued first)
-                    const uint32_t e = entry + ring_of_v(j, g.n, ahead);
-                    if (ok) ok = mbar_wait(smem_u32(&c->kv_full[e % S::kStages]), (e / S::kStages) & 1, ctl);
-                    ok = __all_sync(0xffffffffu, ok);
-                    const int key = key0 + row;
-                    if (ok && (key < g.lo || key >= g.hi)) {
-                        uint8_t* v = ring + (e % S::kStages) * S::kTileB + row * 128;
-#pragma unroll
-                        for (int x = 0; x < S::kBlocks; ++x)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(v + x * 16384 + ((i + row) & 7) * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async_smem();
-                }
-                tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(smem_u32(&c->p_full[t]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c->p_full[t]));
+                if (!ok) break;
                 ++visit;
                 ++done;
             }
-            entry += 2 * g.n;
+            if (!ok) break;
+            entry += n;                                      // V tiles so far
 
             // ------------------------------------------------------------------------------------- results
             if (done > 0) {
-                if (ok) ok = mbar_wait(smem_u32(&c->o_full[t]), (visit - 1) & 1, ctl);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = __all_sync(0xffffffffu, wait(&c->o_full[t], (visit - 1) & 1));
+                if (!ok) break;
                 tc_fence_after();
             }
             float a[2] = {1.0f, 1.0f};                       // weights of the two streams' sums
@@ -708,7 +969,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 float2* ml = reinterpret_cast<float2*>(sQ + S::kTileB);   // (the second tile of queries is not in use)
                 ml[t * 128 + row] = make_float2(m, l);
                 tc_fence_before();
-                streams_barrier();
+                ok = meet_all();
+                if (!ok) break;
                 tc_fence_after();
                 const float2 ml0 = ml[row], ml1 = ml[128 + row];
                 const float m0 = ml0.x, m1 = ml1.x;
@@ -729,7 +991,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             uint16_t* out = reinterpret_cast<uint16_t*>(p.out) + out_row * p.out_token + h * p.out_head;
             // this thread's columns: all of its stream's row, or half of the joined row
             const int col0 = two ? 0 : t * (D / 2), cols = two ? D : D / 2;
-            if (ok && busy) {
+            if (busy) {
 #pragma unroll 1
                 for (int b = 0; b < cols; b += 32) {
                     uint32_t o[32];
@@ -779,6 +1041,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 p.pieces[piece] = d;
             }
             tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&c->seg_empty[segment % kSegments]));
         }
     }
 
@@ -791,6 +1055,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (c->abort_flag) {
             // a wait ran out: copies and products that may still be in flight get time to land
             const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
             while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
         }
         __syncwarp();

@@ -7,6 +7,7 @@
 namespace regenvc {
 
 constexpr int kPagedMaxGrid = 160;           // thread blocks of the attention kernel
+constexpr int kPagedRoundsFrom = 132;         // items from which on there may be one for every thread block
 constexpr int kPagedMaxSequences = 4096;
 constexpr int kPagedRows = 256;              // rows of an item
 

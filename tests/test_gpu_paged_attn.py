@@ -84,3 +84,23 @@ def test_against_the_64_bit_form(new, keys, hq, hk, d, page, dtype, group, windo
     out, lse = B.regenvc_paged_attn_forward(*c["args"], group=group, window=window, lse=True)
     assert B.regenvc_device_status() == B.OK
     check(c, new, keys, out, lse, group, window)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("new,group", [(1, 0), (200, 0), (300, 1), (129, 40)])
+def test_scores_that_rise_along_the_keys(dtype, new, group):
+    """Every 40 keys the scores rise by some 20 nats: references are raised in either half of a tile, again and again."""
+    keys, d = 900, 128
+    c = make([new], [keys], 2, 1, d, 64, dtype, seed=3)
+    k = c["k64"][0]
+    k += (torch.arange(keys) // 40).double()[:, None, None] * 20 / math.sqrt(d)    # q . (1, .., 1) is about d here, below
+    k = k.to(dtype).double()
+    q = (1 + 0.2 * c["q"].double()).to(dtype)
+    c["q"], c["k64"] = q, [k]
+    args = list(c["args"])
+    args[0] = q.to(DEV)
+    at = slots_of(c["table"], 0, keys, 64)
+    args[1][at[0].to(DEV), at[1].to(DEV)] = k.to(dtype).to(DEV)
+    out, lse = B.regenvc_paged_attn_forward(*args, group=group, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, [new], [keys], out, lse, group, 0)
