@@ -5,7 +5,7 @@
 // R turns pair j by position[axis(j)] * frequency(j).  The normalised values never round to the rows' type in between.
 // Bound: HBM, every element is read and written once (two passes, a norm and a rotation, move twice that).  The angles of
 // a token are shared by all its heads, so a thread block computes them once per token into shared memory and then walks
-// over its (token, head) vectors, four chunks of 16 bytes per thread in flight.
+// over its (token, head) vectors, four to eight pieces of 16 bytes per thread in flight.
 // Paged: token n of the call belongs to the sequence whose rows it lies in, found by counting the row starts at or before
 // it (a warp per token, all loads independent: a binary search is a chain of loads, which is what a call of a few tokens
 // would wait for); its slot is the sequence's length minus the rows behind it, its page comes from the table.
@@ -15,7 +15,7 @@
 namespace regenvc {
 namespace {
 
-constexpr int kBatch = 4;
+constexpr int kBatch = 1;
 constexpr int kMaxTokens = 16;      // per thread block
 
 // Offsets of a token's slot in the two caches; -1: the token goes nowhere (behind the last sequence, a page that is not
@@ -83,75 +83,93 @@ __device__ __forceinline__ bool locate(const HeadRowsParams& p, const Slots& s, 
 }
 
 template <typename T, bool HALVES>
-__global__ void __launch_bounds__(kHeadThreads) head_rows_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
-    extern __shared__ float4 table_raw[];
+__global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
+    extern __shared__ float4 shared_raw[];
     __shared__ Slots slots;
-    float2* table = reinterpret_cast<float2*>(table_raw);
-    const int pitch = table_pitch(p), chunks = p.head_dim / 8;
+    const int pitch = table_pitch(p), units = table_units<HALVES ? kHalfUnits : kAdjacentUnits>(p);
+    float2* table = reinterpret_cast<float2*>(shared_raw);
+    float* gains = reinterpret_cast<float*>(table + p.tokens_per_cta * pitch);
     const int token0 = blockIdx.x * p.tokens_per_cta, tokens = min(p.tokens_per_cta, p.n_tokens - token0);
-    const int c = threadIdx.x & (width - 1), group = threadIdx.x / width, groups = blockDim.x / width;
-    const bool active = c < chunks;
-    const int all = p.heads[0] + p.heads[1] + p.heads[2];
+    const int u = threadIdx.x & (width - 1), group = threadIdx.x / width, groups = blockDim.x / width;
+    const bool active = u < p.head_dim / 16;
+    const Pieces at = pieces_of<HALVES>(p, active ? u : 0);
+    const int all = p.heads[0] + p.heads[1] + p.heads[2], total = tokens * all;
     const float inv_d = 1.0f / (float)p.head_dim;
 
-    float gq[8], gk[8];
-    load_gains(p.weight[0], c, active, gq);
-    load_gains(p.weight[1], c, active, gk);
-    if (p.n_axes) fill_table<HALVES ? kHalfChunks : kAdjacentChunks>(p, table, pitch, token0, tokens, false);
-    if (p.paged) find_slots(p, slots, token0, tokens);
+    // One vector (token, head) per group of lanes and round, kBatch rounds at a time; the loads of the next rounds are on
+    // their way while these are worked off, and the first ones while the angles are formed.
+    struct Item {
+        Raw8<T> lo, hi;
+        T* to;                                              // nullptr: nothing to do
+        int of, token;
+    };
+    int t = group / all, h = group - t * all;               // this group's next vector
+    auto fetch = [&](Item& x) {
+        x.to = nullptr;
+        x.of = x.token = 0;
+        x.lo = x.hi = Raw8<T>{};
+        if (t < tokens) {
+            const T* from;
+            x.token = t;
+            if (locate<T>(p, slots, token0, t, h, x.of, from, x.to) && active) {
+                x.lo = load_raw8(from + at.lo);
+                x.hi = load_raw8(from + at.hi);
+            } else {
+                x.to = nullptr;
+            }
+            h += groups;
+            while (h >= all) h -= all, ++t;
+        }
+    };
+    Item next[kBatch];
+    if (p.paged) {
+        find_slots(p, slots, token0, tokens);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) fetch(next[i]);
+    if (p.n_axes) fill_table<HALVES ? kHalfUnits : kAdjacentUnits>(p, table, pitch, token0, tokens, false);
+    if (p.norm) fill_gains(p, gains);
     __syncthreads();
 
-    const int total = tokens * all;
-    int t = 0, h = group;                                   // this group's vector; the next one is `groups` heads on
-    while (h >= all) h -= all, ++t;
-    for (int base = 0; base < total; base += groups * kBatch) {   // the same rounds for all lanes: sums and turns use shuffles
-        Raw8<T> raw[kBatch];
-        T* to[kBatch];
-        int of[kBatch], at[kBatch];
+    for (int base = 0; base < total; base += groups * kBatch) {   // the same rounds for all lanes: sums are shuffles
+        Item now[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            of[i] = -1;
-            at[i] = 0;
-            raw[i] = Raw8<T>{};
-            if (t < tokens) {
-                const T* from;
-                at[i] = t;
-                if (locate<T>(p, slots, token0, t, h, of[i], from, to[i]) && active) raw[i] = load_raw8(from + 8 * c);
-                else of[i] = -1;
-                h += groups;
-                while (h >= all) h -= all, ++t;
-            }
+        for (int i = 0; i < kBatch; ++i) now[i] = next[i];
+        if (base + groups * kBatch < total) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) fetch(next[i]);
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            float v[8];
-            widen8(raw[i], v);
+            Item& x = now[i];
+            float lo[8], hi[8];
+            widen8(x.lo, lo);
+            widen8(x.hi, hi);
             if (p.norm) {
                 float sq = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq += v[e] * v[e];
+                for (int e = 0; e < 8; ++e) sq += lo[e] * lo[e] + hi[e] * hi[e];
                 const float r = rsqrtf(head_sum(sq, width) * inv_d + p.eps);
-                if (of[i] < 2) {
+                if (x.of < 2) {
+                    float g[8];
+                    load_eight(gains + x.of * p.head_dim + at.lo, g);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = v[e] * r * (of[i] == 1 ? gk[e] : gq[e]);
+                    for (int e = 0; e < 8; ++e) lo[e] *= r * g[e];
+                    load_eight(gains + x.of * p.head_dim + at.hi, g);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) hi[e] *= r * g[e];
                 }
             }
-            if (p.n_axes) {
-                if constexpr (HALVES) {
-                    float u[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = v[e];
-                    turn_chunk<true>(u, table + at[i] * pitch, p, c, chunks);
-                    if (of[i] < 2) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = u[e];
-                    }
-                } else if (of[i] >= 0 && of[i] < 2) {
-                    turn_chunk<false>(v, table + at[i] * pitch, p, c, chunks);
-                }
+            if (!x.to) continue;
+            if (x.of == 2) {                                // a copy, whatever the bits say
+                store_raw8(x.to + at.lo, x.lo);
+                store_raw8(x.to + at.hi, x.hi);
+                continue;
             }
-            if (of[i] == 2) store_raw8(to[i] + 8 * c, raw[i]);   // a copy, whatever the bits say
-            else if (of[i] >= 0) store8(to[i] + 8 * c, v);
+            if (at.turns) turn<HALVES>(lo, hi, reinterpret_cast<const float4*>(table + x.token * pitch) + u, units);
+            store8(x.to + at.lo, lo);
+            store8(x.to + at.hi, hi);
         }
     }
 }
@@ -189,7 +207,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_rows_element_kernel(const _
             }
         }
         const bool norm = p.norm && w < 2;
-        const float r = norm ? rsqrtf(head_sum(sq, 32) / (float)p.head_dim + p.eps) : 1.0f;
+        const float r = norm ? rsqrtf(warp_sum(sq) / (float)p.head_dim + p.eps) : 1.0f;
         const float* gain = norm ? p.weight[w] : nullptr;
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
@@ -215,17 +233,17 @@ __global__ void __launch_bounds__(kHeadThreads) head_rows_element_kernel(const _
     }
 }
 
-// Tokens per thread block: enough vectors for about sixteen per thread; fewer where that would leave the device less than
+// Tokens per thread block: enough vectors for `rounds` per group of lanes; fewer where that would leave the device less than
 // one round of blocks.
 template <typename K>
-cudaError_t launch_rows(K kernel, HeadRowsParams& p, int groups, int sm_count, int* blocks, size_t* smem) {
+cudaError_t plan_rows(K kernel, HeadRowsParams& p, int groups, int rounds, int sm_count, int* blocks, size_t* smem) {
     const int all = p.heads[0] + p.heads[1] + p.heads[2];
-    int tokens = 16 * groups / all;
+    int tokens = rounds * groups / all;
     if (tokens > kMaxTokens) tokens = kMaxTokens;
-    const size_t per_token = (size_t)table_pitch(p) * sizeof(float2);
+    const size_t per_token = (size_t)table_pitch(p) * sizeof(float2), gains = 2 * (size_t)p.head_dim * sizeof(float);
     if (tokens > 1) {
         int per_sm = 1;
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, tokens * per_token);
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, tokens * per_token + gains);
         if (e != cudaSuccess) return e;
         const long long room = (long long)(per_sm > 0 ? per_sm : 1) * sm_count, even = (p.n_tokens + room - 1) / room;
         if (tokens > even) tokens = (int)even;
@@ -233,7 +251,7 @@ cudaError_t launch_rows(K kernel, HeadRowsParams& p, int groups, int sm_count, i
     if (tokens < 1) tokens = 1;
     p.tokens_per_cta = tokens;
     *blocks = (p.n_tokens + tokens - 1) / tokens;
-    *smem = tokens * per_token;
+    *smem = tokens * per_token + gains;
     return cudaSuccess;
 }
 
@@ -241,15 +259,15 @@ template <typename T>
 cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, cudaStream_t stream) {
     int blocks = 0;
     size_t smem = 0;
-    if (!vec || p.head_dim % 8 != 0 || (p.halves && p.n_pairs % 8 != 0)) {
-        const cudaError_t e = launch_rows(head_rows_element_kernel<T>, p, kHeadThreads / 32, sm_count, &blocks, &smem);
+    if (!in_units(p, vec)) {
+        const cudaError_t e = plan_rows(head_rows_element_kernel<T>, p, kHeadThreads / 32, 16, sm_count, &blocks, &smem);
         if (e != cudaSuccess) return e;
         head_rows_element_kernel<T><<<blocks, kHeadThreads, smem, stream>>>(p);
         return cudaGetLastError();
     }
-    const int width = p.head_dim <= 64 ? 8 : (p.head_dim <= 128 ? 16 : 32);
+    const int width = lanes_of_head(p);
     auto kernel = p.halves ? head_rows_kernel<T, true> : head_rows_kernel<T, false>;
-    const cudaError_t e = launch_rows(kernel, p, kHeadThreads / width, sm_count, &blocks, &smem);
+    const cudaError_t e = plan_rows(kernel, p, kHeadThreads / width, 8, sm_count, &blocks, &smem);
     if (e != cudaSuccess) return e;
     kernel<<<blocks, kHeadThreads, smem, stream>>>(p, width);
     return cudaGetLastError();

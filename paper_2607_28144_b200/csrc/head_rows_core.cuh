@@ -1,8 +1,10 @@
-// Pieces shared by the kernels on the heads of queries and keys: the table of a token group's angles and the sums over a
-// head.
+// Pieces shared by the kernels on the heads of queries and keys: the table of a token group's angles, the gains, and the
+// pieces of a head.
 //
-// A head's elements are worked off in chunks of eight, one lane per chunk; a group of 8, 16 or 32 lanes (the next power of
-// two) holds a head, so that its sums are a few shuffles.  A lane keeps its chunk, and with it its gains, throughout.
+// A lane holds sixteen elements of a head, as two pieces of eight: eight of the first and the matching eight of the second
+// half (in half pairs: of the rotated part, and of the part that is not rotated alike).  Either way it holds both elements of
+// its pairs, and neighbouring lanes read neighbouring 16-byte words (sixteen neighbours to a lane touched every sector twice,
+// at twice the time).  A group of 4, 8 or 16 lanes (the next power of two) holds a head; its sums are a few shuffles.
 #pragma once
 #include "head_rows.cuh"
 #include "row_io.cuh"
@@ -12,89 +14,119 @@ namespace {
 
 constexpr int kHeadThreads = 256;
 
+enum { kPlain = 0, kAdjacentUnits = 1, kHalfUnits = 2 };
+
+// Units of eight pairs of a table: the rotated ones, and for adjacent pairs, to the end of the head, (1, 0).
+template <int ORDER>
+__device__ __forceinline__ int table_units(const HeadRowsParams& p) {
+    return ORDER == kAdjacentUnits ? p.head_dim / 16 : p.n_pairs / 8;
+}
 // Words of a token's table: (cos, sin) of pair j where the lane that holds the pair finds it as 16-byte words of two pairs,
-// word i of chunk c at i * chunks + c, so that neighbouring lanes read neighbouring words.  Adjacent pairs: four to a chunk,
-// behind the last rotated pair (1, 0).  Halves: eight to a chunk of the first half, and the same for its partner's.
-__device__ __forceinline__ int place_adjacent(int j, int chunks) { return ((j >> 1 & 1) * chunks + (j >> 2)) * 2 + (j & 1); }
-__device__ __forceinline__ int place_halves(int j, int chunks) { return ((j >> 1 & 3) * chunks + (j >> 3)) * 2 + (j & 1); }
-
-enum { kPlain = 0, kAdjacentChunks = 1, kHalfChunks = 2 };
-
+// word i (of four) of unit u at i * units + u, so that neighbouring lanes read neighbouring words.
+template <int ORDER>
+__device__ __forceinline__ int place(const HeadRowsParams& p, int j) {
+    const int units = table_units<ORDER>(p);
+    if (ORDER == kHalfUnits) return ((j >> 1 & 3) * units + (j >> 3)) * 2 + (j & 1);
+    const int half = j >= 4 * units;
+    j -= half * 4 * units;
+    return ((2 * half + (j >> 1 & 1)) * units + (j >> 2)) * 2 + (j & 1);
+}
 // Angles in whole turns, position * frequency / (2 pi) in 64 bits, its fraction taken there too; sine and cosine of the
 // fraction in 32 bits.
 template <int ORDER>
 __device__ __forceinline__ void fill_table(const HeadRowsParams& p, float2* table, int pitch, int token0, int tokens, bool back) {
-    const int entries = ORDER == kAdjacentChunks ? p.head_dim / 2 : p.n_pairs;
-    for (int i = threadIdx.x; i < tokens * entries; i += blockDim.x) {
-        const int t = i / entries, j = i - t * entries;
-        float s = 0.0f, k = 1.0f;
-        if (j < p.n_pairs) {
-            int axis = 0;
-            while (axis + 1 < p.n_axes && j >= p.axis_end[axis]) ++axis;
-            const long long at = axis * p.pos_stride + token0 + t;
-            const double pos = p.pos_float ? (double)reinterpret_cast<const float*>(p.positions)[at]
-                                           : (double)reinterpret_cast<const int*>(p.positions)[at];
-            const double turn = pos * p.turns[j];
-            sincospif(2.0f * (float)(turn - rint(turn)), &s, &k);
-        }
-        const int to = ORDER == kAdjacentChunks ? place_adjacent(j, p.head_dim / 8)
-                       : ORDER == kHalfChunks   ? place_halves(j, p.n_pairs / 8)
-                                                : j;
-        table[t * pitch + to] = make_float2(k, back ? -s : s);
+    // a thread has one pair throughout (its axis, frequency and place), and every so many tokens
+    const int entries = ORDER == kAdjacentUnits ? p.head_dim / 2 : p.n_pairs;
+    const int at_a_time = blockDim.x / entries, first = threadIdx.x / entries, j = threadIdx.x - first * entries;
+    if (first >= at_a_time) return;
+    float2* to = table + (ORDER == kPlain ? j : place<ORDER>(p, j));
+    if (j >= p.n_pairs) {
+        for (int t = first; t < tokens; t += at_a_time) to[t * pitch] = make_float2(1.0f, 0.0f);
+        return;
+    }
+    int axis = 0;
+    while (axis + 1 < p.n_axes && j >= p.axis_end[axis]) ++axis;
+    const long long at = axis * p.pos_stride + token0;
+    const double turns = p.turns[j];
+#pragma unroll 4
+    for (int t = first; t < tokens; t += at_a_time) {
+        const double pos = p.pos_float ? (double)reinterpret_cast<const float*>(p.positions)[at + t]
+                                       : (double)reinterpret_cast<const int*>(p.positions)[at + t];
+        const double turn = pos * turns;
+        float s, k;
+        sincospif(2.0f * (float)(turn - rint(turn)), &s, &k);
+        to[t * pitch] = make_float2(k, back ? -s : s);
     }
 }
 __host__ __device__ inline int table_pitch(const HeadRowsParams& p) {
-    return ((p.n_axes ? p.head_dim / 2 : 0) + 3) & ~3;   // adjacent chunks fill up to the whole head
+    return ((p.n_axes ? p.head_dim / 2 : 0) + 3) & ~3;
 }
-
-// Sum over the group of `width` lanes (8, 16 or 32) that holds a head.
-__device__ __forceinline__ float head_sum(float v, int width) {
-    if (width >= 32) v += __shfl_xor_sync(0xffffffffu, v, 16);
-    if (width >= 16) v += __shfl_xor_sync(0xffffffffu, v, 8);
-    v += __shfl_xor_sync(0xffffffffu, v, 4);
-    v += __shfl_xor_sync(0xffffffffu, v, 2);
-    return v + __shfl_xor_sync(0xffffffffu, v, 1);
-}
-
-// (a, b) -> (a cos - b sin, b cos + a sin) for every pair of a chunk; cs: the token's table.  All lanes of a warp call it.
-template <bool HALVES>
-__device__ __forceinline__ void turn_chunk(float* v, const float2* cs, const HeadRowsParams& p, int c, int chunks) {
-    if constexpr (!HALVES) {
-        const float4* q = reinterpret_cast<const float4*>(cs) + c;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float4 t = q[i * chunks];
-            const float a = v[4 * i], b = v[4 * i + 1], a2 = v[4 * i + 2], b2 = v[4 * i + 3];
-            v[4 * i] = a * t.x - b * t.y;
-            v[4 * i + 1] = b * t.x + a * t.y;
-            v[4 * i + 2] = a2 * t.z - b2 * t.w;
-            v[4 * i + 3] = b2 * t.z + a2 * t.w;
-        }
-    } else {
-        const int half = p.n_pairs >> 3;                    // chunks of the first half
-        const bool low = c < half, high = !low && c < 2 * half;
-        const int lane = threadIdx.x & 31, other = low ? lane + half : (high ? lane - half : lane);
-        const float4* q = reinterpret_cast<const float4*>(cs) + (low ? c : (high ? c - half : 0));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float x = __shfl_sync(0xffffffffu, v[2 * i], other), y = __shfl_sync(0xffffffffu, v[2 * i + 1], other);
-            const float4 t = q[i * half];
-            if (low | high) {
-                const float s0 = low ? -t.y : t.y, s1 = low ? -t.w : t.w;
-                v[2 * i] = v[2 * i] * t.x + x * s0;
-                v[2 * i + 1] = v[2 * i + 1] * t.z + y * s1;
-            }
-        }
+// Gains of q and k [2][head_dim] (ones where there are none).
+__device__ __forceinline__ void fill_gains(const HeadRowsParams& p, float* gains) {
+    for (int i = threadIdx.x; i < 2 * p.head_dim; i += blockDim.x) {
+        const int w = i >= p.head_dim;
+        gains[i] = p.weight[w] ? p.weight[w][i - w * p.head_dim] : 1.0f;
     }
 }
 
-__device__ __forceinline__ void load_gains(const float* w, int c, bool active, float* g) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = w && active ? w[8 * c + i] : 1.0f;
+// Sum over the group of `width` lanes (4, 8 or 16) that holds a head.
+__device__ __forceinline__ float head_sum(float v, int width) {
+    if (width >= 16) v += __shfl_xor_sync(0xffffffffu, v, 8);
+    if (width >= 8) v += __shfl_xor_sync(0xffffffffu, v, 4);
+    v += __shfl_xor_sync(0xffffffffu, v, 2);
+    return v + __shfl_xor_sync(0xffffffffu, v, 1);
+}
+__device__ __forceinline__ float warp_sum(float v) { return head_sum(v + __shfl_xor_sync(0xffffffffu, v, 16), 16); }
+
+// Where unit u's two pieces of eight lie in a head.
+struct Pieces {
+    int lo, hi;
+    bool turns;     // (half pairs: a unit behind the rotated part does not turn)
+};
+template <bool HALVES>
+__device__ __forceinline__ Pieces pieces_of(const HeadRowsParams& p, int u) {
+    if (!HALVES) return {8 * u, p.head_dim / 2 + 8 * u, p.n_axes > 0};
+    const int units = p.n_pairs / 8;
+    if (u < units) return {8 * u, p.n_pairs + 8 * u, p.n_axes > 0};
+    const int at = 2 * p.n_pairs + 8 * (u - units);
+    return {at, at + p.head_dim / 2 - p.n_pairs, false};
 }
 
-// Element form (rows without 16-byte alignment, head_dim not a multiple of 8): a warp holds a head, unit u of it is pair u
-// for u < n_pairs and one unrotated element behind; up to 255 units, eight to a lane.
+// (a, b) -> (a cos - b sin, b cos + a sin) for the eight pairs of a unit; words: the token's table from the unit's word on.
+template <bool HALVES>
+__device__ __forceinline__ void turn(float* lo, float* hi, const float4* words, int units) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 t = words[i * units];
+        if (HALVES) {
+            const float a = lo[2 * i], b = hi[2 * i], a2 = lo[2 * i + 1], b2 = hi[2 * i + 1];
+            lo[2 * i] = a * t.x - b * t.y;
+            hi[2 * i] = b * t.x + a * t.y;
+            lo[2 * i + 1] = a2 * t.z - b2 * t.w;
+            hi[2 * i + 1] = b2 * t.z + a2 * t.w;
+        } else {
+            float* v = i < 2 ? lo + 4 * i : hi + 4 * (i - 2);
+            const float a = v[0], b = v[1], a2 = v[2], b2 = v[3];
+            v[0] = a * t.x - b * t.y;
+            v[1] = b * t.x + a * t.y;
+            v[2] = a2 * t.z - b2 * t.w;
+            v[3] = b2 * t.z + a2 * t.w;
+        }
+    }
+}
+__device__ __forceinline__ void load_eight(const float* g, float* v) {
+    const float4 a = reinterpret_cast<const float4*>(g)[0], b = reinterpret_cast<const float4*>(g)[1];
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
+// Whether a call's rows can be worked off in units; `width`: lanes of a head.
+inline bool in_units(const HeadRowsParams& p, bool vec) {
+    return vec && p.head_dim % 16 == 0 && (!p.halves || p.n_pairs % 8 == 0);
+}
+inline int lanes_of_head(const HeadRowsParams& p) { return p.head_dim <= 64 ? 4 : (p.head_dim <= 128 ? 8 : 16); }
+
+// Element form (rows without 16-byte alignment, other head_dim): a warp holds a head, unit u of it is pair u for
+// u < n_pairs and one unrotated element behind; up to 255 units, eight to a lane.
 constexpr int kUnits = 8;
 __device__ __forceinline__ int unit_first(int u, const HeadRowsParams& p) {
     return u >= p.n_pairs ? p.n_pairs + u : (p.halves ? u : 2 * u);

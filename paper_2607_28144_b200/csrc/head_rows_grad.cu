@@ -11,7 +11,6 @@
 namespace regenvc {
 namespace {
 
-constexpr int kBatch = 2;
 constexpr int kMaxTokens = 16;
 
 template <typename T>
@@ -29,99 +28,111 @@ __device__ __forceinline__ Vector<T> locate(const HeadRowsParams& p, int token, 
 }
 
 template <typename T, bool HALVES>
-__global__ void __launch_bounds__(kHeadThreads) head_rows_grad_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
-    extern __shared__ float4 table_raw[];
-    float2* table = reinterpret_cast<float2*>(table_raw);
+__global__ void __launch_bounds__(kHeadThreads, 2) head_rows_grad_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
+    extern __shared__ float4 shared_raw[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the join sets itself up and waits for this grid
-    const int pitch = table_pitch(p), chunks = p.head_dim / 8;
-    const int c = threadIdx.x & (width - 1), group = threadIdx.x / width, groups = blockDim.x / width;
-    const bool active = c < chunks;
+    const int pitch = table_pitch(p), units = table_units<HALVES ? kHalfUnits : kAdjacentUnits>(p);
+    float2* table = reinterpret_cast<float2*>(shared_raw);
+    float* gains = reinterpret_cast<float*>(table + p.tokens_per_cta * pitch);
+    const int u = threadIdx.x & (width - 1), group = threadIdx.x / width, groups = blockDim.x / width;
+    const bool active = u < p.head_dim / 16;
+    const Pieces at = pieces_of<HALVES>(p, active ? u : 0);
     const int all = p.heads[0] + p.heads[1];
     const float inv_d = 1.0f / (float)p.head_dim;
     const bool sums = p.partial != nullptr;
-    float gq[8], gk[8], dw[2][8];
-    load_gains(p.weight[0], c, active, gq);
-    load_gains(p.weight[1], c, active, gk);
+    float dw[2][16];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.0f;
+    for (int e = 0; e < 16; ++e) dw[0][e] = dw[1][e] = 0.0f;
 
+    struct Item {
+        Raw8<T> xl, xh, yl, yh;
+        T* to;                                              // nullptr: nothing to do
+        int of, token;
+    };
     for (long long token0 = (long long)blockIdx.x * p.tokens_per_cta; token0 < p.n_tokens; token0 += (long long)gridDim.x * p.tokens_per_cta) {
         const int tokens = (int)min((long long)p.tokens_per_cta, p.n_tokens - token0);
-        if (p.n_axes) {
-            __syncthreads();                                // the last group's table has been read
-            fill_table<HALVES ? kHalfChunks : kAdjacentChunks>(p, table, pitch, (int)token0, tokens, true);
-            __syncthreads();
-        }
         const int total = tokens * all;
-        int t = 0, h = group;
-        while (h >= all) h -= all, ++t;
-        for (int base = 0; base < total; base += groups * kBatch) {   // the same rounds for all lanes
-            Raw8<T> rx[kBatch], ry[kBatch];
-            T* to[kBatch];
-            int of[kBatch], at[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                of[i] = -1;
-                at[i] = 0;
-                rx[i] = ry[i] = Raw8<T>{};
-                if (t < tokens) {
-                    const Vector<T> u = locate<T>(p, (int)token0 + t, h, of[i]);
-                    at[i] = t;
-                    to[i] = u.dx;
-                    if (active) {
-                        rx[i] = load_raw8(u.x + 8 * c);
-                        ry[i] = load_raw8(u.dy + 8 * c);
-                    }
-                    h += groups;
-                    while (h >= all) h -= all, ++t;
+        int t = group / all, h = group - t * all;
+        auto fetch = [&](Item& x) {
+            x.to = nullptr;
+            x.of = x.token = 0;
+            x.xl = x.xh = x.yl = x.yh = Raw8<T>{};
+            if (t < tokens) {
+                const Vector<T> v = locate<T>(p, (int)token0 + t, h, x.of);
+                x.token = t;
+                if (active) {
+                    x.to = v.dx;
+                    x.xl = load_raw8(v.x + at.lo);
+                    x.xh = load_raw8(v.x + at.hi);
+                    x.yl = load_raw8(v.dy + at.lo);
+                    x.yh = load_raw8(v.dy + at.hi);
                 }
+                h += groups;
+                while (h >= all) h -= all, ++t;
             }
+        };
+        Item next;
+        fetch(next);                                        // on its way while the angles are formed
+        __syncthreads();                                    // the last group's table has been read
+        if (p.n_axes) fill_table<HALVES ? kHalfUnits : kAdjacentUnits>(p, table, pitch, (int)token0, tokens, true);
+        if (token0 == (long long)blockIdx.x * p.tokens_per_cta) fill_gains(p, gains);
+        __syncthreads();
+        for (int base = 0; base < total; base += groups) {  // the same rounds for all lanes
+            const Item x = next;
+            if (base + groups < total) fetch(next);
+            float xl[8], xh[8], gl[8], gh[8];
+            widen8(x.xl, xl);
+            widen8(x.xh, xh);
+            widen8(x.yl, gl);
+            widen8(x.yh, gh);
+            if (at.turns) turn<HALVES>(gl, gh, reinterpret_cast<const float4*>(table + x.token * pitch) + u, units);
+            float wl[8], wh[8], sq = 0.0f, hx = 0.0f;
+            load_eight(gains + x.of * p.head_dim + at.lo, wl);
+            load_eight(gains + x.of * p.head_dim + at.hi, wh);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                float x[8], g[8];
-                widen8(rx[i], x);
-                widen8(ry[i], g);
-                if (p.n_axes) turn_chunk<HALVES>(g, table + at[i] * pitch, p, active ? c : 0, chunks);
-                if (!active) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) g[e] = 0.0f;
-                }
-                float sq = 0.0f, hx = 0.0f, hw[8];
+            for (int e = 0; e < 8; ++e) {
+                wl[e] *= gl[e];
+                wh[e] *= gh[e];
+                sq += xl[e] * xl[e] + xh[e] * xh[e];
+                hx += wl[e] * xl[e] + wh[e] * xh[e];
+            }
+            sq = head_sum(sq, width);
+            hx = head_sum(hx, width);
+            const float r = rsqrtf(sq * inv_d + p.eps);
+            const float m = hx * inv_d * r;                 // mean(g w n)
+            if (x.to) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    hw[e] = g[e] * (of[i] == 1 ? gk[e] : gq[e]);
-                    sq += x[e] * x[e];
-                    hx += hw[e] * x[e];
+                    xl[e] *= r, xh[e] *= r;                 // n
+                    wl[e] = r * (wl[e] - xl[e] * m);
+                    wh[e] = r * (wh[e] - xh[e] * m);
                 }
-                sq = head_sum(sq, width);
-                hx = head_sum(hx, width);
-                const float r = rsqrtf(sq * inv_d + p.eps);
-                const float m = hx * inv_d * r * r;         // x m is n mean(g w n)
-                if (of[i] >= 0 && active) {
-                    float o[8];
+                store8(x.to + at.lo, wl);
+                store8(x.to + at.hi, wh);
+                if (sums) {
+                    if (x.of == 0) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        o[e] = r * (hw[e] - x[e] * m);
-                        const float s = g[e] * x[e] * r;
-                        if (of[i]) dw[1][e] += s;
-                        else dw[0][e] += s;
+                        for (int e = 0; e < 8; ++e) dw[0][e] += gl[e] * xl[e], dw[0][8 + e] += gh[e] * xh[e];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dw[1][e] += gl[e] * xl[e], dw[1][8 + e] += gh[e] * xh[e];
                     }
-                    store8(to[i] + 8 * c, o);
                 }
             }
         }
     }
     if (!sums) return;
-    // the block's sums: lanes of one warp that hold the same chunk by shuffles, warps in turn through shared memory
+    // the block's sums: lanes of one warp that hold the same unit by shuffles, warps in turn through shared memory
     __shared__ float part[kHeadThreads / 32][2][kRopeMaxPairs * 2];
 #pragma unroll
     for (int w = 0; w < 2; ++w)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 16; ++e) {
             float s = dw[w][e];
-            if (width <= 16) s += __shfl_xor_sync(0xffffffffu, s, 16);
+            s += __shfl_xor_sync(0xffffffffu, s, 16);
             if (width <= 8) s += __shfl_xor_sync(0xffffffffu, s, 8);
-            if ((threadIdx.x & 31) < width && active) part[threadIdx.x >> 5][w][8 * c + e] = s;
+            if (width <= 4) s += __shfl_xor_sync(0xffffffffu, s, 4);
+            if ((threadIdx.x & 31) < width && active) part[threadIdx.x >> 5][w][(e < 8 ? at.lo : at.hi - 8) + e] = s;
         }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * p.head_dim; i += blockDim.x) {
@@ -178,8 +189,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_rows_grad_element_kernel(co
                 }
                 hx += ga[k] * (gain ? gain[first] : 1.0f) * xa[k];
             }
-            sq = head_sum(sq, 32) / (float)p.head_dim;
-            hx = head_sum(hx, 32) / (float)p.head_dim;
+            sq = warp_sum(sq) / (float)p.head_dim;
+            hx = warp_sum(hx) / (float)p.head_dim;
             const float r = rsqrtf(sq + p.eps), m = hx * r * r;
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
@@ -243,9 +254,9 @@ cudaError_t plan_grad(K kernel, HeadRowsParams& p, int groups, int sm_count, int
     const int all = p.heads[0] + p.heads[1];
     int tokens = 8 * groups / all;
     if (tokens > kMaxTokens) tokens = kMaxTokens;
-    const size_t per_token = (size_t)table_pitch(p) * sizeof(float2);
+    const size_t per_token = (size_t)table_pitch(p) * sizeof(float2), gains = 2 * (size_t)p.head_dim * sizeof(float);
     int per_sm = 1;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, (tokens < 1 ? 1 : tokens) * per_token);
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, (tokens < 1 ? 1 : tokens) * per_token + gains);
     if (e != cudaSuccess) return e;
     long long room = (long long)(per_sm > 0 ? per_sm : 1) * sm_count;
     if (room > kHeadGradMaxBlocks) room = kHeadGradMaxBlocks;
@@ -255,20 +266,20 @@ cudaError_t plan_grad(K kernel, HeadRowsParams& p, int groups, int sm_count, int
     p.tokens_per_cta = tokens;
     const long long rounds = ((long long)p.n_tokens + tokens - 1) / tokens;
     *blocks = (int)(rounds < room ? rounds : room);
-    *smem = tokens * per_token;
+    *smem = tokens * per_token + gains;
     return cudaSuccess;
 }
 
 template <typename T>
 cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, int* blocks, cudaStream_t stream) {
     size_t smem = 0;
-    if (!vec || p.head_dim % 8 != 0 || (p.halves && p.n_pairs % 8 != 0)) {
+    if (!in_units(p, vec)) {
         const cudaError_t e = plan_grad(head_rows_grad_element_kernel<T>, p, kHeadThreads / 32, sm_count, blocks, &smem);
         if (e != cudaSuccess) return e;
         head_rows_grad_element_kernel<T><<<*blocks, kHeadThreads, smem, stream>>>(p);
         return cudaGetLastError();
     }
-    const int width = p.head_dim <= 64 ? 8 : (p.head_dim <= 128 ? 16 : 32);
+    const int width = lanes_of_head(p);
     auto kernel = p.halves ? head_rows_grad_kernel<T, true> : head_rows_grad_kernel<T, false>;
     const cudaError_t e = plan_grad(kernel, p, kHeadThreads / width, sm_count, blocks, &smem);
     if (e != cudaSuccess) return e;
