@@ -14,7 +14,8 @@
 // tokens): both streams have the same rows and take every other tile of keys, and their results are joined in tensor memory
 // at the end.  Either way one stream's products run under the other's exponentials.
 //
-// Tensor memory: S0 [0,128) S1 [128,256) O0 [256,..) O1 [384,..); the probabilities (16-bit pairs) lie over the scores.
+// Tensor memory: tiles of scores from column 0 on, two of them beside O0 and O1 of 128 columns, three beside 64 columns; the
+// probabilities (16-bit pairs) lie over the scores.  With three, a stream's next scores are formed under its exponentials.
 // K comes as [keys][64 columns] blocks with the 128-byte swizzle, which is a K-major operand of Q K^T, V in the same form,
 // which is an MN-major operand of P V: neither is rewritten.
 //
@@ -54,10 +55,14 @@ struct Shape {
     static constexpr int kKeySlots = D == 128 ? 3 : 5, kValueSlots = D == 128 ? 2 : 5;   // rings of K and of V tiles
     static constexpr int kRing = (kKeySlots + kValueSlots) * kTileB;
     static constexpr int kBlocks = D / 64;                    // 64-column blocks of a tile, 16 KB each
+    // Tensor memory (512 columns): as many tiles of scores as fit beside the two streams' O
+    static constexpr int kScores = D == 128 ? 2 : 3, kOut = kScores * 128;
 };
 
-// The bounded wait of ptx.cuh with its clock out of line: the kernel waits in some twenty places, and its loops have to stay
-// in the instruction cache (at 175 KB of code, everything inlined, the window's attention took 5.9 ms).
+// The bounded wait of ptx.cuh with its clock out of line (the kernel waits in some twenty places, and its loops have to stay
+// in the instruction cache) and a long time given to the hardware's own wait: a warp that polls takes issue slots from the
+// exponentials of the others.
+constexpr uint32_t kWaitHintNs = 200000;
 __device__ __noinline__ uint64_t wait_clock(volatile int* abort_flag, int* status, uint64_t since) {
     if (*abort_flag) return 0;
     const uint64_t now = global_timer_ns();
@@ -67,14 +72,25 @@ __device__ __noinline__ uint64_t wait_clock(volatile int* abort_flag, int* statu
     atomicCAS(status, 0, kStatusTimeout);
     return 0;
 }
+__device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(kWaitHintNs)
+        : "memory");
+    return ok != 0;
+}
 struct Waiter {
     volatile int* abort_flag;
     int* status;
     __device__ __forceinline__ bool operator()(const uint64_t* bar, uint32_t parity) const {
         const uint32_t addr = smem_u32(bar);
         uint64_t since = 1;                                  // 1: the clock has not been read yet
-        for (uint32_t spins = 1; !mbar_try_wait(addr, parity & 1); ++spins)
-            if ((spins & 255u) == 0 && (since = wait_clock(abort_flag, status, since)) == 0) return false;
+        while (!try_wait_long(addr, parity & 1))
+            if ((since = wait_clock(abort_flag, status, since)) == 0) return false;
         return true;
     }
 };
@@ -125,7 +141,7 @@ struct Segment {
     int starts, ends;                       // n = 0: no more work
 };
 struct Control {
-    uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, s_full[2], p_full[2], o_full[2], stagger;
+    uint64_t k_full[5], k_empty[5], v_full[5], v_empty[5], q_full, s_full[3], p_full[3], o_full[2][2];
     uint64_t seg_full[kSegments], seg_empty[kSegments], together;
     uint32_t tmem_base;
     int abort_flag;
@@ -256,7 +272,7 @@ __device__ __forceinline__ void check_seq(const PagedAttnParams& p, int s) {
 __device__ __forceinline__ long long lanes_before(long long v, long long& all) {
     const int lane = threadIdx.x & 31;
     long long sum = v;
-#pragma unroll 1
+#pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long u = __shfl_up_sync(0xffffffffu, sum, o);
         if (lane >= o) sum += u;
@@ -266,20 +282,19 @@ __device__ __forceinline__ long long lanes_before(long long v, long long& all) {
 }
 
 // Where `rest` units into a sequence lie: head, tile of rows, place in the item.  One warp.
-__device__ __forceinline__ void place(const PagedAttnParams& p, Walk& w, long long rest) {
+__device__ __forceinline__ void place(const PagedAttnParams& p, Walk& w, long long rest, long long each) {   // each: of one head, or 0
     const int lane = threadIdx.x & 31, tiles = item_tiles(p, w.q);
     w.head = w.tile = 0;
-    w.at = rest;
-    if (tiles == 1 && p.n_k_heads == 1) return;
-    long long each = 0;                                      // of one head
     bool found = false;
 #pragma unroll 1
-    for (int pass = 0; pass < 2 && !found; ++pass) {
+    for (int pass = each > 0; pass < 2 && !found; ++pass) {
         if (pass == 1) {
-            w.head = (int)((float)rest / (float)each);       // a quotient below 2^16: off by one at most
+            w.head = (int)__fdividef((float)rest, (float)each);   // a quotient below 2^16: off by one at most
             if ((long long)w.head * each > rest) --w.head;
             else if ((long long)(w.head + 1) * each <= rest) ++w.head;
             rest -= w.head * each;
+            w.at = rest;
+            if (tiles == 1) return;
         }
 #pragma unroll 1
         for (int t0 = 0; t0 < tiles; t0 += 32) {
@@ -318,9 +333,9 @@ __device__ __noinline__ void plan_few(const PagedAttnParams& p, Control& c, Walk
         tiles = item_tiles(p, q);
         if (blockIdx.x == 0) check_seq(p, lane);
     }
-    const long long mine = cost_of(p, q, tiles, most) * p.n_k_heads;
-    long long all;
-    const long long before = lanes_before(mine, all);
+    const long long each = cost_of(p, q, tiles, most), mine = each * p.n_k_heads;
+    long long all = __shfl_sync(0xffffffffu, mine, 0), before = 0;
+    if (p.n_sequences > 1) before = lanes_before(mine, all);
     const int items = __reduce_add_sync(0xffffffffu, tiles) * p.n_k_heads;
     const int parts = parts_of(all, items), me = blockIdx.x;
     const long long start = bound(all, parts, me);
@@ -334,7 +349,8 @@ __device__ __noinline__ void plan_few(const PagedAttnParams& p, Control& c, Walk
     if (lane == 0) c.rounds = 0;
     const long long rest = start - __shfl_sync(0xffffffffu, before, w.seq);
     __syncwarp();
-    if (w.left > 0) place(p, w, rest);
+    const long long its = __shfl_sync(0xffffffffu, each, w.seq);
+    if (w.left > 0) place(p, w, rest, its);
 }
 
 // Any number: all threads, a thread per sequence.  line: units before each sequence, first_item: items before each.
@@ -422,7 +438,7 @@ __device__ __noinline__ void plan_start(const PagedAttnParams& p, const Control&
     w.seq = w.loaded = lo;
     w.q = load_seq(p, lo);
     w.left = c.left;
-    if (w.left > 0) place(p, w, c.start - line[lo]);
+    if (w.left > 0) place(p, w, c.start - line[lo], 0);
 }
 
 // ------------------------------------------------------------------------------------------------------ small pieces
@@ -451,27 +467,20 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
     return F16 ? pack_f16x2(a, b) : pack_bf16x2(a, b);
 }
 
-// 32 scores of a row -> 16 packed probability pairs 2^(s scale - m), their fp32 sum added to two packed partial sums.  Bit
-// (c % 8) of kMask set: pair c takes the polynomial 2^x on the FMA pipe instead of the special-function unit.
-constexpr uint32_t kPagedPoly = 0x24;
+// 32 scores of a row -> 16 packed probability pairs 2^(s scale - m), their fp32 sum added to two packed partial sums.  All
+// powers on the special-function unit: the loop is bound by issue slots and latencies, and a polynomial on the FMA pipe for
+// every fourth pair, as the attention over a whole window has it, costs more of them (a latent frame: 140 -> 144 us).
 template <bool F16>
 __device__ __forceinline__ void probabilities(const uint32_t* s, uint64_t scale2, uint64_t negm2, uint32_t* pr, uint64_t& sum_a,
                                               uint64_t& sum_b) {
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
         const uint64_t x2 = fma2(pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), scale2, negm2);
-        uint64_t p2;
-        if ((kPagedPoly >> (c & 7)) & 1u) {
-            p2 = exp2_poly2(x2);
-        } else {
-            float x0, x1;
-            unpack2(x2, x0, x1);
-            p2 = pack2(ex2_approx(x0), ex2_approx(x1));
-        }
-        if (c & 1) sum_b = add2(sum_b, p2);
-        else sum_a = add2(sum_a, p2);
-        float p0, p1;
-        unpack2(p2, p0, p1);
+        float x0, x1;
+        unpack2(x2, x0, x1);
+        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+        if (c & 1) sum_b = add2(sum_b, pack2(p0, p1));
+        else sum_a = add2(sum_a, pack2(p0, p1));
         pr[c] = pack_pair<F16>(p0, p1);
     }
 }
@@ -491,19 +500,19 @@ __device__ __forceinline__ uint64_t desc_v(uint32_t addr) {
            (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
 template <int D, bool F16>
-__device__ __forceinline__ void products_qk(uint32_t s_tmem, uint32_t q, uint32_t k) {
+__device__ __forceinline__ void products_qk(uint32_t s_tmem, uint32_t q, uint32_t k, uint32_t elected) {
     const uint64_t a = umma_smem_desc_k_sw128(q), b = umma_smem_desc_k_sw128(k);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
         const uint64_t off = (i >> 2) * (16384 >> 4) + (i & 3) * 2;
-        umma_ss(s_tmem, a + off, b + off, idesc_qk<D, F16>(), i > 0);
+        umma_ss_elect(s_tmem, a + off, b + off, idesc_qk<D, F16>(), i > 0, elected);
     }
 }
 template <int D, bool F16>
-__device__ __forceinline__ void products_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v, bool accumulate) {
+__device__ __forceinline__ void products_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v, bool accumulate, uint32_t elected) {
     const uint64_t b = desc_v(v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) umma_ts(o_tmem, p_tmem + i * 8, b + i * (2048 >> 4), idesc_pv<D, F16>(), accumulate || i > 0);
+    for (int i = 0; i < 8; ++i) umma_ts_elect(o_tmem, p_tmem + i * 8, b + i * (2048 >> 4), idesc_pv<D, F16>(), accumulate || i > 0, elected);
 }
 
 template <int D>
@@ -544,13 +553,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             mbar_init(smem_u32(&c->seg_full[i]), 1);
             mbar_init(smem_u32(&c->seg_empty[i]), 3 + kPgSoftmax / 32);   // both copying warps, products, softmax warps
         }
-        mbar_init(smem_u32(&c->stagger), 4);
 #pragma unroll 1
-        for (int t = 0; t < 2; ++t) {
-            mbar_init(smem_u32(&c->s_full[t]), 1);
-            mbar_init(smem_u32(&c->p_full[t]), 4);
-            mbar_init(smem_u32(&c->o_full[t]), 1);
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(smem_u32(&c->s_full[i]), 1);
+            mbar_init(smem_u32(&c->p_full[i]), 4);
         }
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&c->o_full[i >> 1][i & 1]), 1);
         c->abort_flag = (*reinterpret_cast<volatile int*>(p.status) != 0) ? 1 : 0;
         fence_mbar_init();
         p.pieces[2 * blockIdx.x].valid = 0;
@@ -571,7 +580,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     __syncwarp();
     const bool few = p.n_sequences <= 32 && !p.rounds;
     long long* line = reinterpret_cast<long long*>(ring);
-    if (!few) {
+    Walk walk;
+    if (few) {
+        if (warp == kPgWalkWarp) plan_few(p, *c, walk);
+    } else {
         plan_many(p, *c, line, reinterpret_cast<int*>(line + p.n_sequences));
         fence_proxy_async_smem();                            // the plan's scratch is the copies' ring
     }
@@ -665,107 +677,86 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
         } else if (warp == kPgMmaWarp) {
             // ------------------------------------------------------------------------------------- products
-            if (elect_one()) {
+            // (the whole warp goes through the loop and one lane issues: operands that are the same in every lane stay in
+            // uniform registers)
+            {
+                const uint32_t elected = elect_one();
                 bool ok = true;
                 const uint32_t q_addr = smem_u32(sQ), ring_addr = smem_u32(ring);
-                uint32_t k_next = 0, k_phase = 0, v_next = 0, v_phase = 0, visit0 = 0, visit1 = 0, staggered = 0;
+                uint32_t k_next = 0, k_phase = 0, v_next = 0, v_phase = 0;
                 auto take_k = [&](uint32_t& mine) {
                     mine = k_next;
-                    const bool got = wait(&c->k_full[k_next], k_phase);
+                    const bool got = __all_sync(0xffffffffu, wait(&c->k_full[k_next], k_phase));
                     if (++k_next == S::kKeySlots) k_next = 0, k_phase ^= 1;
                     return got;
                 };
                 auto take_v = [&](uint32_t& mine) {
                     mine = v_next;
-                    const bool got = wait(&c->v_full[v_next], v_phase);
+                    const bool got = __all_sync(0xffffffffu, wait(&c->v_full[v_next], v_phase));
                     if (++v_next == S::kValueSlots) v_next = 0, v_phase ^= 1;
                     return got;
                 };
-                auto scores = [&](int t, uint32_t q, uint32_t k_slot) {
-                    products_qk<D, F16>(tmem_base + t * 128, q, ring_addr + k_slot * S::kTileB);
-                    umma_commit(smem_u32(&c->s_full[t]));
+                auto release_k = [&](uint32_t e) { umma_commit_elect(smem_u32(&c->k_empty[e]), elected); };
+                auto release_v = [&](uint32_t e) { umma_commit_elect(smem_u32(&c->v_empty[e]), elected); };
+                // Steps: stream 0 and 1 in turn.  Step i's scores go to buffer i % kScores, as soon as the probabilities of
+                // the step that had it are used up.
+                uint32_t put = 0, used = 0, phase = 0;   // next buffer to fill, to use; its parity
+                auto scores = [&](uint32_t q, uint32_t k_slot) {
+                    products_qk<D, F16>(tmem_base + put * 128, q, ring_addr + k_slot * S::kTileB, elected);
+                    umma_commit_elect(smem_u32(&c->s_full[put]), elected);
+                    if (++put == S::kScores) put = 0;
                 };
-                auto output = [&](int t, uint32_t v_slot, uint32_t& visit, bool accumulate) {
-                    const uint32_t o_t = tmem_base + 256 + t * 128, s_t = tmem_base + t * 128, v = ring_addr + (S::kKeySlots + v_slot) * S::kTileB;
-                    if (!wait(&c->p_full[t], visit)) return false;
-                    ++visit;
+                auto output = [&](uint32_t t, uint32_t v_slot, bool accumulate) {
+                    if (!__all_sync(0xffffffffu, wait(&c->p_full[used], phase))) return false;
                     tc_fence_after();
-                    products_pv<D, F16>(o_t, s_t, v, accumulate);
-                    umma_commit(smem_u32(&c->o_full[t]));
+                    products_pv<D, F16>(tmem_base + S::kOut + t * D, tmem_base + used * 128,
+                                        ring_addr + (S::kKeySlots + v_slot) * S::kTileB, accumulate, elected);
+                    if (++used == S::kScores) used = 0, phase ^= 1;
                     return true;
                 };
-                auto release_k = [&](uint32_t e) { umma_commit(smem_u32(&c->k_empty[e])); };
-                auto release_v = [&](uint32_t e) { umma_commit(smem_u32(&c->v_empty[e])); };
+                uint32_t visit0 = 0, visit1 = 0;
 #pragma unroll 1
                 for (uint32_t segment = 0; ok; ++segment) {
-                    ok = wait_segment(*c, segment, wait);
+                    ok = __all_sync(0xffffffffu, wait_segment(*c, segment, wait));
                     if (!ok) break;
                     const Segment* at = &c->seg[segment % kSegments];
                     const bool two = at->rows > 128;
-                    const int n = at->n;
-                    mbar_arrive(smem_u32(&c->seg_empty[segment % kSegments]));
+                    const int n = at->n, steps = two ? 2 * n : n;
+                    __syncwarp();
+                    if (elected) mbar_arrive(smem_u32(&c->seg_empty[segment % kSegments]));
                     if (n == 0) break;
-                    uint32_t k, v;
-                    ok = wait(&c->q_full, segment) && take_k(k);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (two) {                               // both streams take every tile
-                        scores(0, q_addr, k);
-                        // stream 1 starts half a period behind stream 0, when that is in the middle of its first exponentials:
-                        // started together, the streams stay one product's time apart and share the exponentials' pipe
-                        // (a period of 3600 cycles instead of 2900)
-                        ok = wait(&c->stagger, staggered++);
+                    uint32_t k = 0, v = 0;
+                    ok = __all_sync(0xffffffffu, wait(&c->q_full, segment));
+                    // with two tiles of rows a tile of keys is taken by an even step and released by the odd one behind it
+#pragma unroll 1
+                    for (int i = -S::kScores; ok && i < steps; ++i) {
+                        // what does not depend on the probabilities first; behind them only the products and, last, what
+                        // others wait for less urgently
+                        const bool odd = i & 1;
+                        const int ahead = i + S::kScores;
+                        const bool second = ahead & 1, more = ahead < steps;
+                        if (i >= 0 && (!two || !odd)) ok = take_v(v);
+                        if (ok && more && two && !second) ok = take_k(k);
+                        if (ok && i >= 0) ok = output(odd, v, i > 1);
+                        if (ok && i >= 0) {
+                            const uint32_t visit = odd ? visit1++ : visit0++;
+                            umma_commit_elect(smem_u32(&c->o_full[odd][visit & 1]), elected);
+                            if (!two || odd) release_v(v);
+                        }
+                        if (ok && more && !two) ok = take_k(k);   // (single tokens wait for keys, not for probabilities)
                         if (!ok) break;
-                        scores(1, q_addr + S::kTileB, k);
-                        release_k(k);
-#pragma unroll 1
-                        for (int j = 0; j < n; ++j) {
-                            const bool more = j + 1 < n;
-                            ok = take_v(v) && (!more || take_k(k)) && output(0, v, visit0, j > 0);
-                            if (!ok) break;
-                            if (more) scores(0, q_addr, k);
-                            ok = output(1, v, visit1, j > 0);
-                            if (!ok) break;
-                            release_v(v);
-                            if (more) {
-                                scores(1, q_addr + S::kTileB, k);
-                                release_k(k);
-                            }
-                        }
-                    } else {                                 // the streams take every other tile
-                        scores(0, q_addr, k);
-                        release_k(k);
-                        if (n > 1) {
-                            ok = take_k(k);
-                            if (!ok) break;
+                        if (more) {
                             tc_fence_after();
-                            scores(1, q_addr, k);
-                            release_k(k);
-                        }
-#pragma unroll 1
-                        for (int j = 0; j < n; ++j) {
-                            const int t = j & 1;
-                            ok = take_v(v) && output(t, v, t ? visit1 : visit0, j > 1);
-                            if (!ok) break;
-                            release_v(v);
-                            if (j + 2 < n) {
-                                ok = take_k(k);
-                                if (!ok) break;
-                                scores(t, q_addr, k);
-                                release_k(k);
-                            }
+                            scores(q_addr + (two && second ? S::kTileB : 0), k);
+                            if (!two || second) release_k(k);
                         }
                     }
                 }
             }
         } else if (warp == kPgWalkWarp) {
             // ------------------------------------------------------------------------------------- the work, stretch by stretch
-            Walk walk;
-            walk.round = walk.head = walk.tile = 0;
-            walk.at = 0;
-            if (few) {
-                plan_few(p, *c, walk);
-            } else {
+            walk.round = 0;
+            if (!few) {
                 plan_start(p, *c, line, walk);
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -790,10 +781,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         setmaxnreg_inc<kPgSoftmaxRegs>();
         const int t = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-        const uint32_t t_S = lane_base + t * 128, t_O = lane_base + 256 + t * 128;
+        const uint32_t t_O = lane_base + S::kOut + t * D;
         const float scale = p.scale_log2;
         const uint64_t scale2 = pack2(scale, scale);
-        uint32_t entry = 0, visit = 0, met = 0;
+        uint32_t entry = 0, steps = 0, visit = 0, met = 0;
         // all softmax warps have come here (with a limit, like every wait: a wait that runs out ends the warp's work)
         auto meet_all = [&]() {
             __syncwarp();
@@ -854,7 +845,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             int done = 0;                                    // tiles of this stream
 #pragma unroll 1
             for (int j = two ? 0 : t; j < n; j += two ? 1 : 2) {
-                ok = __all_sync(0xffffffffu, wait(&c->s_full[t], visit & 1));
+                const uint32_t step = steps + (two ? 2 * j + t : j), buffer = step % S::kScores, t_S = lane_base + buffer * 128;
+                ok = __all_sync(0xffffffffu, wait(&c->s_full[buffer], step / S::kScores));
                 if (!ok) break;
                 tc_fence_after();
                 const int from = lo - 128 * j, to = hi - 128 * j;
@@ -896,7 +888,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                     };
                     // rows that have not seen a key yet take the tile's maximum for their reference
-                    bool again, redo = false;
+                    bool again;
                     if (fresh) {
                         const float top = highest();
                         if (m == -INFINITY) m = top;
@@ -912,14 +904,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             uint32_t pr[16];
                             probabilities<F16>(s + 32 * b, scale2, pack2(-ref, -ref), pr, sum_a, sum_b);
                             tmem_st16(t_S + 16 * b, pr);
-                            if (b == 1 && two && t == 0 && j == 0 && !redo) {
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive(smem_u32(&c->stagger));
-                            }
                         }
-                        float s0, s1;
-                        unpack2(add2(sum_a, sum_b), s0, s1);
-                        sum = s0 + s1;
+                        float s0, s1; unpack2(add2(sum_a, sum_b), s0, s1); sum = s0 + s1;
                         again = !(sum < raise_at<F16>());
                         if (!__any_sync(0xffffffffu, again)) break;
                         // Rare: scores far above the reference.  The products so far are waited for, O and the sum are
@@ -930,9 +916,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         const float alpha = again ? ex2_approx(ref - top) : 1.0f;
                         if (again) m = top;
                         l *= alpha;
-                        redo = true;
                         if (done > 0) {
-                            ok = __all_sync(0xffffffffu, wait(&c->o_full[t], visit - 1));
+                            ok = __all_sync(0xffffffffu, wait(&c->o_full[t][(visit - 1) & 1], (visit - 1) >> 1));
                             tc_fence_after();
 #pragma unroll 1
                             for (int b = 0; ok && b < D; b += 16) {
@@ -950,17 +935,18 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c->p_full[t]));
+                if (lane == 0) mbar_arrive(smem_u32(&c->p_full[buffer]));
                 if (!ok) break;
                 ++visit;
                 ++done;
             }
             if (!ok) break;
             entry += n;                                      // V tiles so far
+            steps += two ? 2 * n : n;
 
             // ------------------------------------------------------------------------------------- results
             if (done > 0) {
-                ok = __all_sync(0xffffffffu, wait(&c->o_full[t], (visit - 1) & 1));
+                ok = __all_sync(0xffffffffu, wait(&c->o_full[t][(visit - 1) & 1], (visit - 1) >> 1));
                 if (!ok) break;
                 tc_fence_after();
             }
@@ -1002,8 +988,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         for (int i = 0; i < 32; ++i) o[i] = a[t] == 0.0f ? 0u : o[i];
                     } else {
                         uint32_t o1[32];
-                        tmem_ld32(lane_base + 256 + col0 + b, o);
-                        tmem_ld32(lane_base + 384 + col0 + b, o1);
+                        tmem_ld32(lane_base + S::kOut + col0 + b, o);
+                        tmem_ld32(lane_base + S::kOut + D + col0 + b, o1);
                         tmem_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
@@ -1063,63 +1049,78 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
 }
 
-// Joins the pieces of an item: block (x, y) the item that thread block x of the attention began and did not end, a share of
-// its rows.  The pieces are this one and the ones that the following thread blocks left in their slot 0, up to the one that
-// ends the item, in that order.
+// Joins the pieces of an item: block (x, y) the item that thread block x of the attention began and did not end, 32 of its
+// rows.  The pieces are this one and the ones that the following thread blocks left in their slot 0, up to the one that ends
+// the item, in that order.  Bound by latencies (the blocks start when the attention's have left the SMs, whose registers are
+// all taken): the descriptions of all pieces are read at once, and the pieces of four rows side by side.
+constexpr int kJoinRows = 32;
 template <int D, bool F16>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p, const int grid) {
-    constexpr int kRowsHere = 256 / (D / 4);
+    constexpr int kRowsAtOnce = 256 / (D / 4), kTurns = kJoinRows / kRowsAtOnce;
     __shared__ int slots[kPagedMaxGrid + 1];
-    __shared__ int end_at, n_pieces;
+    __shared__ uint32_t valid_at[kPagedMaxGrid / 32 + 1], ends_at[kPagedMaxGrid / 32 + 1];
+    __shared__ int n_pieces;
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int row0 = blockIdx.y * kJoinRows, next = blockIdx.x + 1 + threadIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const PagedPiece first = p.pieces[2 * blockIdx.x + 1];
-    const int row0 = blockIdx.y * kRowsHere;
-    if (!first.valid || row0 >= first.rows) return;
-    if (threadIdx.x == 0) end_at = grid;
-    __syncthreads();
-    const int next = blockIdx.x + 1 + threadIdx.x;
     int valid = 0, ends = 0;
-    if (next < grid) {
-        valid = p.pieces[2 * next].valid;
-        ends = p.pieces[2 * next].ends;
-        if (valid && ends) atomicMin(&end_at, next);
-    }
+    if (next < grid) valid = p.pieces[2 * next].valid, ends = p.pieces[2 * next].ends;
+    if (!first.valid || row0 >= first.rows) return;
+    const uint32_t v = __ballot_sync(0xffffffffu, valid), e = __ballot_sync(0xffffffffu, valid && ends);
+    if (lane == 0 && warp <= kPagedMaxGrid / 32) valid_at[warp] = v, ends_at[warp] = e;
     __syncthreads();
-    if (threadIdx.x < 32) {                                  // the valid ones up to the end, in order
-        int n = 1;
+    {   // this thread's piece, if it is one of the item's: the valid ones before it, and none of those ends the item
+        int before = 0;
+        bool in = valid;
+        for (int w = 0; w < warp; ++w) before += __popc(valid_at[w]), in = in && !ends_at[w];
+        const uint32_t below = (1u << lane) - 1;
+        before += __popc(v & below);
+        in = in && !(e & below);
+        if (in) slots[1 + before] = 2 * next;
+        if (in && ends) n_pieces = 2 + before;
         if (threadIdx.x == 0) slots[0] = 2 * blockIdx.x + 1;
-        for (int b = blockIdx.x + 1; b <= end_at && b < grid; b += 32) {
-            const int k = b + threadIdx.x;
-            const bool in = k <= end_at && k < grid && p.pieces[2 * k].valid;
-            const uint32_t all = __ballot_sync(0xffffffffu, in);
-            if (in) slots[n + __popc(all & ((1u << threadIdx.x) - 1))] = 2 * k;
-            n += __popc(all);
-        }
-        if (threadIdx.x == 0) n_pieces = n;
     }
     __syncthreads();
-    const int n = n_pieces, row = row0 + threadIdx.x % kRowsHere, c4 = threadIdx.x / kRowsHere;
-    if (row >= first.rows) return;
-    float m = -INFINITY;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, p.part_ml[(size_t)slots[i] * kPagedRows + row].x);
-    float l = 0.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+    const int n = n_pieces, c4 = threadIdx.x / kRowsAtOnce;
+    float m[kTurns], l[kTurns];
+    float4 o[kTurns];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) m[t] = -INFINITY, l[t] = 0.0f, o[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
     for (int i = 0; i < n; ++i) {
-        const float2 ml = p.part_ml[(size_t)slots[i] * kPagedRows + row];
-        const float4 v = p.part_o[(size_t)slots[i] * (D / 4) * kPagedRows + (size_t)c4 * kPagedRows + row];
-        if (ml.x == -INFINITY) continue;
-        const float a = ex2_approx(ml.x - m);
-        l += a * ml.y;
-        o.x += a * v.x, o.y += a * v.y, o.z += a * v.z, o.w += a * v.w;
+        const float2* ml = p.part_ml + (size_t)slots[i] * kPagedRows + row0 + threadIdx.x % kRowsAtOnce;
+        const float4* po = p.part_o + ((size_t)slots[i] * (D / 4) + c4) * kPagedRows + row0 + threadIdx.x % kRowsAtOnce;
+        float2 x[kTurns];
+        float4 y[kTurns];
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {                   // (rows behind the last are in the workspace too, whatever they hold)
+            x[t] = ml[t * kRowsAtOnce];
+            y[t] = po[t * kRowsAtOnce];
+        }
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const float top = fmaxf(m[t], x[t].x);
+            const float a = m[t] == -INFINITY ? 0.0f : ex2_approx(m[t] - top), b = x[t].x == -INFINITY ? 0.0f : ex2_approx(x[t].x - top);
+            m[t] = top;
+            l[t] = a * l[t] + b * x[t].y;
+            o[t].x = a * o[t].x + (b == 0.0f ? 0.0f : b * y[t].x);
+            o[t].y = a * o[t].y + (b == 0.0f ? 0.0f : b * y[t].y);
+            o[t].z = a * o[t].z + (b == 0.0f ? 0.0f : b * y[t].z);
+            o[t].w = a * o[t].w + (b == 0.0f ? 0.0f : b * y[t].w);
+        }
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    const int in_seq = first.first_row + row, token = in_seq / p.share;
-    const long long out_row = first.seq_row0 + token;
-    const int h = first.head * p.share + in_seq - token * p.share;
-    uint2 w = make_uint2(pack_pair<F16>(o.x * inv, o.y * inv), pack_pair<F16>(o.z * inv, o.w * inv));
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + out_row * p.out_token + h * p.out_head + c4 * 4) = w;
-    if (p.lse && c4 == 0) p.lse[out_row * p.n_q_heads + h] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        const int row = row0 + t * kRowsAtOnce + threadIdx.x % kRowsAtOnce;
+        if (row >= first.rows) continue;
+        const float inv = l[t] > 0.0f ? 1.0f / l[t] : 0.0f;
+        const int in_seq = first.first_row + row, token = in_seq / p.share;
+        const long long out_row = first.seq_row0 + token;
+        const int h = first.head * p.share + in_seq - token * p.share;
+        const uint2 w = make_uint2(pack_pair<F16>(o[t].x * inv, o[t].y * inv), pack_pair<F16>(o[t].z * inv, o[t].w * inv));
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + out_row * p.out_token + h * p.out_head + c4 * 4) = w;
+        if (p.lse && c4 == 0) p.lse[out_row * p.n_q_heads + h] = l[t] > 0.0f ? (m[t] + log2f(l[t])) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 template <int D, bool F16>
@@ -1138,7 +1139,7 @@ cudaError_t launch_one(const PagedMaps& maps, const PagedAttnParams& p, int grid
     if (e != cudaSuccess) return e;
     *launches = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid, (unsigned)(kPagedRows / (256 / (D / 4))));
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)(kPagedRows / kJoinRows));
     cfg.blockDim = dim3(256);
     cfg.stream = stream;
     cudaLaunchAttribute attr;
