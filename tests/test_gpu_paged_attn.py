@@ -104,3 +104,160 @@ def test_scores_that_rise_along_the_keys(dtype, new, group):
     out, lse = B.regenvc_paged_attn_forward(*args, group=group, lse=True)
     assert B.regenvc_device_status() == B.OK
     check(c, [new], [keys], out, lse, group, 0)
+
+
+@pytest.mark.parametrize("group,window", [(1, 0), (0, 0), (3, 1)])
+def test_rows_that_see_nothing(group, window):
+    """Sequences with fewer cached tokens than rows, none at all, and none of either."""
+    new, keys = [5, 4, 0, 200, 2], [3, 0, 0, 150, 9]
+    c = make(new, keys, 4, 2, 128, 16, BF, seed=5)
+    out, lse = B.regenvc_paged_attn_forward(*c["args"], group=group, window=window, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, new, keys, out, lse, group, window)
+    assert (out[5:9] == 0).all() and torch.isinf(lse[5:9]).all()
+    if group:
+        assert (out[:2] == 0).all() and torch.isinf(lse[:2]).all()
+
+
+def test_strided_operands_padded_rows_and_a_scale():
+    new, keys = [3, 130], [40, 300]
+    c = make(new, keys, 6, 3, 64, 16, FP, seed=6, pad=7)
+    q, kc, vc, table, lengths, starts = c["args"]
+    rows = torch.randn(140, 12, 64, device=DEV).to(FP)                # a projection's rows: q, k, v side by side
+    rows[:, :6] = q
+    both = torch.full((kc.shape[0], 2, *kc.shape[1:]), math.nan, dtype=FP, device=DEV)   # keys and values in one tensor
+    both[:, 0], both[:, 1] = kc, vc
+    wide = torch.zeros((2, table.shape[1] + 3), dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    out = torch.full((140, 6, 80), 7.0, dtype=FP, device=DEV)
+    lse = torch.full((140, 6), 7.0, device=DEV)
+    B.regenvc_paged_attn_forward(rows[:, :6], both[:, 0], both[:, 1], wide[:, :table.shape[1]], lengths, starts, group=1, scale=0.21,
+                                 out=out[..., :64], lse=lse)
+    assert B.regenvc_device_status() == B.OK
+    check(c, new, keys, out[..., :64], lse, 1, 0, 0.21)
+    assert (out[133:] == 7).all() and (out[..., 64:] == 7).all() and (lse[133:] == 7).all()
+
+
+def test_pages_before_the_window_need_not_exist():
+    new, keys, page = [70, 1], [1000, 513], 32
+    c = make(new, keys, 2, 1, 128, page, BF, seed=7)
+    args = list(c["args"])
+    group, window = 10, 7
+    table = args[3].clone()
+    for s, (m, n) in enumerate(zip(new, keys)):
+        first = max(0, ((n - m) // group - window + 1) * group)       # the first token that any of them sees
+        table[s, :first // page] = -1
+        for t in range(first // page):
+            args[1][c["table"][s, t]] = math.inf
+            args[2][c["table"][s, t]] = math.nan
+        args[1][c["table"][s, first // page], :first % page] = math.nan
+        args[2][c["table"][s, first // page], :first % page] = math.inf
+    args[3] = table
+    out, lse = B.regenvc_paged_attn_forward(*args, group=group, window=window, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, new, keys, out, lse, group, window)
+
+
+@pytest.mark.parametrize("new,keys,hq,hk,d,group,window", [
+    ([3000], [5000], 16, 16, 128, 500, 4),                            # whole items in rounds, then the rest of the line
+    ([2600, 1, 700], [2600, 4000, 9000], 24, 12, 64, 1, 0),
+    ([1] * 40, [700] * 40, 8, 8, 128, 0, 0),                          # more sequences than a warp has lanes
+    ([1] * 3 + [260], [20000, 1, 64, 20000], 2, 1, 128, 1, 0)])       # items cut into many pieces
+def test_splits_of_the_work(new, keys, hq, hk, d, group, window):
+    c = make(new, keys, hq, hk, d, 64, BF, seed=8)
+    out, lse = B.regenvc_paged_attn_forward(*c["args"], group=group, window=window, lse=True)
+    again, lse2 = B.regenvc_paged_attn_forward(*c["args"], group=group, window=window, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, new, keys, out, lse, group, window)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)         # the same split, the same sums
+
+
+def test_a_thousand_sequences():
+    g = torch.Generator().manual_seed(9)
+    keys = torch.randint(1, 60, (1000,), generator=g).tolist()
+    new = torch.randint(0, 3, (1000,), generator=g).tolist()
+    keys = [max(k, n) for k, n in zip(keys, new)]
+    c = make(new, keys, 2, 2, 64, 16, FP, seed=9)
+    out, lse = B.regenvc_paged_attn_forward(*c["args"], group=1, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, new, keys, out, lse, 1, 0)
+
+
+def test_offsets_past_32_bits():
+    """Caches of 2.3 10^9 elements each; the sequence lies at their end."""
+    c = make([2], [130], 8, 8, 128, 16, BF, seed=10)
+    q, kc, vc, table, lengths, starts = c["args"]
+    pages = 140000
+    big_k, big_v = (torch.empty((pages, 16, 8, 128), dtype=BF, device=DEV) for _ in range(2))
+    shift = pages - kc.shape[0]
+    big_k[shift:], big_v[shift:] = kc, vc
+    out, lse = B.regenvc_paged_attn_forward(q, big_k, big_v, torch.where(table < 10 ** 6, table + shift, table), lengths, starts,
+                                            group=1, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, [2], [130], out, lse, 1, 0)
+
+
+def test_contradictions_are_reported_and_nothing_else_is_read():
+    c = make([1, 1], [40, 50], 2, 2, 128, 16, BF, seed=11)
+    args = list(c["args"])
+    bad = args[3].clone()
+    bad[1, 1] = -5
+    B.regenvc_paged_attn_forward(*args[:3], bad, *args[4:], group=1)
+    assert B.regenvc_device_status() == B.ERR_RANGE
+    bad[1, 1] = 10 ** 6
+    B.regenvc_paged_attn_forward(*args[:3], bad, *args[4:], group=1)
+    assert B.regenvc_device_status() == B.ERR_RANGE
+    for lengths, starts in (([40, 10 ** 9], [0, 1, 2]), ([-1, 50], [0, 1, 2]), ([40, 50], [0, 2, 1]), ([40, 50], [0, 1, 900]),
+                            ([40, 50], [-3, 1, 2])):
+        B.regenvc_paged_attn_forward(*args[:4], torch.tensor(lengths, dtype=torch.int32, device=DEV),
+                                     torch.tensor(starts, dtype=torch.int32, device=DEV), group=1)
+        assert B.regenvc_device_status() == B.ERR_RANGE
+    out, lse = B.regenvc_paged_attn_forward(*args, group=1, lse=True)     # and the next call is normal again
+    assert B.regenvc_device_status() == B.OK
+    check(c, [1, 1], [40, 50], out, lse, 1, 0)
+
+
+def test_two_streams_at_once_and_a_graph_that_follows_the_lengths():
+    new, keys = [1, 40, 3], [200, 600, 77]
+    c = make(new, keys, 4, 2, 128, 16, BF, seed=12)
+    args = list(c["args"])
+    want, _ = B.regenvc_paged_attn_forward(*args, group=1)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].append(B.regenvc_paged_attn_forward(*args, group=1)[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for part in outs for o in part)
+    assert B.regenvc_device_status() == B.OK
+    size = B.regenvc_paged_attn_workspace_bytes(4, 2, 128)
+    graphs, results = [], []
+    for _ in range(2):                                                # a workspace each: they may be replayed at a time
+        ws, out = torch.empty(size, dtype=torch.uint8, device=DEV), torch.zeros_like(args[0])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.regenvc_paged_attn_forward(*args, group=1, out=out, workspace=ws)
+        graphs.append((g, ws))
+        results.append(out)
+    for lengths in (keys, [150, 555, 3], [1, 40, 50]):
+        args[4].copy_(torch.tensor(lengths, dtype=torch.int32))
+        torch.cuda.synchronize()
+        for (g, _), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        want, _ = B.regenvc_paged_attn_forward(*args, group=1)
+        assert torch.equal(results[0], want) and torch.equal(results[1], want)
+    assert B.regenvc_device_status() == B.OK
+
+
+def test_nothing_runs_while_a_status_is_set_and_all_does_afterwards():
+    c = make([1], [40], 2, 2, 64, 16, FP, seed=13)
+    B.regenvc_debug_expire_wait(200)
+    B.regenvc_paged_attn_forward(*c["args"])                          # its waits fall through
+    assert B.regenvc_device_status() == B.ERR_TIMEOUT
+    out, lse = B.regenvc_paged_attn_forward(*c["args"], lse=True)
+    assert B.regenvc_device_status() == B.OK
+    check(c, [1], [40], out, lse, 0, 0)

@@ -136,3 +136,86 @@ def test_append(new, keys, hq, hk, d, page, dtype, widths, halves, norm, order):
         qr, qm = head64(q.double(), None if w[0] is None else w[0].double(), pos, widths, 10000.0, halves, False, 1e-6, norm)
         assert ((q_out.double() - qr).abs()[:n] <= forward_bound(qr, qm, dtype, d)[:n]).all()
         assert (q_out[n:] == 7.0).all()
+
+
+def test_in_place_on_views_of_one_tensor():
+    """q, k and v as a projection leaves them; forward, and the gradients over their own operands."""
+    g = torch.Generator().manual_seed(3)
+    for dtype, halves in ((BF, False), (F32, True)):
+        rows = torch.randn(50, 6 + 2 + 2, 128, generator=g).to(dtype).to(DEV)
+        pos = torch.arange(50, dtype=torch.int32, device=DEV).view(1, -1)
+        w = (1 + 0.3 * torch.randn(128, generator=g)).to(DEV)
+        how = dict(q_weight=w, k_weight=w, halves=halves)
+        q, k = rows[:, :6], rows[:, 6:8]
+        want = B.regenvc_qk_norm_rope_forward(q, k, pos, [128], **how)
+        kept = rows.clone()
+        grads = B.regenvc_qk_norm_rope_backward(want[0], want[1], q, k, pos, [128], **how)
+        got = B.regenvc_qk_norm_rope_forward(q, k, pos, [128], q_out=q, k_out=k, **how)
+        assert got[0].data_ptr() == rows.data_ptr()
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(rows[:, 8:], kept[:, 8:])
+        again = B.regenvc_qk_norm_rope_backward(q, k, kept[:, :6], kept[:, 6:8], pos, [128], dq=q, dk=k, **how)
+        assert torch.equal(q, grads["dq"]) and torch.equal(k, grads["dk"]) and torch.equal(rows[:, 8:], kept[:, 8:])
+        assert torch.equal(again["dq_weight"], grads["dq_weight"]) and torch.equal(again["dk_weight"], grads["dk_weight"])
+
+
+def test_values_are_copied_bit_by_bit_and_extremes_stay_in_their_row():
+    v = torch.tensor([0x7FC1, 0x7F80, 0xFF80, 0x0001, 0x8000, 0x7F7F] + [0x3F80] * 122, dtype=torch.int32).to(torch.int16).view(BF)
+    rows = torch.ones(3, 1, 128, dtype=BF, device=DEV)
+    rows[1] = v.to(DEV)
+    kc, vc = (torch.zeros(1, 8, 1, 128, dtype=BF, device=DEV) for _ in range(2))
+    lists = (torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.tensor([5], dtype=torch.int32, device=DEV),
+             torch.tensor([0, 3], dtype=torch.int32, device=DEV))
+    B.regenvc_paged_append(rows, rows, kc, vc, *lists, norm=B.NORM_RMS)
+    assert torch.equal(vc[0, 2:5].view(torch.int16), rows.view(torch.int16))
+    assert (kc[0, 2] == 1).all() and (kc[0, 4] == 1).all() and (kc[0, :2] == 0).all()
+    big = torch.full((2, 1, 128), 3e38, dtype=F32, device=DEV)
+    big[1] = 0
+    out, _ = B.regenvc_qk_norm_rope_forward(big, None)
+    assert (out == 0).all()                                            # past fp32's range, and a row of zeros
+
+
+def test_appending_to_places_that_do_not_exist_is_reported():
+    rows = torch.ones(4, 1, 64, dtype=BF, device=DEV)
+    starts = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV)
+    for lengths, table in (([2, 2], [[0, 1], [-1, 1]]), ([2, 2], [[0, 1], [2, 1]]), ([2, 1], [[0, 0], [1, 0]]), ([2, 17], [[0, 0], [1, 1]])):
+        kc, vc = (torch.zeros(2, 8, 1, 64, dtype=BF, device=DEV) for _ in range(2))
+        B.regenvc_paged_append(rows, rows, kc, vc, torch.tensor(table, dtype=torch.int32, device=DEV),
+                               torch.tensor(lengths, dtype=torch.int32, device=DEV), starts)
+        assert B.regenvc_device_status() == B.ERR_RANGE
+        assert (kc[0, :2] == 1).all() and (kc[0, 2:] == 0).all()       # the other sequence's tokens are there
+    assert B.regenvc_device_status() == B.OK
+
+
+def test_on_another_stream_and_in_a_graph():
+    case = CASES[2]
+    q, k, pos, widths, how = operands(case)
+    want = B.regenvc_qk_norm_rope_forward(q, k, pos, widths, **how)
+    grads = B.regenvc_qk_norm_rope_backward(*want, q, k, pos, widths, **how)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = B.regenvc_qk_norm_rope_forward(q, k, pos, widths, stream=s, **how)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    q2 = q.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = B.regenvc_qk_norm_rope_forward(q2, k, pos, widths, **how)
+        back = B.regenvc_qk_norm_rope_backward(*out, q2, k, pos, widths, **how)
+    for scale in (1.0, 2.0):
+        q2.copy_(scale * q)
+        g.replay()
+        torch.cuda.synchronize()
+        ref = B.regenvc_qk_norm_rope_forward(q2, k, pos, widths, **how)
+        rb = B.regenvc_qk_norm_rope_backward(*ref, q2, k, pos, widths, **how)
+        assert torch.equal(out[0], ref[0]) and all(torch.equal(back[x], rb[x]) for x in rb)
+    assert all(torch.equal(grads[x], B.regenvc_qk_norm_rope_backward(*want, q, k, pos, widths, **how)[x]) for x in grads)
+
+
+def test_offsets_past_32_bits():
+    pages = 140000                                                     # 2.3 10^9 elements
+    kc, vc = (torch.empty((pages, 16, 8, 128), dtype=BF, device=DEV) for _ in range(2))
+    rows = torch.randn(3, 8, 128, device=DEV).to(BF)
+    table = torch.tensor([[pages - 1]], dtype=torch.int32, device=DEV)
+    B.regenvc_paged_append(rows, rows, kc, vc, table, torch.tensor([16], dtype=torch.int32, device=DEV),
+                           torch.tensor([0, 3], dtype=torch.int32, device=DEV))
+    assert torch.equal(kc[-1, 13:], rows) and torch.equal(vc[-1, 13:], rows)
