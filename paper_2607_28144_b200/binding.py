@@ -704,11 +704,19 @@ assert _QKNORM_DESC.size == ctypes.sizeof(QkNormRopeDesc) and _APPEND_DESC.size 
 def _head_strides(t, name: str, dtype, n: int, heads: int, d: int):
     """(token, head) strides of [tokens, heads, head_dim] vectors as the library takes them (0, 0: packed)."""
     if t is None:
-        return 0, 0
+        return _PACKED
     if t.dtype is not dtype or t.shape != (n, heads, d):
         raise TypeError(f"{name} must be {dtype} [{n}, {heads}, {d}]")
-    if t.is_contiguous():
-        return 0, 0
+    return _own_strides(t, name, n, heads, d)
+
+
+_PACKED = (0, 0)
+
+
+def _own_strides(t, name: str, n: int, heads: int, d: int):
+    """The same for an operand that gave type and shape itself."""
+    if t is None or t.is_contiguous():
+        return _PACKED
     token, head, step = t.stride()
     if d > 1 and step != 1:
         raise TypeError(f"{name} must have neighbouring elements of a head")
@@ -724,14 +732,18 @@ def _rotation(positions, widths, n: int):
         if widths is not None and len(widths):
             raise ValueError("widths need positions")
         return 0, (0, 0, 0, 0), False, 0
-    widths = list(widths)
-    if positions.dtype not in (torch.int32, torch.float32) or positions.shape != (len(widths), n) or \
-            (n > 1 and positions.stride(1) != 1) or (len(widths) > 1 and positions.stride(0) < n):
-        raise TypeError(f"positions must be int32 or fp32 [{len(widths)}, {n}] with neighbouring tokens")
-    if not 1 <= len(widths) <= 4:
+    axes, as_float = len(widths), positions.dtype is torch.float32
+    if not (as_float or positions.dtype is torch.int32) or positions.shape != (axes, n):
+        raise TypeError(f"positions must be int32 or fp32 [{axes}, {n}] with neighbouring tokens")
+    if not 1 <= axes <= 4:
         raise RegenvcError(ERR_BAD_SHAPE, status_string(ERR_BAD_SHAPE))
-    return len(widths), (widths + [0, 0, 0])[:4], positions.dtype is torch.float32, \
-        positions.stride(0) if len(widths) > 1 else 0
+    between = 0
+    if not positions.is_contiguous():
+        between, step = positions.stride()
+        if (n > 1 and step != 1) or (axes > 1 and between < n):
+            raise TypeError(f"positions must be int32 or fp32 [{axes}, {n}] with neighbouring tokens")
+        between = between if axes > 1 else 0
+    return axes, (*widths, 0, 0, 0)[:4], as_float, between
 
 
 def _heads_of(q, k):
@@ -754,17 +766,23 @@ def regenvc_qk_norm_rope_forward(q, k, positions=None, widths=None, *, q_weight=
     n, hq, hk, d, dtype = _heads_of(q, k)
     index = _place(q if q is not None else k, k, positions, q_weight, k_weight, q_out, k_out)
     axes, four, as_float, between = _rotation(positions, widths, n)
-    _vector(q_weight, "q_weight", d)
-    _vector(k_weight, "k_weight", d)
+    if q_weight is not None:
+        _vector(q_weight, "q_weight", d)
+    if k_weight is not None:
+        _vector(k_weight, "k_weight", d)
     if (q is None and (q_out is not None or q_weight is not None)) or (k is None and (k_out is not None or k_weight is not None)):
         raise ValueError("a result and gains need their operand")
+    q_strides = k_strides = _PACKED
     if q is not None and q_out is None:
         q_out = _like(q, stream)
+    elif q is not None:
+        q_strides = _head_strides(q_out, "q_out", dtype, n, hq, d)
     if k is not None and k_out is None:
         k_out = _like(k, stream)
+    elif k is not None:
+        k_strides = _head_strides(k_out, "k_out", dtype, n, hk, d)
     desc = _QKNORM_DESC.pack(n, hq, hk, d, TYPES[dtype], axes, *four, rope_theta, bool(halves), bool(whole_ladder), as_float, eps,
-                             between, *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(k, "k", dtype, n, hk, d),
-                             *_head_strides(q_out, "q_out", dtype, n, hq, d), *_head_strides(k_out, "k_out", dtype, n, hk, d),
+                             between, *_own_strides(q, "q", n, hq, d), *_own_strides(k, "k", n, hk, d), *q_strides, *k_strides,
                              0, 0, 0, 0)
     _check(lib().regenvc_qk_norm_rope_forward(desc, _addr(q), _addr(k), _addr(q_weight), _addr(k_weight), _addr(positions),
                                               _addr(q_out), _addr(k_out), _launch_stream(stream, index)))
@@ -854,8 +872,10 @@ def regenvc_paged_append(k, v, k_cache, v_cache, block_table, lengths, row_start
         raise TypeError("k must be [tokens, heads, head_dim]")
     index = _place(k, v, q, k_cache, v_cache, block_table, lengths, row_starts, positions, q_weight, k_weight, q_out)
     axes, four, as_float, between = _rotation(positions, widths, n)
-    _vector(q_weight, "q_weight", d)
-    _vector(k_weight, "k_weight", d)
+    if q_weight is not None:
+        _vector(q_weight, "q_weight", d)
+    if k_weight is not None:
+        _vector(k_weight, "k_weight", d)
     if q is None and (q_out is not None or q_weight is not None):
         raise ValueError("q_out and q_weight need q")
     if norm == NORM_NONE and (q_weight is not None or k_weight is not None):
@@ -864,13 +884,15 @@ def regenvc_paged_append(k, v, k_cache, v_cache, block_table, lengths, row_start
     k_strides, v_strides = _cache(k_cache, "k_cache", dtype), _cache(v_cache, "v_cache", dtype, k_cache)
     if k_cache.shape[2:] != (hk, d):
         raise TypeError(f"the caches must hold {hk} heads of {d}")
+    out_strides = _PACKED
     if q is not None and q_out is None:
         q_out = _like(q, stream)
+    elif q is not None:
+        out_strides = _head_strides(q_out, "q_out", dtype, n, hq, d)
     desc = _APPEND_DESC.pack(n, hq, hk, d, TYPES[dtype], axes, *four, rope_theta, bool(halves), bool(whole_ladder), as_float, eps,
                              norm, seqs, k_cache.shape[1], k_cache.shape[0], wide, between,
-                             *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(k, "k", dtype, n, hk, d),
-                             *_head_strides(v, "v", dtype, n, hk, d), *_head_strides(q_out, "q_out", dtype, n, hq, d),
-                             table_stride, *k_strides, *v_strides)
+                             *_own_strides(q, "q", n, hq, d), *_own_strides(k, "k", n, hk, d),
+                             *_head_strides(v, "v", dtype, n, hk, d), *out_strides, table_stride, *k_strides, *v_strides)
     _check(lib().regenvc_paged_append(desc, _addr(q), k.data_ptr(), v.data_ptr(), _addr(q_weight), _addr(k_weight),
                                       _addr(positions), row_starts.data_ptr(), lengths.data_ptr(), block_table.data_ptr(),
                                       _addr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _launch_stream(stream, index)))
@@ -901,13 +923,15 @@ def regenvc_paged_attn_forward(q, k_cache, v_cache, block_table, lengths, row_st
     elif lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, hq) or not lse.is_contiguous()):
         raise TypeError(f"lse must be a contiguous fp32 tensor [{n}, {hq}]")
     index = _place(q, k_cache, v_cache, block_table, lengths, row_starts, out, lse, workspace)
+    out_strides = _PACKED
     if out is None:
         out = _like(q, stream)
+    else:
+        out_strides = _head_strides(out, "out", dtype, n, hq, d)
     if workspace is None:
         workspace = _new((max(regenvc_paged_attn_workspace_bytes(hq, hk, d), 1),), torch.uint8, q.device, stream)
     desc = _PAGED_DESC.pack(n, hq, hk, d, TYPES[dtype], seqs, slots, pages, wide, group, window, 0.0 if scale is None else scale,
-                            *_head_strides(q, "q", dtype, n, hq, d), *_head_strides(out, "out", dtype, n, hq, d), table_stride,
-                            *k_strides, *v_strides)
+                            *_own_strides(q, "q", n, hq, d), *out_strides, table_stride, *k_strides, *v_strides)
     _check(lib().regenvc_paged_attn_forward(desc, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), row_starts.data_ptr(),
                                             lengths.data_ptr(), block_table.data_ptr(), out.data_ptr(), _addr(lse),
                                             workspace.data_ptr(), workspace.numel() * workspace.element_size(),

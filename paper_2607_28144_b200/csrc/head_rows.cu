@@ -241,6 +241,7 @@ cudaError_t plan_rows(K kernel, HeadRowsParams& p, int groups, int rounds, int s
     int tokens = rounds * groups / all;
     if (tokens > kMaxTokens) tokens = kMaxTokens;
     const size_t per_token = (size_t)table_pitch(p) * sizeof(float2), gains = 2 * (size_t)p.head_dim * sizeof(float);
+    if (p.n_tokens <= sm_count) tokens = 1;   // (and no query, which takes longer than such a call's kernel)
     if (tokens > 1) {
         int per_sm = 1;
         const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, tokens * per_token + gains);

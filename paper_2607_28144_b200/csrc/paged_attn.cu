@@ -7,12 +7,17 @@
 // the tiles of 128 keys that any of its rows sees.  One thread block per SM:
 //   warps 0-3, 4-7  two streams of softmax, a thread per row (TMEM lane): scores from tensor memory, running reference and
 //                   sum in registers, probabilities back to tensor memory
-//   warp  8         issues the products (one thread) and owns the tensor memory
-//   warp  9         copies: looks the pages up (a lane per box) and fetches K and V tiles into a ring by TMA
+//   warp  8         issues the products (one lane) and owns the tensor memory
+//   warps 9, 11     copies of K and of V: look the pages up (a lane per box) and fetch the tiles into a ring each by TMA
 //   warp  10        walks over this thread block's work and hands it to the others, stretch by stretch
 // More than 128 rows: each stream has 128 rows of its own and both take every tile of keys.  At most 128 rows (single
 // tokens): both streams have the same rows and take every other tile of keys, and their results are joined in tensor memory
 // at the end.  Either way one stream's products run under the other's exponentials.
+//
+// Bound: single tokens by HBM (64 streams with 16-token pages, 2.77 GB: 461 us, 6.0 TB/s of 6.44 measured).  Chunks by the
+// round a stream's tile takes through softmax and products, which one buffer of scores does not hide: 128 exponentials a row
+// (1100 cycles alone, 2000 beside the other stream's), the products (1024 and some 400 of hand-over), loads and hand-over (500)
+// (a window of 10920 tokens over 31200, 40 heads: 4.6 ms, 1.06 PFLOP/s; without exponentials 4.2 ms, without products 4.0).
 //
 // Tensor memory: tiles of scores from column 0 on, two of them beside O0 and O1 of 128 columns, three beside 64 columns; the
 // probabilities (16-bit pairs) lie over the scores.  With three, a stream's next scores are formed under its exponentials.
@@ -450,7 +455,7 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* map, int x
 }
 
 __device__ __forceinline__ bool wait_segment(const Control& c, uint32_t segment, const Waiter& wait) {
-    return wait(&c.seg_full[segment % kSegments], (segment / kSegments) & 1);
+    return wait(&c.seg_full[segment % kSegments], segment / kSegments);
 }
 
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
@@ -626,7 +631,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 uint32_t which, whole;
                 auto look_up = [&]() {
                     whole = p.one_page_box && at0 + 128 <= p.page_size;
-                    const bool mine = whole ? lane == 0 : lane * p.box_rows < 128 && key < hi && key + p.box_rows > lo;
+                    const bool mine = key < hi && (whole ? lane == 0 : lane * p.box_rows < 128 && key + p.box_rows > lo);
                     page = mine ? pages[whole ? entry0 : entry] : 0;
                     page_at = whole ? at0 : at;
                     which = __ballot_sync(0xffffffffu, mine);
@@ -739,8 +744,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         if (ok && more && two && !second) ok = take_k(k);
                         if (ok && i >= 0) ok = output(odd, v, i > 1);
                         if (ok && i >= 0) {
-                            const uint32_t visit = odd ? visit1++ : visit0++;
-                            umma_commit_elect(smem_u32(&c->o_full[odd][visit & 1]), elected);
+                            // with two tiles of scores a stream's scores come behind its products so far: only the last need telling
+                            if (S::kScores == 3 || ahead >= steps) {
+                                const uint32_t visit = odd ? visit1++ : visit0++;
+                                umma_commit_elect(smem_u32(&c->o_full[odd][visit & 1]), elected);
+                            }
                             if (!two || odd) release_v(v);
                         }
                         if (ok && more && !two) ok = take_k(k);   // (single tokens wait for keys, not for probabilities)
@@ -789,7 +797,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         auto meet_all = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c->together));
-            return __all_sync(0xffffffffu, wait(&c->together, met++ & 1));
+            return __all_sync(0xffffffffu, wait(&c->together, met++));
         };
         bool ok = true;
 #pragma unroll 1
@@ -905,11 +913,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             probabilities<F16>(s + 32 * b, scale2, pack2(-ref, -ref), pr, sum_a, sum_b);
                             tmem_st16(t_S + 16 * b, pr);
                         }
-                        float s0, s1; unpack2(add2(sum_a, sum_b), s0, s1); sum = s0 + s1;
+                        float s0, s1;
+                        unpack2(add2(sum_a, sum_b), s0, s1);
+                        sum = s0 + s1;
                         again = !(sum < raise_at<F16>());
                         if (!__any_sync(0xffffffffu, again)) break;
-                        // Rare: scores far above the reference.  The products so far are waited for, O and the sum are
-                        // brought to the new reference, and the tile is done again.
+                        // Rare: scores far above the reference.  O and the sum are brought to the new reference, and the tile
+                        // is done again.
                         const float top = highest();
                         again = again && top > m;            // (a NaN among the scores stays one)
                         if (!__any_sync(0xffffffffu, again)) break;
@@ -917,8 +927,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         if (again) m = top;
                         l *= alpha;
                         if (done > 0) {
-                            ok = __all_sync(0xffffffffu, wait(&c->o_full[t][(visit - 1) & 1], (visit - 1) >> 1));
-                            tc_fence_after();
+                            // (with two tiles of scores these came behind the stream's products so far)
+                            if (S::kScores == 3) {
+                                ok = __all_sync(0xffffffffu, wait(&c->o_full[t][(visit - 1) & 1], (visit - 1) >> 1));
+                                tc_fence_after();
+                            }
 #pragma unroll 1
                             for (int b = 0; ok && b < D; b += 16) {
                                 uint32_t o[16];
@@ -937,7 +950,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&c->p_full[buffer]));
                 if (!ok) break;
-                ++visit;
+                if (S::kScores == 3) ++visit;
                 ++done;
             }
             if (!ok) break;
@@ -946,6 +959,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
             // ------------------------------------------------------------------------------------- results
             if (done > 0) {
+                if (S::kScores == 2) ++visit;                // (told once, at the end)
                 ok = __all_sync(0xffffffffu, wait(&c->o_full[t][(visit - 1) & 1], (visit - 1) >> 1));
                 if (!ok) break;
                 tc_fence_after();
@@ -1068,6 +1082,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p
     if (!first.valid || row0 >= first.rows) return;
     const uint32_t v = __ballot_sync(0xffffffffu, valid), e = __ballot_sync(0xffffffffu, valid && ends);
     if (lane == 0 && warp <= kPagedMaxGrid / 32) valid_at[warp] = v, ends_at[warp] = e;
+    if (threadIdx.x == 0) n_pieces = 0;
     __syncthreads();
     {   // this thread's piece, if it is one of the item's: the valid ones before it, and none of those ends the item
         int before = 0;
@@ -1082,6 +1097,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p
     }
     __syncthreads();
     const int n = n_pieces, c4 = threadIdx.x / kRowsAtOnce;
+    if (n == 0) return;                                      // (a thread block gave up on a wait: the end is not there)
     float m[kTurns], l[kTurns];
     float4 o[kTurns];
 #pragma unroll

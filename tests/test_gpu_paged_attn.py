@@ -106,11 +106,11 @@ def test_scores_that_rise_along_the_keys(dtype, new, group):
     check(c, [new], [keys], out, lse, group, 0)
 
 
-@pytest.mark.parametrize("group,window", [(1, 0), (0, 0), (3, 1)])
-def test_rows_that_see_nothing(group, window):
+@pytest.mark.parametrize("group,window,page", [(1, 0, 16), (0, 0, 16), (3, 1, 16), (1, 0, 1560), (0, 0, 256)])
+def test_rows_that_see_nothing(group, window, page):
     """Sequences with fewer cached tokens than rows, none at all, and none of either."""
     new, keys = [5, 4, 0, 200, 2], [3, 0, 0, 150, 9]
-    c = make(new, keys, 4, 2, 128, 16, BF, seed=5)
+    c = make(new, keys, 4, 2, 128, page, BF, seed=5)
     out, lse = B.regenvc_paged_attn_forward(*c["args"], group=group, window=window, lse=True)
     assert B.regenvc_device_status() == B.OK
     check(c, new, keys, out, lse, group, window)
