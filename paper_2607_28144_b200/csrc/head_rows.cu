@@ -3,9 +3,15 @@
 //     y = R(position) (x / sqrt(mean(x^2) + eps) * w)      over the elements of one head; values are copied
 //
 // R turns pair j by position[axis(j)] * frequency(j).  The normalised values never round to the rows' type in between.
-// Bound: HBM, every element is read and written once (two passes, a norm and a rotation, move twice that).  The angles of
-// a token are shared by all its heads, so a thread block computes them once per token into shared memory and then walks
-// over its (token, head) vectors, four to eight pieces of 16 bytes per thread in flight.
+// Bound: HBM, every element is read and written once (two passes, a norm and a rotation, move twice that); next to it issue
+// slots and shared memory's ports.  The angles of a token are shared by all its heads, so a thread block computes them once per
+// token into shared memory.  A group of lanes then has one token and walks over its heads: addresses are two multiply-adds, and
+// angles and gains come in words without bank conflicts (a walk over (token, head) pairs whose lanes read gains 32 bytes apart
+// took 330 instructions and 65 shared wavefronts a vector, and 32 us where this takes 27).  One vector is in flight per group
+// beside the one at hand, with four blocks on an SM: angles or gains held in registers over the walk spill (31 to 55 us), three
+// blocks 30 us, five 37.
+// Measured, 10920 tokens, 12 + 12 heads of 128, bf16: 27.0 us, 5.0 TB/s of what it has to move; with the values into a cache
+// of 1560-token pages 42.6 us, 4.7 TB/s; one token 3 us, 64 tokens appended 5 us (a chain of list, page and row behind a launch).
 // Paged: token n of the call belongs to the sequence whose rows it lies in, found by counting the row starts at or before
 // it (a warp per token, all loads independent: a binary search is a chain of loads, which is what a call of a few tokens
 // would wait for); its slot is the sequence's length minus the rows behind it, its page comes from the table.
@@ -15,8 +21,7 @@
 namespace regenvc {
 namespace {
 
-constexpr int kBatch = 1;
-constexpr int kMaxTokens = 16;      // per thread block
+constexpr int kMaxTokens = kHeadTokens;
 
 // Offsets of a token's slot in the two caches; -1: the token goes nowhere (behind the last sequence, a page that is not
 // there).
@@ -58,7 +63,7 @@ __device__ __forceinline__ void find_slots(const HeadRowsParams& p, Slots& s, in
     }
 }
 
-// Where vector (t, h) comes from and goes to; w: 0 q, 1 k, 2 v.
+// The element form's: where vector (t, h) comes from and goes to; w: 0 q, 1 k, 2 v.
 template <typename T>
 __device__ __forceinline__ bool locate(const HeadRowsParams& p, const Slots& s, int token0, int t, int h, int& w, const T*& from, T*& to) {
     w = 0;
@@ -86,91 +91,84 @@ template <typename T, bool HALVES>
 __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
     extern __shared__ float4 shared_raw[];
     __shared__ Slots slots;
-    const int pitch = table_pitch(p), units = table_units<HALVES ? kHalfUnits : kAdjacentUnits>(p);
+    const int pitch = table_pitch(p), units = p.head_dim / 16, turning = table_units<HALVES ? kHalfUnits : kAdjacentUnits>(p);
     float2* table = reinterpret_cast<float2*>(shared_raw);
     float* gains = reinterpret_cast<float*>(table + p.tokens_per_cta * pitch);
     const int token0 = blockIdx.x * p.tokens_per_cta, tokens = min(p.tokens_per_cta, p.n_tokens - token0);
-    const int u = threadIdx.x & (width - 1), group = threadIdx.x / width, groups = blockDim.x / width;
-    const bool active = u < p.head_dim / 16;
-    const Pieces at = pieces_of<HALVES>(p, active ? u : 0);
-    const int all = p.heads[0] + p.heads[1] + p.heads[2], total = tokens * all;
+    // a group of lanes has one token, and every so many of its vectors
+    const int u = threadIdx.x & (width - 1), group = threadIdx.x / width, step = blockDim.x / width / p.tokens_per_cta;
+    const int t = group / step, all = p.heads[0] + p.heads[1] + p.heads[2], rounds = (all + step - 1) / step;
+    bool active = u < units && t < tokens;
+    const Pieces at = pieces_of<HALVES>(p, u < units ? u : 0);
     const float inv_d = 1.0f / (float)p.head_dim;
-
-    // One vector (token, head) per group of lanes and round, kBatch rounds at a time; the loads of the next rounds are on
-    // their way while these are worked off, and the first ones while the angles are formed.
-    struct Item {
-        Raw8<T> lo, hi;
-        T* to;                                              // nullptr: nothing to do
-        int of, token;
-    };
-    int t = group / all, h = group - t * all;               // this group's next vector
-    auto fetch = [&](Item& x) {
-        x.to = nullptr;
-        x.of = x.token = 0;
-        x.lo = x.hi = Raw8<T>{};
-        if (t < tokens) {
-            const T* from;
-            x.token = t;
-            if (locate<T>(p, slots, token0, t, h, x.of, from, x.to) && active) {
-                x.lo = load_raw8(from + at.lo);
-                x.hi = load_raw8(from + at.hi);
-            } else {
-                x.to = nullptr;
-            }
-            h += groups;
-            while (h >= all) h -= all, ++t;
-        }
-    };
-    Item next[kBatch];
     if (p.paged) {
         find_slots(p, slots, token0, tokens);
         __syncthreads();
+        active = active && slots.rows[t];
     }
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) fetch(next[i]);
-    if (p.n_axes) fill_table<HALVES ? kHalfUnits : kAdjacentUnits>(p, table, pitch, token0, tokens, false);
-    if (p.norm) fill_gains(p, gains);
-    __syncthreads();
 
-    for (int base = 0; base < total; base += groups * kBatch) {   // the same rounds for all lanes: sums are shuffles
-        Item now[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) now[i] = next[i];
-        if (base + groups * kBatch < total) {
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) fetch(next[i]);
+    // The loads of the next round are on their way while this one is worked off, the first ones while the angles are formed.
+    struct Item {
+        Raw8<T> lo, hi;
+        T* to;                                              // nullptr: nothing to do
+        int of;                                             // 0 q, 1 k, 2 v
+    };
+    const int lo_bytes = at.lo * (int)sizeof(T), hi_from_lo = at.hi - at.lo;
+    const int q_heads = p.heads[0], qk_heads = q_heads + p.heads[1];
+    int h = group - t * step;                               // this group's next vector
+    auto fetch = [&](Item& x) {
+        x.to = nullptr;
+        x.of = (h >= q_heads) + (h >= qk_heads);
+        const long long slot = !p.paged || !x.of ? 0 : (x.of == 1 ? slots.k[t] : slots.v[t]);
+        if (active && h < all && slot >= 0) {
+            const HeadRowsView& o = p.view[x.of];
+            const int token = token0 + t, head = h - (x.of == 0 ? 0 : (x.of == 1 ? q_heads : qk_heads));
+            const T* v = reinterpret_cast<const T*>(o.from + (long long)token * o.from_token + (long long)head * o.from_head + lo_bytes);
+            x.to = reinterpret_cast<T*>(o.to + (long long)token * o.to_token + (long long)head * o.to_head + lo_bytes) + slot;
+            x.lo = load_raw8_once(v);
+            x.hi = load_raw8_once(v + hi_from_lo);
+        } else {
+            x.lo = x.hi = Raw8<T>{};
         }
+        h += step;
+    };
+    Item next;
+    fetch(next);
+    if (p.n_axes) fill_table<HALVES ? kHalfUnits : kAdjacentUnits>(p, table, pitch, token0, tokens, false);
+    if (p.norm) fill_gains<HALVES>(p, gains);
+    __syncthreads();
+    const ulonglong2* words = reinterpret_cast<const ulonglong2*>(table + t * pitch) + u;
+
+    for (int r = 0; r < rounds; ++r) {                      // the same rounds for all lanes: sums are shuffles
+        const Item x = next;
+        if (r + 1 < rounds) fetch(next);
+        Unit v = widen<HALVES>(x.lo, x.hi);
+        if (p.norm) {
+            uint64_t sq = 0;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            Item& x = now[i];
-            float lo[8], hi[8];
-            widen8(x.lo, lo);
-            widen8(x.hi, hi);
-            if (p.norm) {
-                float sq = 0.0f;
+            for (int e = 0; e < 4; ++e) sq = fma2(v.b[e], v.b[e], fma2(v.a[e], v.a[e], sq));
+            const float scale = rsqrtf(head_sum(sum2(sq), width) * inv_d + p.eps);
+            if (x.of < 2 && x.to) {
+                const Unit gain = load_gains<HALVES>(reinterpret_cast<const ulonglong2*>(gains) + x.of * 4 * units + u, units);
+                const uint64_t r2 = pack2(scale, scale);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq += lo[e] * lo[e] + hi[e] * hi[e];
-                const float r = rsqrtf(head_sum(sq, width) * inv_d + p.eps);
-                if (x.of < 2) {
-                    float g[8];
-                    load_eight(gains + x.of * p.head_dim + at.lo, g);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) lo[e] *= r * g[e];
-                    load_eight(gains + x.of * p.head_dim + at.hi, g);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) hi[e] *= r * g[e];
+                for (int e = 0; e < 4; ++e) {
+                    v.a[e] = mul2(v.a[e], mul2(r2, gain.a[e]));
+                    v.b[e] = mul2(v.b[e], mul2(r2, gain.b[e]));
                 }
             }
-            if (!x.to) continue;
-            if (x.of == 2) {                                // a copy, whatever the bits say
-                store_raw8(x.to + at.lo, x.lo);
-                store_raw8(x.to + at.hi, x.hi);
-                continue;
-            }
-            if (at.turns) turn<HALVES>(lo, hi, reinterpret_cast<const float4*>(table + x.token * pitch) + u, units);
-            store8(x.to + at.lo, lo);
-            store8(x.to + at.hi, hi);
         }
+        if (!x.to) continue;
+        if (x.of == 2) {                                    // a copy, whatever the bits say
+            store_raw8(x.to, x.lo);
+            store_raw8(x.to + hi_from_lo, x.hi);
+            continue;
+        }
+        if (at.turns) turn(v, load_angles(words, turning));
+        float lo[8], hi[8];
+        spread<HALVES>(v, lo, hi);
+        store8(x.to, lo);
+        store8(x.to + hi_from_lo, hi);
     }
 }
 
@@ -233,44 +231,28 @@ __global__ void __launch_bounds__(kHeadThreads) head_rows_element_kernel(const _
     }
 }
 
-// Tokens per thread block: enough vectors for `rounds` per group of lanes; fewer where that would leave the device less than
-// one round of blocks.
-template <typename K>
-cudaError_t plan_rows(K kernel, HeadRowsParams& p, int groups, int rounds, int sm_count, int* blocks, size_t* smem) {
-    const int all = p.heads[0] + p.heads[1] + p.heads[2];
-    int tokens = rounds * groups / all;
-    if (tokens > kMaxTokens) tokens = kMaxTokens;
-    const size_t per_token = (size_t)table_pitch(p) * sizeof(float2), gains = 2 * (size_t)p.head_dim * sizeof(float);
-    if (p.n_tokens <= sm_count) tokens = 1;   // (and no query, which takes longer than such a call's kernel)
-    if (tokens > 1) {
-        int per_sm = 1;
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, tokens * per_token + gains);
-        if (e != cudaSuccess) return e;
-        const long long room = (long long)(per_sm > 0 ? per_sm : 1) * sm_count, even = (p.n_tokens + room - 1) / room;
-        if (tokens > even) tokens = (int)even;
-    }
-    if (tokens < 1) tokens = 1;
-    p.tokens_per_cta = tokens;
-    *blocks = (p.n_tokens + tokens - 1) / tokens;
-    *smem = tokens * per_token + gains;
-    return cudaSuccess;
+size_t shared_bytes(const HeadRowsParams& p) {
+    return p.tokens_per_cta * (size_t)table_pitch(p) * sizeof(float2) + 2 * (size_t)p.head_dim * sizeof(float);
 }
 
 template <typename T>
 cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, cudaStream_t stream) {
-    int blocks = 0;
-    size_t smem = 0;
-    if (!in_units(p, vec)) {
-        const cudaError_t e = plan_rows(head_rows_element_kernel<T>, p, kHeadThreads / 32, 16, sm_count, &blocks, &smem);
-        if (e != cudaSuccess) return e;
-        head_rows_element_kernel<T><<<blocks, kHeadThreads, smem, stream>>>(p);
-        return cudaGetLastError();
-    }
-    const int width = lanes_of_head(p);
+    const int all = p.heads[0] + p.heads[1] + p.heads[2];
+    const bool unit = in_units(p, vec, sizeof(T));
+    const int width = unit ? lanes_of_head(p) : 32;
     auto kernel = p.halves ? head_rows_kernel<T, true> : head_rows_kernel<T, false>;
-    const cudaError_t e = plan_rows(kernel, p, kHeadThreads / width, 8, sm_count, &blocks, &smem);
-    if (e != cudaSuccess) return e;
-    kernel<<<blocks, kHeadThreads, smem, stream>>>(p, width);
+    int per_sm = 1;
+    p.tokens_per_cta = kMaxTokens;
+    if (p.n_tokens > sm_count) {   // (a query takes longer than the kernel of a call of a few tokens)
+        const cudaError_t e = unit ? cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, shared_bytes(p))
+                                   : cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, head_rows_element_kernel<T>, kHeadThreads, shared_bytes(p));
+        if (e != cudaSuccess) return e;
+    }
+    p.tokens_per_cta = tokens_of_block(p.n_tokens, all, kHeadThreads / width, 12, 2ll * per_sm * sm_count);
+    const int blocks = (p.n_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta;
+    const size_t smem = shared_bytes(p);
+    if (unit) kernel<<<blocks, kHeadThreads, smem, stream>>>(p, width);
+    else head_rows_element_kernel<T><<<blocks, kHeadThreads, smem, stream>>>(p);
     return cudaGetLastError();
 }
 

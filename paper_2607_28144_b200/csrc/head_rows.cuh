@@ -7,6 +7,13 @@
 
 namespace regenvc {
 
+// Where an operand's vectors lie, strides in bytes, for the kernels on units: an address is then two multiply-adds.
+struct HeadRowsView {
+    const char *from, *dy;
+    char* to;
+    int from_token, from_head, dy_token, dy_head, to_token, to_head;
+};
+
 struct HeadRowsParams {
     const void* in[3];                 // q, k, v: [tokens][heads][head_dim]
     void* out[3];                      // q, k: rows; paged: k, v: the caches
@@ -32,7 +39,8 @@ struct HeadRowsParams {
     long long grad_token[2], grad_head[2];
     float* dweight[2];
     float* partial;                    // [blocks][2][head_dim]
-    int tokens_per_cta;                // set by the launchers
+    int tokens_per_cta;                // set by the launchers, as is:
+    HeadRowsView view[3];
     double turns[kRopeMaxPairs];       // frequency / (2 pi) of a pair: whole turns per unit of position
 };
 

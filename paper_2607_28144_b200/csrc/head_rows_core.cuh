@@ -5,6 +5,8 @@
 // half (in half pairs: of the rotated part, and of the part that is not rotated alike).  Either way it holds both elements of
 // its pairs, and neighbouring lanes read neighbouring 16-byte words (sixteen neighbours to a lane touched every sector twice,
 // at twice the time).  A group of 4, 8 or 16 lanes (the next power of two) holds a head; its sums are a few shuffles.
+// What these kernels run out of first is issue slots, so a lane's eight pairs are four twos of pairs, first elements in one
+// 64-bit register and second elements in another, and all arithmetic is on two of them at once.
 #pragma once
 #include "head_rows.cuh"
 #include "row_io.cuh"
@@ -21,15 +23,15 @@ template <int ORDER>
 __device__ __forceinline__ int table_units(const HeadRowsParams& p) {
     return ORDER == kAdjacentUnits ? p.head_dim / 16 : p.n_pairs / 8;
 }
-// Words of a token's table: (cos, sin) of pair j where the lane that holds the pair finds it as 16-byte words of two pairs,
-// word i (of four) of unit u at i * units + u, so that neighbouring lanes read neighbouring words.
+// Where in a token's table (in floats) the cosine of pair j lies; its sine lies two behind.  Two pairs make a 16-byte word
+// (cos, cos, sin, sin), word i (of four) of unit u is at i * units + u: neighbouring lanes read neighbouring words.
 template <int ORDER>
 __device__ __forceinline__ int place(const HeadRowsParams& p, int j) {
     const int units = table_units<ORDER>(p);
-    if (ORDER == kHalfUnits) return ((j >> 1 & 3) * units + (j >> 3)) * 2 + (j & 1);
+    if (ORDER == kHalfUnits) return ((j >> 1 & 3) * units + (j >> 3)) * 4 + (j & 1);
     const int half = j >= 4 * units;
     j -= half * 4 * units;
-    return ((2 * half + (j >> 1 & 1)) * units + (j >> 2)) * 2 + (j & 1);
+    return ((2 * half + (j >> 1 & 1)) * units + (j >> 2)) * 4 + (j & 1);
 }
 // Angles in whole turns, position * frequency / (2 pi) in 64 bits, its fraction taken there too; sine and cosine of the
 // fraction in 32 bits.
@@ -39,9 +41,10 @@ __device__ __forceinline__ void fill_table(const HeadRowsParams& p, float2* tabl
     const int entries = ORDER == kAdjacentUnits ? p.head_dim / 2 : p.n_pairs;
     const int at_a_time = blockDim.x / entries, first = threadIdx.x / entries, j = threadIdx.x - first * entries;
     if (first >= at_a_time) return;
-    float2* to = table + (ORDER == kPlain ? j : place<ORDER>(p, j));
+    float* to = reinterpret_cast<float*>(table) + (ORDER == kPlain ? 2 * j : place<ORDER>(p, j));
+    const int sine = ORDER == kPlain ? 1 : 2;
     if (j >= p.n_pairs) {
-        for (int t = first; t < tokens; t += at_a_time) to[t * pitch] = make_float2(1.0f, 0.0f);
+        for (int t = first; t < tokens; t += at_a_time) to[2 * t * pitch] = 1.0f, to[2 * t * pitch + sine] = 0.0f;
         return;
     }
     int axis = 0;
@@ -55,17 +58,40 @@ __device__ __forceinline__ void fill_table(const HeadRowsParams& p, float2* tabl
         const double turn = pos * turns;
         float s, k;
         sincospif(2.0f * (float)(turn - rint(turn)), &s, &k);
-        to[t * pitch] = make_float2(k, back ? -s : s);
+        to[2 * t * pitch] = k;
+        to[2 * t * pitch + sine] = back ? -s : s;
     }
 }
 __host__ __device__ inline int table_pitch(const HeadRowsParams& p) {
     return ((p.n_axes ? p.head_dim / 2 : 0) + 3) & ~3;
 }
+// Where the gains of an operand lie (in floats, head_dim of them): word i (of four) of unit u at i * units + u, as above, in
+// the order of Unit.  offset: of an element in its head.
+template <bool HALVES>
+__device__ __forceinline__ int gain_place(const HeadRowsParams& p, int offset) {
+    const int units = p.head_dim / 16;
+    int u, second, e;                                       // e: of the eight of a piece
+    if (HALVES) {
+        const int turned = 2 * p.n_pairs, behind = offset >= turned, half = behind ? p.head_dim / 2 - p.n_pairs : p.n_pairs;
+        offset -= behind ? turned : 0;
+        second = offset >= half;
+        offset -= second ? half : 0;
+        u = (behind ? p.n_pairs / 8 : 0) + offset / 8;
+        e = offset & 7;
+        return ((2 * second + (e >> 2)) * units + u) * 4 + (e & 3);
+    }
+    second = offset >= p.head_dim / 2;
+    offset -= second ? p.head_dim / 2 : 0;
+    u = offset / 8;
+    e = offset & 7;
+    return ((2 * second + (e >> 2)) * units + u) * 4 + ((e & 1) << 1 | (e >> 1 & 1));
+}
 // Gains of q and k [2][head_dim] (ones where there are none).
+template <bool HALVES>
 __device__ __forceinline__ void fill_gains(const HeadRowsParams& p, float* gains) {
     for (int i = threadIdx.x; i < 2 * p.head_dim; i += blockDim.x) {
-        const int w = i >= p.head_dim;
-        gains[i] = p.weight[w] ? p.weight[w][i - w * p.head_dim] : 1.0f;
+        const int w = i >= p.head_dim, offset = i - w * p.head_dim;
+        gains[w * p.head_dim + gain_place<HALVES>(p, offset)] = p.weight[w] ? p.weight[w][offset] : 1.0f;
     }
 }
 
@@ -92,38 +118,122 @@ __device__ __forceinline__ Pieces pieces_of(const HeadRowsParams& p, int u) {
     return {at, at + p.head_dim / 2 - p.n_pairs, false};
 }
 
-// (a, b) -> (a cos - b sin, b cos + a sin) for the eight pairs of a unit; words: the token's table from the unit's word on.
+// A unit's eight pairs: two i holds the pairs 2i and 2i + 1, first elements in a, second ones in b.
+struct Unit {
+    uint64_t a[4], b[4];
+};
+// Offset in its head of element `second` (0 or 1) of pair 2i + k.
 template <bool HALVES>
-__device__ __forceinline__ void turn(float* lo, float* hi, const float4* words, int units) {
+__device__ __forceinline__ int offset_of(const Pieces& at, int i, int k, int second) {
+    return HALVES ? (second ? at.hi : at.lo) + 2 * i + k : (i < 2 ? at.lo + 4 * i : at.hi + 4 * (i - 2)) + 2 * k + second;
+}
+template <bool HALVES, typename T>
+__device__ __forceinline__ Unit widen(const Raw8<T>& lo, const Raw8<T>& hi) {
+    float l[8], h[8];
+    widen8(lo, l);
+    widen8(hi, h);
+    Unit v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float4 t = words[i * units];
-        if (HALVES) {
-            const float a = lo[2 * i], b = hi[2 * i], a2 = lo[2 * i + 1], b2 = hi[2 * i + 1];
-            lo[2 * i] = a * t.x - b * t.y;
-            hi[2 * i] = b * t.x + a * t.y;
-            lo[2 * i + 1] = a2 * t.z - b2 * t.w;
-            hi[2 * i + 1] = b2 * t.z + a2 * t.w;
-        } else {
-            float* v = i < 2 ? lo + 4 * i : hi + 4 * (i - 2);
-            const float a = v[0], b = v[1], a2 = v[2], b2 = v[3];
-            v[0] = a * t.x - b * t.y;
-            v[1] = b * t.x + a * t.y;
-            v[2] = a2 * t.z - b2 * t.w;
-            v[3] = b2 * t.z + a2 * t.w;
-        }
+        const float* f = i < 2 ? l + 4 * i : h + 4 * (i - 2);
+        v.a[i] = HALVES ? pack2(l[2 * i], l[2 * i + 1]) : pack2(f[0], f[2]);
+        v.b[i] = HALVES ? pack2(h[2 * i], h[2 * i + 1]) : pack2(f[1], f[3]);
+    }
+    return v;
+}
+template <bool HALVES>
+__device__ __forceinline__ void spread(const Unit& v, float* l, float* h) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float* f = i < 2 ? l + 4 * i : h + 4 * (i - 2);
+        if (HALVES) unpack2(v.a[i], l[2 * i], l[2 * i + 1]), unpack2(v.b[i], h[2 * i], h[2 * i + 1]);
+        else unpack2(v.a[i], f[0], f[2]), unpack2(v.b[i], f[1], f[3]);
     }
 }
-__device__ __forceinline__ void load_eight(const float* g, float* v) {
-    const float4 a = reinterpret_cast<const float4*>(g)[0], b = reinterpret_cast<const float4*>(g)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// The gains of a unit; words: those of its operand from the unit's word on.
+template <bool HALVES>
+__device__ __forceinline__ Unit load_gains(const ulonglong2* words, int units) {
+    Unit v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const ulonglong2 g = words[i * units];
+        if (HALVES) {
+            uint64_t* to = i < 2 ? v.a + 2 * i : v.b + 2 * (i - 2);
+            to[0] = g.x, to[1] = g.y;
+        } else {
+            v.a[i] = g.x, v.b[i] = g.y;
+        }
+    }
+    return v;
+}
+// (a, b) -> (a cos - b sin, b cos + a sin)
+struct Angles {
+    uint64_t cos[4], sin[4];
+};
+__device__ __forceinline__ Angles load_angles(const ulonglong2* words, int units) {   // words: the token's, from the unit's on
+    Angles v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const ulonglong2 t = words[i * units];
+        v.cos[i] = t.x, v.sin[i] = t.y;
+    }
+    return v;
+}
+__device__ __forceinline__ void turn(Unit& v, const Angles& by) {
+    const uint64_t minus = pack2(-1.0f, -1.0f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t a = v.a[i], b = v.b[i];
+        v.a[i] = fma2(a, by.cos[i], mul2(mul2(b, minus), by.sin[i]));
+        v.b[i] = fma2(b, by.cos[i], mul2(a, by.sin[i]));
+    }
+}
+__device__ __forceinline__ float sum2(uint64_t v) {
+    float a, b;
+    unpack2(v, a, b);
+    return a + b;
 }
 
-// Whether a call's rows can be worked off in units; `width`: lanes of a head.
-inline bool in_units(const HeadRowsParams& p, bool vec) {
-    return vec && p.head_dim % 16 == 0 && (!p.halves || p.n_pairs % 8 == 0);
+// Whether a call's rows can be worked off in units: aligned, whole units, strides of less than 2 GB (farther vectors take the
+// element form, with 64-bit strides).  Fills the views.
+inline bool in_units(HeadRowsParams& p, bool vec, int size) {
+    if (!vec || p.head_dim % 16 || (p.halves && p.n_pairs % 8)) return false;
+    bool fits = true;
+    auto bytes = [&](long long stride, int extent) {   // (of one vector no stride is taken)
+        if (extent <= 1) return 0;
+        fits = fits && stride * size >= 0 && stride * size <= 0x7FFFFFFFll;
+        return (int)(stride * size);
+    };
+    for (int w = 0; w < 3; ++w) {
+        HeadRowsView& v = p.view[w];
+        v = {};
+        if (!p.heads[w]) continue;
+        v.from = (const char*)p.in[w];
+        v.to = (char*)p.out[w];
+        v.from_token = bytes(p.in_token[w], p.n_tokens);
+        v.from_head = bytes(p.in_head[w], p.heads[w]);
+        v.to_token = p.paged && w ? 0 : bytes(p.out_token[w], p.n_tokens);   // (a cache's slots have offsets of their own)
+        v.to_head = bytes(p.out_head[w], p.heads[w]);
+        if (w == 2 || !p.grad[w]) continue;
+        v.dy = (const char*)p.grad[w];
+        v.dy_token = bytes(p.grad_token[w], p.n_tokens);
+        v.dy_head = bytes(p.grad_head[w], p.heads[w]);
+    }
+    return fits;
 }
 inline int lanes_of_head(const HeadRowsParams& p) { return p.head_dim <= 64 ? 4 : (p.head_dim <= 128 ? 8 : 16); }
+
+// Tokens per thread block: a power of two, so that a token has a whole number of the block's groups and these walk over its
+// heads.  More of them leave less of the last round empty and form angles with more of the block at a time; up to `rounds`
+// rounds, and only while `blocks` blocks are left.
+constexpr int kHeadTokens = 16;
+inline int tokens_of_block(int n_tokens, int all, int groups, int rounds, long long blocks) {
+    int tokens = 1;
+    while (2 * tokens <= kHeadTokens && 2 * tokens <= groups && ((long long)all * 2 * tokens + groups - 1) / groups <= rounds &&
+           (n_tokens + 2 * tokens - 1) / (2 * tokens) >= blocks)
+        tokens *= 2;
+    return tokens;
+}
 
 // Element form (rows without 16-byte alignment, other head_dim): a warp holds a head, unit u of it is pair u for
 // u < n_pairs and one unrotated element behind; up to 255 units, eight to a lane.

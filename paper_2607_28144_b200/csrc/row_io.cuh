@@ -36,6 +36,14 @@ __device__ __forceinline__ void store_raw8(T* p, const Raw8<T>& r) {
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(p)[i] = r.w[i];
 }
+// The same for data that a kernel touches once (first to leave the caches).
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw8_once(const T* p) {
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+}
 __device__ __forceinline__ void widen2(uint32_t w, float& a, float& b, const __nv_bfloat16*) {
     a = __uint_as_float(w << 16);
     b = __uint_as_float(w & 0xFFFF0000u);
@@ -75,6 +83,19 @@ __device__ __forceinline__ void store8(T* p, const float* v) {
         const T* tag = nullptr;
         *reinterpret_cast<uint4*>(p) = make_uint4(narrow2(v[0], v[1], tag), narrow2(v[2], v[3], tag),
                                                   narrow2(v[4], v[5], tag), narrow2(v[6], v[7], tag));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8_once(T* p, const float* v) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            __stcs(reinterpret_cast<float4*>(p) + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+    } else {
+        const T* tag = nullptr;
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(narrow2(v[0], v[1], tag), narrow2(v[2], v[3], tag),
+                                                       narrow2(v[4], v[5], tag), narrow2(v[6], v[7], tag)));
     }
 }
 

@@ -219,3 +219,59 @@ def test_offsets_past_32_bits():
     B.regenvc_paged_append(rows, rows, kc, vc, table, torch.tensor([16], dtype=torch.int32, device=DEV),
                            torch.tensor([0, 3], dtype=torch.int32, device=DEV))
     assert torch.equal(kc[-1, 13:], rows) and torch.equal(vc[-1, 13:], rows)
+
+
+# blocks of 2, 4, 8 and 16 tokens, with a last one that is not full; heads that leave a part of the last round empty
+MANY = [
+    (2501, 2, 1, 128, BF, (44, 42, 42), False, False, False, True),
+    (5003, 9, 4, 64, FP, (20, 12), True, True, False, True),
+    (9999, 5, 2, 80, BF, (24, 20, 20), False, False, False, True),
+    (19003, 3, 0, 32, F32, (16, 8), True, False, False, True),
+    (30001, 1, 1, 16, BF, (16,), False, False, True, True),
+]
+
+
+@pytest.mark.parametrize("case", MANY)
+def test_blocks_of_several_tokens(case):
+    test_forward(case)
+    test_gradients_of_the_formula(case)
+
+
+def test_appending_blocks_of_several_tokens():
+    new, keys, page, d = [4000, 1, 5501], [4100, 900, 5501], 24, 64
+    g = torch.Generator().manual_seed(page)
+    table, pages = scatter_pages(keys, page, "tokens", g)
+    n = sum(new)
+    q, k, v = (torch.randn(n, h, d, generator=g).to(BF).to(DEV) for h in (4, 1, 1))
+    kc, vc = (torch.zeros(pages, page, 1, d, dtype=BF, device=DEV) for _ in range(2))
+    starts = [sum(new[:i]) for i in range(len(new) + 1)]
+    pos = torch.arange(n, dtype=torch.int32, device=DEV).view(1, -1)
+    lists = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in (keys, starts)]
+    q_out = B.regenvc_paged_append(k, v, kc, vc, table.to(DEV), *lists, q=q, positions=pos, widths=[d], norm=B.NORM_RMS)
+    qr, kr = B.regenvc_qk_norm_rope_forward(q, k, pos, [d])
+    assert torch.equal(q_out, qr)
+    for s, (m, total) in enumerate(zip(new, keys)):
+        page_at, slot_at = slots_of(table, s, total, page)
+        at = page_at[total - m:].to(DEV), slot_at[total - m:].to(DEV)
+        part = slice(starts[s], starts[s] + m)
+        assert torch.equal(kc[at], kr[part]) and torch.equal(vc[at], v[part])
+    assert int((vc != 0).any(dim=3).sum()) <= n and B.regenvc_device_status() == B.OK
+
+
+def test_vectors_more_than_two_gigabytes_apart():
+    far = (1 << 30) + 64                                               # elements between the two heads: 2 GB and a little
+    room = torch.empty(far + 64 * 3, dtype=BF, device=DEV)
+    x = room.as_strided((3, 2, 64), (64, far, 1))
+    x.copy_(torch.randn(3, 2, 64, generator=torch.Generator().manual_seed(1)).to(BF))
+    near = x.contiguous()
+    w = torch.ones(64, device=DEV)
+    pos = torch.arange(3, dtype=torch.int32, device=DEV).view(1, -1)
+    want, _ = B.regenvc_qk_norm_rope_forward(near, None, pos, [64], q_weight=w)
+    ref, mag = reference(near, w, pos, (64,), dict(halves=False, whole_ladder=False))
+    got, _ = B.regenvc_qk_norm_rope_forward(x, None, pos, [64], q_weight=w)
+    for y in (want, got):
+        assert ((y.double() - ref).abs() <= forward_bound(ref, mag, BF, 64)).all()
+    back = B.regenvc_qk_norm_rope_backward(want, None, x, None, pos, [64], q_weight=w)
+    dx, mag, dw, dwm = head_grads64(near.double(), w.double(), want.double(), pos, (64,), 10000.0, False, False, 1e-6)
+    assert ((back["dq"].double() - dx).abs() <= half_step(BF) * dx.abs() + 176 * U * mag + floor_step(BF)).all()
+    assert ((back["dq_weight"].double() - dw).abs() <= 134 * U * dwm).all()
