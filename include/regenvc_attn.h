@@ -326,7 +326,8 @@ int regenvc_qk_norm_rope_backward(const regenvc_qk_norm_rope_desc* desc, const v
  *   scale  : > 0, or 0 for 1 / sqrt(head_dim)
  *   lse    : fp32 [n_tokens][n_q_heads] or NULL: natural logarithm of the sum of the exponentials of a row's scores
  *   A row that sees nothing gives zeros (lse -inf).  What lies in unseen slots (behind a length, before the window of all
- *   of a call's rows, in unused pages) does not matter; tokens that any new token of their sequence sees must be finite.
+ *   of a call's rows, in unused pages) does not matter; values that any new token of their sequence sees must be finite.
+ *   A NaN in q or in a key makes the rows that see it NaN (lse too), and no others.
  *   page_size: a multiple of 8 (REGENVC_ERR_UNSUPPORTED); rows of q, out and the caches allow 16-byte accesses
  *   (REGENVC_ERR_MISALIGNED).  Probabilities are rounded to the cache's type, everything else is fp32.
  *   workspace : regenvc_paged_attn_workspace_bytes() bytes (0 for invalid arguments), 16-byte aligned, its content of no

@@ -156,8 +156,8 @@ struct Control {
     long long start, left;
     int item_seq[kMaxRounds], item_head[kMaxRounds], item_tile[kMaxRounds];
     // the plan's sums
-    long long warp_cost[kPgThreads / 32], taken, before;
-    int warp_items[kPgThreads / 32], most;
+    long long warp_cost[kPgThreads / 32], warp_items[kPgThreads / 32], taken, before;
+    int most;
 };
 
 __device__ __forceinline__ void plan_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kPgThreads) : "memory"); }
@@ -170,8 +170,8 @@ __device__ __forceinline__ long long bound(long long all, int n, int i) {
     return i >= n ? all : (long long)((double)all * (double)__fdividef((float)i, (float)n));
 }
 // Parts: one per item or per four units, whichever are more, as far as there are thread blocks.
-__device__ __forceinline__ int parts_of(long long all, int items) {
-    const long long most = max((long long)items, (all + 3) / 4);
+__device__ __forceinline__ int parts_of(long long all, long long items) {
+    const long long most = max(items, (all + 3) / 4);
     return (int)min((long long)gridDim.x, max(most, 1ll));
 }
 
@@ -361,8 +361,8 @@ __device__ __noinline__ void plan_few(const PagedAttnParams& p, Control& c, Walk
 // Any number: all threads, a thread per sequence.  line: units before each sequence, first_item: items before each.
 __device__ __noinline__ void plan_many(const PagedAttnParams& p, Control& c, long long* line, int* first_item) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_seq = p.n_sequences, grid = gridDim.x, me = blockIdx.x;
-    long long all = 0;
-    int items = 0, most = 0;
+    long long all = 0, items = 0;
+    int most = 0;
     if (tid == 0) c.most = 0, c.taken = c.before = 0;
 #pragma unroll 1
     for (int s0 = 0; s0 < n_seq; s0 += kPgThreads) {
@@ -378,8 +378,8 @@ __device__ __noinline__ void plan_many(const PagedAttnParams& p, Control& c, lon
         most = max(most, top);
         long long warp_cost, warp_items;
         long long before = lanes_before(cost, warp_cost);
-        int items_before = (int)lanes_before((long long)tiles * p.n_k_heads, warp_items);
-        if (lane == 0) c.warp_cost[warp] = warp_cost, c.warp_items[warp] = (int)warp_items;
+        long long items_before = lanes_before((long long)tiles * p.n_k_heads, warp_items);
+        if (lane == 0) c.warp_cost[warp] = warp_cost, c.warp_items[warp] = warp_items;
         plan_barrier();
         before += all, items_before += items;
 #pragma unroll 1
@@ -387,7 +387,8 @@ __device__ __noinline__ void plan_many(const PagedAttnParams& p, Control& c, lon
             if (w < warp) before += c.warp_cost[w], items_before += c.warp_items[w];
             all += c.warp_cost[w], items += c.warp_items[w];
         }
-        if (s < n_seq) line[s] = before, first_item[s] = items_before;
+        // (rounds take items from the first on: numbers past a few thousand are only compared)
+        if (s < n_seq) line[s] = before, first_item[s] = (int)min(items_before, 1ll << 30);
         plan_barrier();
     }
     const int parts = parts_of(all, items);
@@ -399,7 +400,7 @@ __device__ __noinline__ void plan_many(const PagedAttnParams& p, Control& c, lon
         if (lane == 0) atomicMax(&c.most, most);
         plan_barrier();
         const long long fair = bound(all, grid, 1) - 2 - (all >> 20);
-        rounds = (int)min((long long)min(kMaxRounds, items / grid), (long long)((float)fair / (float)c.most * 0.9999f));
+        rounds = (int)min(min((long long)kMaxRounds, items / grid), (long long)((float)fair / (float)c.most * 0.9999f));
         rounds = max(rounds, 0);
         long long mine = 0;
         if (tid < grid) {
@@ -981,11 +982,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             } else if (m == -INFINITY) {
                 a[t] = 0.0f;
             }
-            if (m == -INFINITY) l = 0.0f;
             const bool alone = g.starts && g.ends;
             const int piece = 2 * blockIdx.x + (g.starts ? 1 : 0);
             const int part_row = first + row;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = l > 0.0f ? 1.0f / l : l;       // 0: sees nothing; NaN: a score was NaN, and so is the row
             const long long out_row = g.q.row0 + token;
             const int h = g.head * p.share + in_seq - token * p.share;
             uint16_t* out = reinterpret_cast<uint16_t*>(p.out) + out_row * p.out_token + h * p.out_head;
@@ -1031,7 +1031,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 }
                 if (valid && (two || t == 0)) {
                     if (!alone) p.part_ml[(size_t)piece * kPagedRows + part_row] = make_float2(m, l);
-                    else if (p.lse) p.lse[out_row * p.n_q_heads + h] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                    else if (p.lse) p.lse[out_row * p.n_q_heads + h] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
                 }
             }
             if (!alone && tid == 0) {
@@ -1129,13 +1129,13 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p
     for (int t = 0; t < kTurns; ++t) {
         const int row = row0 + t * kRowsAtOnce + threadIdx.x % kRowsAtOnce;
         if (row >= first.rows) continue;
-        const float inv = l[t] > 0.0f ? 1.0f / l[t] : 0.0f;
+        const float inv = l[t] > 0.0f ? 1.0f / l[t] : l[t];
         const int in_seq = first.first_row + row, token = in_seq / p.share;
         const long long out_row = first.seq_row0 + token;
         const int h = first.head * p.share + in_seq - token * p.share;
         const uint2 w = make_uint2(pack_pair<F16>(o[t].x * inv, o[t].y * inv), pack_pair<F16>(o[t].z * inv, o[t].w * inv));
         *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + out_row * p.out_token + h * p.out_head + c4 * 4) = w;
-        if (p.lse && c4 == 0) p.lse[out_row * p.n_q_heads + h] = l[t] > 0.0f ? (m[t] + log2f(l[t])) * 0.6931471805599453f : -INFINITY;
+        if (p.lse && c4 == 0) p.lse[out_row * p.n_q_heads + h] = l[t] > 0.0f ? (m[t] + log2f(l[t])) * 0.6931471805599453f : (l[t] == 0.0f ? -INFINITY : l[t]);
     }
 }
 

@@ -261,3 +261,29 @@ def test_nothing_runs_while_a_status_is_set_and_all_does_afterwards():
     out, lse = B.regenvc_paged_attn_forward(*c["args"], lse=True)
     assert B.regenvc_device_status() == B.OK
     check(c, [1], [40], out, lse, 0, 0)
+
+
+@pytest.mark.parametrize("new,keys,group,d", [([300], [700], 1, 128), ([1, 1, 20], [9000, 40, 300], 1, 128), ([140, 3], [400, 90], 0, 64)])
+def test_what_is_not_a_number_stays_in_the_rows_that_see_it(new, keys, group, d):
+    hq, hk, page = 4, 2, 16
+    c = make(new, keys, hq, hk, d, page, BF, seed=5)
+    q, kc = c["args"][0], c["args"][1]
+    for row, head in ((0, 1), (new[0] - 1, 3), (sum(new) - 1, 0)):
+        c["q"][row, head] = math.nan
+    q.copy_(c["q"])
+    key = keys[-1] - 2                                       # of the last sequence, in one head of the cache
+    page_at, slot_at = slots_of(c["table"], len(keys) - 1, keys[-1], page)
+    kc[int(page_at[key]), int(slot_at[key]), 1, 3] = math.nan
+    c["k64"][-1][key, 1, 3] = math.nan
+    out, lse = B.regenvc_paged_attn_forward(*c["args"], group=group, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    at = 0
+    for s, (m, n) in enumerate(zip(new, keys)):
+        ref, ref_lse, bound, lse_bound = attend64(c["q"][at:at + m].double().to(DEV), c["k64"][s].to(DEV), c["v64"][s].to(DEV),
+                                                  sees(m, n, group, 0), 1 / math.sqrt(d), BF)
+        got, got_lse = out[at:at + m].double(), lse[at:at + m].double()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref)) and torch.equal(torch.isnan(got_lse), torch.isnan(ref_lse))
+        fine = ~torch.isnan(ref_lse)
+        assert fine.any() or m == 1
+        assert ((got - ref).abs() <= bound)[fine].all() and ((got_lse - ref_lse).abs() <= lse_bound)[fine].all()
+        at += m
