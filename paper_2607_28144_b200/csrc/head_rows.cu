@@ -7,11 +7,11 @@
 // slots and shared memory's ports.  The angles of a token are shared by all its heads, so a thread block computes them once per
 // token into shared memory.  A group of lanes then has one token and walks over its heads: addresses are two multiply-adds, and
 // angles and gains come in words without bank conflicts (a walk over (token, head) pairs whose lanes read gains 32 bytes apart
-// took 330 instructions and 65 shared wavefronts a vector, and 32 us where this takes 27).  One vector is in flight per group
+// took 330 instructions and 65 shared wavefronts a vector, and 32 us where this takes 26).  One vector is in flight per group
 // beside the one at hand, with four blocks on an SM: angles or gains held in registers over the walk spill (31 to 55 us), three
 // blocks 30 us, five 37.
-// Measured, 10920 tokens, 12 + 12 heads of 128, bf16: 27.0 us, 5.0 TB/s of what it has to move; with the values into a cache
-// of 1560-token pages 42.6 us, 4.7 TB/s; one token 3 us, 64 tokens appended 5 us (a chain of list, page and row behind a launch).
+// Measured, 10920 tokens, 12 + 12 heads of 128, bf16: 25.9 us, 5.2 TB/s of what it has to move (27.0 with one kernel for rows
+// and caches); with the values into a cache of 1560-token pages 42.1 us, 4.8 TB/s; one token 3 us, 64 tokens appended 5 us (a chain of list, page and row behind a launch).
 // Paged: token n of the call belongs to the sequence whose rows it lies in, found by counting the row starts at or before
 // it (a warp per token, all loads independent: a binary search is a chain of loads, which is what a call of a few tokens
 // would wait for); its slot is the sequence's length minus the rows behind it, its page comes from the table.
@@ -87,7 +87,7 @@ __device__ __forceinline__ bool locate(const HeadRowsParams& p, const Slots& s, 
     return true;
 }
 
-template <typename T, bool HALVES>
+template <typename T, bool HALVES, bool PAGED>
 __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
     extern __shared__ float4 shared_raw[];
     __shared__ Slots slots;
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid
     bool active = u < units && t < tokens;
     const Pieces at = pieces_of<HALVES>(p, u < units ? u : 0);
     const float inv_d = 1.0f / (float)p.head_dim;
-    if (p.paged) {
+    if (PAGED) {
         find_slots(p, slots, token0, tokens);
         __syncthreads();
         active = active && slots.rows[t];
@@ -118,11 +118,11 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid
     int h = group - t * step;                               // this group's next vector
     auto fetch = [&](Item& x) {
         x.to = nullptr;
-        x.of = (h >= q_heads) + (h >= qk_heads);
-        const long long slot = !p.paged || !x.of ? 0 : (x.of == 1 ? slots.k[t] : slots.v[t]);
+        x.of = (h >= q_heads) + (PAGED && h >= qk_heads);
+        const long long slot = !PAGED || !x.of ? 0 : (x.of == 1 ? slots.k[t] : slots.v[t]);
         if (active && h < all && slot >= 0) {
             const HeadRowsView& o = p.view[x.of];
-            const int token = token0 + t, head = h - (x.of == 0 ? 0 : (x.of == 1 ? q_heads : qk_heads));
+            const int token = token0 + t, head = h - (x.of == 0 ? 0 : (!PAGED || x.of == 1 ? q_heads : qk_heads));
             const T* v = reinterpret_cast<const T*>(o.from + (long long)token * o.from_token + (long long)head * o.from_head + lo_bytes);
             x.to = reinterpret_cast<T*>(o.to + (long long)token * o.to_token + (long long)head * o.to_head + lo_bytes) + slot;
             x.lo = load_raw8_once(v);
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid
 #pragma unroll
             for (int e = 0; e < 4; ++e) sq = fma2(v.b[e], v.b[e], fma2(v.a[e], v.a[e], sq));
             const float scale = rsqrtf(head_sum(sum2(sq), width) * inv_d + p.eps);
-            if (x.of < 2 && x.to) {
+            if ((!PAGED || x.of < 2) && x.to) {
                 const Unit gain = load_gains<HALVES>(reinterpret_cast<const ulonglong2*>(gains) + x.of * 4 * units + u, units);
                 const uint64_t r2 = pack2(scale, scale);
 #pragma unroll
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid
             }
         }
         if (!x.to) continue;
-        if (x.of == 2) {                                    // a copy, whatever the bits say
+        if (PAGED && x.of == 2) {                                    // a copy, whatever the bits say
             store_raw8(x.to, x.lo);
             store_raw8(x.to + hi_from_lo, x.hi);
             continue;
@@ -240,7 +240,8 @@ cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, cudaStream_t
     const int all = p.heads[0] + p.heads[1] + p.heads[2];
     const bool unit = in_units(p, vec, sizeof(T));
     const int width = unit ? lanes_of_head(p) : 32;
-    auto kernel = p.halves ? head_rows_kernel<T, true> : head_rows_kernel<T, false>;
+    auto kernel = p.halves ? (p.paged ? head_rows_kernel<T, true, true> : head_rows_kernel<T, true, false>)
+                           : (p.paged ? head_rows_kernel<T, false, true> : head_rows_kernel<T, false, false>);
     int per_sm = 1;
     p.tokens_per_cta = kMaxTokens;
     if (p.n_tokens > sm_count) {   // (a query takes longer than the kernel of a call of a few tokens)
