@@ -491,13 +491,19 @@ __device__ __forceinline__ void probabilities(const uint32_t* s, uint64_t scale2
     }
 }
 
-template <int D, bool F16>
+// Items of at most 16 rows (single tokens) have products of 64 rows instead of 128: the first 16 lie in lanes 0-15 of both
+// forms, and what the other lanes hold is nobody's.  They take the same time but less power, which is what holds long runs of
+// such calls: 64 streams at 600 calls in a row 528 -> 496 us, another GPU 495 -> 466 (the SM clock falls to 1.8 instead of
+// 1.65 GHz; the first ten calls take 462 us either way).  At 64 columns the form stays in the instructions: chosen at run time
+// it costs chunks 2 % (215 -> 220 us).
+constexpr int kFewRows = 16;
+template <int D, bool F16, int M>
 __device__ constexpr uint32_t idesc_qk() {
-    return F16 ? umma_idesc_f16_f32acc(128, 128) : umma_idesc_bf16_f32acc(128, 128);
+    return F16 ? umma_idesc_f16_f32acc(M, 128) : umma_idesc_bf16_f32acc(M, 128);
 }
-template <int D, bool F16>
+template <int D, bool F16, int M>
 __device__ constexpr uint32_t idesc_pv() {
-    return (F16 ? umma_idesc_f16_f32acc(128, D) : umma_idesc_bf16_f32acc(128, D)) | (1u << 16);   // V: MN-major
+    return (F16 ? umma_idesc_f16_f32acc(M, D) : umma_idesc_bf16_f32acc(M, D)) | (1u << 16);   // V: MN-major
 }
 // V's tile as an MN-major operand: the 64 columns of a block are one 128-byte row per key, eight keys to 1024 bytes; the
 // next 64 columns lie a block of 16 KB on.
@@ -506,19 +512,19 @@ __device__ __forceinline__ uint64_t desc_v(uint32_t addr) {
            (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
 template <int D, bool F16>
-__device__ __forceinline__ void products_qk(uint32_t s_tmem, uint32_t q, uint32_t k, uint32_t elected) {
+__device__ __forceinline__ void products_qk(uint32_t s_tmem, uint32_t q, uint32_t k, uint32_t idesc, uint32_t elected) {
     const uint64_t a = umma_smem_desc_k_sw128(q), b = umma_smem_desc_k_sw128(k);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
         const uint64_t off = (i >> 2) * (16384 >> 4) + (i & 3) * 2;
-        umma_ss_elect(s_tmem, a + off, b + off, idesc_qk<D, F16>(), i > 0, elected);
+        umma_ss_elect(s_tmem, a + off, b + off, idesc, i > 0, elected);
     }
 }
 template <int D, bool F16>
-__device__ __forceinline__ void products_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v, bool accumulate, uint32_t elected) {
+__device__ __forceinline__ void products_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v, uint32_t idesc, bool accumulate, uint32_t elected) {
     const uint64_t b = desc_v(v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) umma_ts_elect(o_tmem, p_tmem + i * 8, b + i * (2048 >> 4), idesc_pv<D, F16>(), accumulate || i > 0, elected);
+    for (int i = 0; i < 8; ++i) umma_ts_elect(o_tmem, p_tmem + i * 8, b + i * (2048 >> 4), idesc, accumulate || i > 0, elected);
 }
 
 template <int D>
@@ -707,8 +713,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 // Steps: stream 0 and 1 in turn.  Step i's scores go to buffer i % kScores, as soon as the probabilities of
                 // the step that had it are used up.
                 uint32_t put = 0, used = 0, phase = 0;   // next buffer to fill, to use; its parity
+                uint32_t idesc_s = 0, idesc_o = 0;
                 auto scores = [&](uint32_t q, uint32_t k_slot) {
-                    products_qk<D, F16>(tmem_base + put * 128, q, ring_addr + k_slot * S::kTileB, elected);
+                    products_qk<D, F16>(tmem_base + put * 128, q, ring_addr + k_slot * S::kTileB, idesc_s, elected);
                     umma_commit_elect(smem_u32(&c->s_full[put]), elected);
                     if (++put == S::kScores) put = 0;
                 };
@@ -716,7 +723,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     if (!__all_sync(0xffffffffu, wait(&c->p_full[used], phase))) return false;
                     tc_fence_after();
                     products_pv<D, F16>(tmem_base + S::kOut + t * D, tmem_base + used * 128,
-                                        ring_addr + (S::kKeySlots + v_slot) * S::kTileB, accumulate, elected);
+                                        ring_addr + (S::kKeySlots + v_slot) * S::kTileB, idesc_o, accumulate, elected);
                     if (++used == S::kScores) used = 0, phase ^= 1;
                     return true;
                 };
@@ -728,6 +735,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     const Segment* at = &c->seg[segment % kSegments];
                     const bool two = at->rows > 128;
                     const int n = at->n, steps = two ? 2 * n : n;
+                    const bool few_rows = D == 128 && at->rows <= kFewRows;
+                    idesc_s = few_rows ? idesc_qk<D, F16, 64>() : idesc_qk<D, F16, 128>();
+                    idesc_o = few_rows ? idesc_pv<D, F16, 64>() : idesc_pv<D, F16, 128>();
                     __syncwarp();
                     if (elected) mbar_arrive(smem_u32(&c->seg_empty[segment % kSegments]));
                     if (n == 0) break;
@@ -849,7 +859,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
             // tiles that all rows of the warp see whole
             const int open0 = (__reduce_max_sync(0xffffffffu, max(lo, 0)) + 127) / 128, open1 = __reduce_min_sync(0xffffffffu, max(hi, 0)) / 128;
-            float m = -INFINITY, l = 0.0f;
+            float m = valid ? -INFINITY : 0.0f, l = 0.0f;    // (what is not a row never asks for another reference)
             bool fresh = true;                               // some row of the warp has not seen a key yet
             int done = 0;                                    // tiles of this stream
 #pragma unroll 1
@@ -917,7 +927,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         float s0, s1;
                         unpack2(add2(sum_a, sum_b), s0, s1);
                         sum = s0 + s1;
-                        again = !(sum < raise_at<F16>());
+                        again = valid && !(sum < raise_at<F16>());
                         if (!__any_sync(0xffffffffu, again)) break;
                         // Rare: scores far above the reference.  O and the sum are brought to the new reference, and the tile
                         // is done again.
