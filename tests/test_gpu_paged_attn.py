@@ -287,3 +287,18 @@ def test_what_is_not_a_number_stays_in_the_rows_that_see_it(new, keys, group, d)
         assert fine.any() or m == 1
         assert ((got - ref).abs() <= bound)[fine].all() and ((got_lse - ref_lse).abs() <= lse_bound)[fine].all()
         at += m
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hq,hk", [(1, 1), (4, 1), (8, 2)])
+def test_items_of_about_sixteen_rows(dtype, hq, hk):
+    """Products of 64 and of 128 rows in turn in a thread block; a first call leaves NaN in lanes that are nobody's."""
+    new, keys = [16, 17, 4, 5, 1, 40], [700, 300, 2000, 129, 5000, 41]
+    hot = make([256], [256], hq, hk, 128, 16, dtype, seed=7)
+    hot["args"][0].fill_(math.nan)
+    B.regenvc_paged_attn_forward(*hot["args"], group=0)
+    for heat, group in ((1.0, 1), (40.0, 0)):
+        c = make(new, keys, hq, hk, 128, 16, dtype, seed=11, heat=heat)
+        out, lse = B.regenvc_paged_attn_forward(*c["args"], group=group, lse=True)
+        assert B.regenvc_device_status() == B.OK
+        check(c, new, keys, out, lse, group, 0)
