@@ -43,8 +43,10 @@ __device__ __forceinline__ void find_slots(const HeadRowsParams& p, Slots& s, in
             long long k = -1, v = -1;
             const bool row = seq >= 0 && seq < p.n_sequences;
             if (row) {
-                const long long at = (long long)p.lengths[seq] - (p.row_starts[seq + 1] - n);
-                bool good = at >= 0 && at < (long long)p.pages_per_sequence * p.page_size;
+                // (starts that do not ascend may count a row to a sequence that does not have it)
+                const int first = p.row_starts[seq], end = p.row_starts[seq + 1];
+                const long long at = (long long)p.lengths[seq] - ((long long)end - n);
+                bool good = first <= n && n < end && end <= p.n_tokens && at >= 0 && at < (long long)p.pages_per_sequence * p.page_size;
                 if (good) {
                     const int slot = (int)(at / p.page_size), in_page = (int)(at - (long long)slot * p.page_size);
                     const int page = p.table[seq * p.table_stride + slot];
@@ -60,6 +62,16 @@ __device__ __forceinline__ void find_slots(const HeadRowsParams& p, Slots& s, in
             s.v[t] = v;
             s.rows[t] = row;
         }
+    }
+}
+
+// Lists that contradict each other or the call's sizes, wherever the rows lie that they leave without a place: reported by the
+// first block.  The last warps begin, which have no row to look up where a block has fewer than eight.
+__device__ __forceinline__ void check_lists(const HeadRowsParams& p) {
+    for (int s = blockDim.x - 1 - threadIdx.x; s < p.n_sequences; s += blockDim.x) {
+        const int first = p.row_starts[s], end = p.row_starts[s + 1], keys = p.lengths[s];
+        if (first < 0 || end < first || end > p.n_tokens || keys < end - first || keys > (long long)p.pages_per_sequence * p.page_size)
+            atomicCAS(p.status, 0, kStatusRange);
     }
 }
 
@@ -103,6 +115,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid
     const float inv_d = 1.0f / (float)p.head_dim;
     if (PAGED) {
         find_slots(p, slots, token0, tokens);
+        if (blockIdx.x == 0) check_lists(p);
         __syncthreads();
         active = active && slots.rows[t];
     }
@@ -182,7 +195,10 @@ __global__ void __launch_bounds__(kHeadThreads) head_rows_element_kernel(const _
     const int lane = threadIdx.x & 31, all = p.heads[0] + p.heads[1] + p.heads[2];
     const int units = p.head_dim - p.n_pairs;
     if (p.n_axes) fill_table<kPlain>(p, table, pitch, token0, tokens, false);
-    if (p.paged) find_slots(p, slots, token0, tokens);
+    if (p.paged) {
+        find_slots(p, slots, token0, tokens);
+        if (blockIdx.x == 0) check_lists(p);
+    }
     __syncthreads();
     for (int i = threadIdx.x >> 5; i < tokens * all; i += blockDim.x >> 5) {
         const int t = i / all;
