@@ -24,13 +24,17 @@
 // K comes as [keys][64 columns] blocks with the 128-byte swizzle, which is a K-major operand of Q K^T, V in the same form,
 // which is an MN-major operand of P V: neither is rewritten.
 //
-// Softmax: a row's reference is its maximum over the first tile in which it sees a key.  No later maximum is taken: a
+// Softmax: a row's reference is set by its maximum over the first tile in which it sees a key.  No later maximum is taken: a
 // tile's probabilities are formed against the reference, and only if their sum leaves the range of the probabilities' type
 // (65504) or 2^32 (bf16, whose range is fp32's) the reference is raised, O rescaled and the tile done again.  A larger
 // probability costs no precision, it has as many bits as one below 1.
-// Scores, sums, O are fp32; probabilities are rounded to the cache's type, which the product P V takes both operands in
-// (half a step of 2^-9 or 2^-12 each, independent from key to key).  Keys that no row of the item sees (behind the length,
-// before the window) are zeroed in V's tile, so that what lies there does not reach a sum as 0 * NaN.
+// Scores, sums, O are fp32; probabilities are rounded to the cache's type, which the product P V takes both operands in: off
+// by up to 2^-8 (bf16) or 2^-11 (fp16) of one, independent from key to key.  fp16 ends at steps of 2^-24, where errors are not
+// independent: many keys alike far below the reference all lose, or gain, the same.  Its reference lies 2^8 below the maximum
+// (128 such probabilities sum to 2^15), so that what vanishes is below 2^-33 of the largest weight: 10^6 such keys weigh 1.2e-4
+// of it (3 % with the maximum as reference).  Time as with the maximum (nine chunks and tokens: 214.8 and 214.4 us).
+// Keys that no row of the item sees (behind the length, before the window) are zeroed in V's tile, so that what lies there does
+// not reach a sum as 0 * NaN.
 //
 // Work: the units (item, key tile) form one line, cut into equal parts for the thread blocks; an item that is cut leaves
 // unnormalised pieces which a second kernel joins in order.  Where several tiles of rows share a head's keys, whole items
@@ -53,6 +57,9 @@ constexpr int kMaxRounds = 64;
 // Sums of 128 probabilities from which on a row's reference is set anew: far inside what the probabilities' type holds.
 template <bool F16>
 __device__ constexpr float raise_at() { return F16 ? 65504.0f : 4294967296.0f; }
+// Powers of two by which a row's reference lies below the maximum that sets it.
+template <bool F16>
+__device__ constexpr float below_top() { return F16 ? 8.0f : 0.0f; }
 
 template <int D>
 struct Shape {
@@ -906,10 +913,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             for (int b = 0; b < 4; ++b) mx[b] = max3(mx[b], __uint_as_float(s[i + 2 * b]), __uint_as_float(s[i + 2 * b + 1]));
                         return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                     };
-                    // rows that have not seen a key yet take the tile's maximum for their reference
+                    // rows that have not seen a key yet take their reference from the tile's maximum
                     bool again;
                     if (fresh) {
-                        const float top = highest();
+                        const float top = highest() - below_top<F16>();
                         if (m == -INFINITY) m = top;
                         fresh = __any_sync(0xffffffffu, m == -INFINITY);
                     }
@@ -931,7 +938,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                         if (!__any_sync(0xffffffffu, again)) break;
                         // Rare: scores far above the reference.  O and the sum are brought to the new reference, and the tile
                         // is done again.
-                        const float top = highest();
+                        const float top = highest() - below_top<F16>();
                         again = again && top > m;            // (a NaN among the scores stays one)
                         if (!__any_sync(0xffffffffu, again)) break;
                         const float alpha = again ? ex2_approx(ref - top) : 1.0f;
