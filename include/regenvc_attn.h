@@ -331,7 +331,7 @@ int regenvc_qk_norm_rope_backward(const regenvc_qk_norm_rope_desc* desc, const v
  *   A NaN in q or in a key makes the rows that see it NaN (lse too), and no others.
  *   page_size: a multiple of 8 (REGENVC_ERR_UNSUPPORTED); rows of q, out and the caches allow 16-byte accesses
  *   (REGENVC_ERR_MISALIGNED).  Probabilities are rounded to the cache's type, everything else is fp32; in fp16 a key of less
- *   than 2^-33 of the row's largest weight counts in lse only.
+ *   than 2^-33 of the row's largest weight counts in lse only, in bf16 values below 2^-85 lose bits.
  *   workspace : regenvc_paged_attn_workspace_bytes() bytes (0 for invalid arguments), 16-byte aligned, its content of no
  *            matter; calls that may overlap on the GPU (and graphs that may be replayed at a time) need one each
  *   Waits inside are bounded as in the other attention kernels.  The same call on the same lengths gives the same bits.

@@ -26,13 +26,16 @@
 //
 // Softmax: a row's reference is set by its maximum over the first tile in which it sees a key.  No later maximum is taken: a
 // tile's probabilities are formed against the reference, and only if their sum leaves the range of the probabilities' type
-// (65504) or 2^32 (bf16, whose range is fp32's) the reference is raised, O rescaled and the tile done again.  A larger
-// probability costs no precision, it has as many bits as one below 1.
+// (fp16: 65504) or reaches 1 (bf16) the reference is raised, O rescaled and the tile done again.  A larger probability costs no
+// precision, it has as many bits as one below 1.
 // Scores, sums, O are fp32; probabilities are rounded to the cache's type, which the product P V takes both operands in: off
 // by up to 2^-8 (bf16) or 2^-11 (fp16) of one, independent from key to key.  fp16 ends at steps of 2^-24, where errors are not
 // independent: many keys alike far below the reference all lose, or gain, the same.  Its reference lies 2^8 below the maximum
 // (128 such probabilities sum to 2^15), so that what vanishes is below 2^-33 of the largest weight: 10^6 such keys weigh 1.2e-4
 // of it (3 % with the maximum as reference).  Time as with the maximum (nine chunks and tokens: 214.8 and 214.4 us).
+// bf16 has fp32's range: its reference lies 2^32 above the maximum, so that probabilities and their sums stay below 1 and O is
+// finite for whatever finite values, up to bf16's largest (formed against the maximum itself, with 2^32 for scores to rise, it
+// overflowed from 2^95 on).  What pays are values below 2^-85, whose products leave fp32's normal range.
 // Keys that no row of the item sees (behind the length, before the window) are zeroed in V's tile, so that what lies there does
 // not reach a sum as 0 * NaN.
 //
@@ -54,12 +57,19 @@ static_assert(kPgSoftmaxRegs * kPgSoftmax + kPgControlRegs * 128 <= kPgLaunchReg
 constexpr int kPgMmaWarp = 8, kPgKeyWarp = 9, kPgWalkWarp = 10, kPgValueWarp = 11;
 constexpr int kSegments = 4;      // stretches of work handed to the warps ahead
 constexpr int kMaxRounds = 64;
-// Sums of 128 probabilities from which on a row's reference is set anew: far inside what the probabilities' type holds.
+// Sums of 128 probabilities from which on a row's reference is set anew.
 template <bool F16>
-__device__ constexpr float raise_at() { return F16 ? 65504.0f : 4294967296.0f; }
+__device__ constexpr float raise_at() { return F16 ? 65504.0f : 1.0f; }
 // Powers of two by which a row's reference lies below the maximum that sets it.
 template <bool F16>
-__device__ constexpr float below_top() { return F16 ? 8.0f : 0.0f; }
+__device__ constexpr float below_top() { return F16 ? 8.0f : -32.0f; }
+// Natural logarithm of a row's sum l against its reference m; both are brought near to the maximum first, where their parts
+// are small.
+template <bool F16>
+__device__ __forceinline__ float log_sum(float m, float l) {
+    constexpr float back = F16 ? 1.0f / 256.0f : 4294967296.0f;   // 2^-below_top
+    return l > 0.0f ? ((m + below_top<F16>()) + log2f(l * back)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
+}
 
 template <int D>
 struct Shape {
@@ -1048,7 +1058,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 }
                 if (valid && (two || t == 0)) {
                     if (!alone) p.part_ml[(size_t)piece * kPagedRows + part_row] = make_float2(m, l);
-                    else if (p.lse) p.lse[out_row * p.n_q_heads + h] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : (l == 0.0f ? -INFINITY : l);
+                    else if (p.lse) p.lse[out_row * p.n_q_heads + h] = log_sum<F16>(m, l);
                 }
             }
             if (!alone && tid == 0) {
@@ -1152,7 +1162,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p
         const int h = first.head * p.share + in_seq - token * p.share;
         const uint2 w = make_uint2(pack_pair<F16>(o[t].x * inv, o[t].y * inv), pack_pair<F16>(o[t].z * inv, o[t].w * inv));
         *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + out_row * p.out_token + h * p.out_head + c4 * 4) = w;
-        if (p.lse && c4 == 0) p.lse[out_row * p.n_q_heads + h] = l[t] > 0.0f ? (m[t] + log2f(l[t])) * 0.6931471805599453f : (l[t] == 0.0f ? -INFINITY : l[t]);
+        if (p.lse && c4 == 0) p.lse[out_row * p.n_q_heads + h] = log_sum<F16>(m[t], l[t]);
     }
 }
 

@@ -119,3 +119,23 @@ def test_a_strong_key_anywhere(dtype, at):
     for gap in (7.0, 9.0, 15.0, 17.0, 24.0, 33.0, 60.0):
         k[at, 0, 0] = gap
         check(q, k, randn(keys, 1, d, dtype=dtype, seed=4), group=0, scale=math.log(2.0))
+
+
+@pytest.mark.parametrize("step", [0.5, 3.0, 7.0, 12.0, 20.0, 30.0])
+@pytest.mark.parametrize("new,d", [(1, 128), (140, 128), (140, 64)])
+def test_large_values_under_rising_scores(step, new, d):
+    """bf16 values of 10^38: the result is a mean of them and finite, whatever the sums on the way there are."""
+    keys = 2000
+    q, k = torch.zeros(new, 1, d, dtype=BF, device=DEV), torch.zeros(keys, 1, d, dtype=BF, device=DEV)
+    q[..., 0], k[:, 0, 0] = 1.0, (torch.arange(keys, device=DEV) // 200 * step).to(BF)
+    v = (1 + randn(keys, 1, d, dtype=torch.float32, seed=5).abs().clamp(max=1.9)) * 1e38
+    out, _ = check(q, k, v.to(BF), group=0, scale=math.log(2.0))
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("new,d", [(1, 128), (140, 128), (140, 64)])
+def test_small_values(new, d):
+    """bf16 values of 2^-80: their products with probabilities are in fp32's range."""
+    keys = 2000
+    v = (randn(keys, 1, d, dtype=torch.float32, seed=5) * 2.0 ** -80).to(BF)
+    check(randn(new, 1, d, dtype=BF, seed=6) * 2, randn(keys, 1, d, dtype=BF, seed=7), v, group=0)
