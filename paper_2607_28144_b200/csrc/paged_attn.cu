@@ -1094,12 +1094,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 // rows.  The pieces are this one and the ones that the following thread blocks left in their slot 0, up to the one that ends
 // the item, in that order.  Bound by latencies (the blocks start when the attention's have left the SMs, whose registers are
 // all taken): the descriptions of all pieces are read at once, and the pieces of four rows side by side.
-constexpr int kJoinRows = 32;
+constexpr int kJoinRows = 32, kJoinThreads = 256;
 template <int D, bool F16>
-__global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p, const int grid) {
-    constexpr int kRowsAtOnce = 256 / (D / 4), kTurns = kJoinRows / kRowsAtOnce;
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAttnParams p, const int grid) {
+    constexpr int kRowsAtOnce = kJoinThreads / (D / 4), kTurns = kJoinRows / kRowsAtOnce;
+    constexpr int kWarps = kJoinThreads / 32;
+    static_assert(kPagedMaxGrid <= 32 * kWarps, "a thread per piece");
     __shared__ int slots[kPagedMaxGrid + 1];
-    __shared__ uint32_t valid_at[kPagedMaxGrid / 32 + 1], ends_at[kPagedMaxGrid / 32 + 1];
+    __shared__ uint32_t valid_at[kWarps], ends_at[kWarps];
     __shared__ int n_pieces;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int row0 = blockIdx.y * kJoinRows, next = blockIdx.x + 1 + threadIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1108,7 +1110,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnParams p
     if (next < grid) valid = p.pieces[2 * next].valid, ends = p.pieces[2 * next].ends;
     if (!first.valid || row0 >= first.rows) return;
     const uint32_t v = __ballot_sync(0xffffffffu, valid), e = __ballot_sync(0xffffffffu, valid && ends);
-    if (lane == 0 && warp <= kPagedMaxGrid / 32) valid_at[warp] = v, ends_at[warp] = e;
+    if (lane == 0) valid_at[warp] = v, ends_at[warp] = e;
     if (threadIdx.x == 0) n_pieces = 0;
     __syncthreads();
     {   // this thread's piece, if it is one of the item's: the valid ones before it, and none of those ends the item
@@ -1183,7 +1185,7 @@ cudaError_t launch_one(const PagedMaps& maps, const PagedAttnParams& p, int grid
     *launches = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid, (unsigned)(kPagedRows / kJoinRows));
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;

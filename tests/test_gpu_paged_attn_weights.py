@@ -139,3 +139,31 @@ def test_small_values(new, d):
     keys = 2000
     v = (randn(keys, 1, d, dtype=torch.float32, seed=5) * 2.0 ** -80).to(BF)
     check(randn(new, 1, d, dtype=BF, seed=6) * 2, randn(keys, 1, d, dtype=BF, seed=7), v, group=0)
+
+
+@pytest.mark.parametrize("new,keys,hq,hk,d", [([256], [40000], 1, 1, 128), ([129], [38000], 1, 1, 128), ([16], [80000], 1, 1, 64),
+                                              ([200, 1], [25000, 19000], 2, 1, 64)])
+def test_items_cut_over_every_thread_block(new, keys, hq, hk, d):
+    """One item's pieces lie in all the blocks; every row of the join against the definition."""
+    q = randn(sum(new), hq, d, dtype=BF, seed=6)
+    k, v = (randn(sum(keys), hk, d, dtype=BF, seed=s) for s in (7, 8))
+    page = 8
+    need = [-(-m // page) for m in keys]
+    caches = [torch.full((sum(need), page, hk, d), math.nan, dtype=BF, device=DEV) for _ in range(2)]
+    table, at, row = torch.zeros((len(new), max(need)), dtype=torch.int32, device=DEV), 0, 0
+    for s, (m, n) in enumerate(zip(keys, need)):
+        table[s, :n] = torch.arange(at, at + n, device=DEV)
+        for c, t in zip(caches, (k, v)):
+            c[at:at + n].view(-1, hk, d)[:m] = t[row:row + m]
+        at, row = at + n, row + m
+    starts = [sum(new[:i]) for i in range(len(new) + 1)]
+    out, lse = B.regenvc_paged_attn_forward(q, *caches, table, torch.tensor(keys, dtype=torch.int32, device=DEV),
+                                            torch.tensor(starts, dtype=torch.int32, device=DEV), group=1, lse=True)
+    assert B.regenvc_device_status() == B.OK
+    row = 0
+    for s, (m, n) in enumerate(zip(new, keys)):
+        part = slice(starts[s], starts[s] + m)
+        ref, ref_lse, bound, lse_bound = definition(q[part], k[row:row + n], v[row:row + n], 1, 1 / math.sqrt(d))
+        assert ((out[part].double() - ref).abs() <= bound).all()
+        assert ((lse[part].double() - ref_lse).abs() <= lse_bound).all()
+        row += n
