@@ -836,12 +836,12 @@ def _cache(t, name: str, dtype, like=None):
     pages, slots, heads, d = t.shape
     strides = list(t.stride()[:3])
     for i, count in enumerate((pages, slots, heads)):
-        if count == 1:                     # never used: behind everything else
-            strides[i] = 0
+        if count == 1:                     # never used: a short one for heads and slots, behind everything else for pages
+            strides[i] = -(-d // 8) * 8 if i else 0
         elif strides[i] < d:
             raise ValueError(f"{name} has vectors that overlap (an expanded tensor?)")
-    top = max([d] + [s * c for s, c in zip(strides, (pages, slots, heads))])
-    return tuple(s or -(-top // 8) * 8 for s in strides)
+    top = max(d, strides[1] * slots, strides[2] * heads)
+    return strides[0] or -(-top // 8) * 8, strides[1], strides[2]
 
 
 def _paged_lists(block_table, lengths, row_starts):

@@ -77,7 +77,8 @@ bool clear_of(const HeadView& out, const HeadView* ins, int n, const HeadView* i
     return true;
 }
 
-// A cache [pages][slots][heads][head_dim] in any order of its strides: vectors do not share memory.
+// A cache [pages][slots][heads][head_dim] in any order of its strides: vectors do not share memory.  The stride of an axis with
+// one entry is never used and taken as a short one.
 struct CacheView {
     long long page, slot, head, in_page;   // in_page: elements from a page's first to one past its last
     Span span;
@@ -87,6 +88,10 @@ int cache_of(const void* ptr, long long page, long long slot, long long head, in
     c->head = head ? head : head_dim;
     c->slot = slot ? slot : (long long)heads * head_dim;
     c->page = page ? page : (long long)page_size * heads * head_dim;
+    const long long unused = (head_dim + 7) / 8 * 8;
+    if (heads == 1) c->head = unused;
+    if (page_size == 1) c->slot = unused;
+    if (n_pages == 1) c->page = unused;
     if (c->head < head_dim || c->head > kMaxStride || c->slot < head_dim || c->slot > kMaxStride || c->page < head_dim ||
         c->page > kMaxPageStride)
         return REGENVC_ERR_BAD_SHAPE;
@@ -306,11 +311,12 @@ int regenvc_paged_append(const regenvc_paged_append_desc* d, const void* q, cons
         const bool k_first = (const char*)k_cache < (const char*)v_cache;
         const CacheView &low = k_first ? cache[0] : cache[1], &high = k_first ? cache[1] : cache[0];
         const long long gap = ((const char*)high.span.p - (const char*)low.span.p) / (long long)size;
-        const bool by_page = low.page == high.page && gap >= low.in_page && gap + high.in_page <= low.page;
+        const bool one = d->n_pages == 1;
+        const bool by_page = low.page == high.page && gap >= low.in_page && (one || gap + high.in_page <= low.page);
         // or a slot's key beside its value
         const long long low_slot = (d->n_k_heads - 1) * low.head + d->head_dim, high_slot = (d->n_k_heads - 1) * high.head + d->head_dim;
         const bool by_slot = low.page == high.page && low.slot == high.slot && gap >= low_slot && gap + high_slot <= low.slot &&
-                             low.page >= (d->page_size - 1) * low.slot + low.slot;
+                             (one || low.page >= (d->page_size - 1) * low.slot + low.slot);
         if (!by_page && !by_slot) return REGENVC_ERR_ALIASING;
     }
     for (int i = 0; i < 3; ++i) {

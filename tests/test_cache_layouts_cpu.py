@@ -1,0 +1,42 @@
+"""Host-side checks of cache layouts and scales of the operators over cached windows.  Every call is refused."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2607_28144_b200 import binding as B
+from paper_2607_28144_b200 import build
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build()
+    return B.lib()
+
+
+A = [0x100000000 * (i + 1) for i in range(24)]   # far apart, never dereferenced: every call below must fail
+
+
+def append(L, kc, vc, q_out=A[9], **kw):
+    d = dict(n_tokens=5, n_q_heads=4, n_k_heads=2, head_dim=64, type=0, n_sequences=3, page_size=16, n_pages=10, pages_per_sequence=4)
+    d.update(kw)
+    return L.regenvc_paged_append(ctypes.byref(B.PagedAppendDesc(**d)), A[0], A[1], A[2], None, None, None, A[6], A[7], A[8], q_out, kc, vc, None)
+
+
+def test_strides_of_axes_with_one_entry_are_not_looked_at(L):
+    """Refused for what comes later (keys given as the cache), not for a stride that no address uses."""
+    for kw in (dict(n_k_heads=1, k_cache_head_stride=1 << 33, v_cache_head_stride=3), dict(page_size=1, k_slot_stride=1 << 33, v_slot_stride=8),
+               dict(n_pages=1, k_page_stride=1 << 40, v_page_stride=1)):
+        assert append(L, A[1], A[11], **kw) == B.ERR_ALIASING, kw
+    for kw in (dict(k_cache_head_stride=1 << 33), dict(k_slot_stride=1 << 33), dict(k_page_stride=1 << 40)):
+        assert append(L, A[1], A[11], **kw) == B.ERR_BAD_SHAPE, kw
+
+
+def test_the_binding_names_short_strides_for_axes_with_one_entry():
+    """Views of one tensor of 2^32 elements: (page, slot, head) strides that the library takes."""
+    both = torch.empty((1 << 20, 2, 16, 1, 128), dtype=torch.bfloat16, device="meta")
+    assert B._cache(both[:, 0], "k_cache", torch.bfloat16) == (4096, 128, 128)
+    both = torch.empty((1 << 20, 2, 1, 16, 128), dtype=torch.bfloat16, device="meta")
+    assert B._cache(both[:, 1], "v_cache", torch.bfloat16) == (4096, 128, 128)
+    one = torch.empty((1, 2, 1 << 20, 16, 128), dtype=torch.bfloat16, device="meta")
+    assert B._cache(one[:, :, :, :8][:, 1], "v_cache", torch.bfloat16)[1:] == (2048, 128)
