@@ -301,8 +301,9 @@ int regenvc_qk_norm_rope_backward(const regenvc_qk_norm_rope_desc* desc, const v
  * attend to them: a paged cache for any number of streams, and attention over it.
  *
  * The cache is two tensors of pages, keys and values: element (page, slot, head, i) at page * page_stride + slot *
- * slot_stride + head * head_stride + i, in any order of the strides (0: packed [pages][slots][heads][head_dim]).  Token t of
- * sequence s lies in slot t % page_size of page block_table[s * table_stride + t / page_size].
+ * slot_stride + head * head_stride + i, in any order of the strides (0: packed [pages][slots][heads][head_dim]; of an axis
+ * with one entry: of no matter).  Both may be views of one tensor that holds a page's, a slot's or a head's keys beside its
+ * values.  Token t of sequence s lies in slot t % page_size of page block_table[s * table_stride + t / page_size].
  *   row_starts : int32 [n_sequences + 1], ascending; rows row_starts[s] .. row_starts[s + 1] - 1 of the call's tensors are
  *                sequence s's new tokens (none: equal); rows behind the last sequence (a padded batch) are left as they were
  *   lengths    : int32 [n_sequences], cached tokens of each sequence with the new ones, which are the last of them

@@ -1,7 +1,5 @@
 // Entry points of the operators of attention over cached windows: queries and keys normalised and rotated, appending to a
 // paged cache, attention over it.  Arguments are checked before any CUDA call; nothing is allocated.
-#include <algorithm>
-
 #include "head_rows.cuh"
 #include "op_checks.cuh"
 #include "paged_attn.cuh"
@@ -95,17 +93,10 @@ int cache_of(const void* ptr, long long page, long long slot, long long head, in
     if (c->head < head_dim || c->head > kMaxStride || c->slot < head_dim || c->slot > kMaxStride || c->page < head_dim ||
         c->page > kMaxPageStride)
         return REGENVC_ERR_BAD_SHAPE;
-    struct Axis {
-        long long stride, count;
-    } axes[3] = {{c->head, heads}, {c->slot, page_size}, {c->page, n_pages}};
     c->in_page = (heads - 1) * c->head + (page_size - 1) * c->slot + head_dim;
-    std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+    Axis axes[3] = {{c->head, heads}, {c->slot, page_size}, {c->page, n_pages}};
     long long extent = head_dim;
-    for (const Axis& a : axes) {
-        if (a.count == 1) continue;
-        if (a.stride < extent) return REGENVC_ERR_BAD_SHAPE;
-        extent += (a.count - 1) * a.stride;
-    }
+    if (!nested(axes, 3, &extent)) return REGENVC_ERR_BAD_SHAPE;
     c->span = Span{ptr, (size_t)extent * size};
     return REGENVC_OK;
 }
@@ -307,17 +298,20 @@ int regenvc_paged_append(const regenvc_paged_append_desc* d, const void* q, cons
         if (meet(cache[w].span, out.span)) return REGENVC_ERR_ALIASING;
     }
     if (meet(cache[0].span, cache[1].span)) {
-        // one tensor with a page's keys beside its values: clear of one another inside the pages' stride
+        // One tensor with keys beside values: a pair of them is one more axis, in any place among the others; or a page's or a
+        // slot's keys lie in front of its values, in orders of their own.
         const bool k_first = (const char*)k_cache < (const char*)v_cache;
         const CacheView &low = k_first ? cache[0] : cache[1], &high = k_first ? cache[1] : cache[0];
         const long long gap = ((const char*)high.span.p - (const char*)low.span.p) / (long long)size;
-        const bool one = d->n_pages == 1;
-        const bool by_page = low.page == high.page && gap >= low.in_page && (one || gap + high.in_page <= low.page);
-        // or a slot's key beside its value
-        const long long low_slot = (d->n_k_heads - 1) * low.head + d->head_dim, high_slot = (d->n_k_heads - 1) * high.head + d->head_dim;
-        const bool by_slot = low.page == high.page && low.slot == high.slot && gap >= low_slot && gap + high_slot <= low.slot &&
-                             (one || low.page >= (d->page_size - 1) * low.slot + low.slot);
-        if (!by_page && !by_slot) return REGENVC_ERR_ALIASING;
+        Axis axes[4] = {{low.head, d->n_k_heads}, {low.slot, d->page_size}, {low.page, d->n_pages}, {gap, 2}};
+        long long extent = d->head_dim;
+        const bool alike = low.head == high.head && low.slot == high.slot && low.page == high.page && nested(axes, 4, &extent);
+        const bool by_page = low.page == high.page && gap >= low.in_page && gap + high.in_page <= low.page;
+        const int heads_behind = d->n_k_heads - 1;
+        axes[0] = {low.slot, d->page_size}, axes[1] = {low.page, d->n_pages};
+        extent = gap + heads_behind * high.head + d->head_dim;
+        const bool by_slot = low.slot == high.slot && low.page == high.page && gap >= heads_behind * low.head + d->head_dim && nested(axes, 2, &extent);
+        if (!alike && !by_page && !by_slot) return REGENVC_ERR_ALIASING;
     }
     for (int i = 0; i < 3; ++i) {
         p.in[i] = in[i].p;

@@ -1,6 +1,7 @@
 // Checks of arguments shared by the entry points beside the attention (host code): alignment, overlap of strided operands,
 // vectors that do not share memory, the ladder of a rotation's frequencies.
 #pragma once
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/regenvc_attn.h"
@@ -41,6 +42,21 @@ inline bool head_strides(long long token_in, long long head_in, long long tokens
     *token = token_in ? token_in : (long long)heads * head_dim;
     if (*head < head_dim || *head > kMaxStride || *token < head_dim || *token > kMaxStride) return false;
     return *token >= (heads - 1) * *head + head_dim || *head >= (tokens - 1) * *token + head_dim;
+}
+
+// Axes of which each one's stride clears all that lies on those with shorter strides, from `extent` elements on: no two of
+// their places share memory.  Sorts them; `extent` becomes that of all together.
+struct Axis {
+    long long stride, count;
+};
+inline bool nested(Axis* axes, int n, long long* extent) {
+    std::sort(axes, axes + n, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+    for (int i = 0; i < n; ++i) {
+        if (axes[i].count == 1) continue;
+        if (axes[i].stride < *extent) return false;
+        *extent += (axes[i].count - 1) * axes[i].stride;
+    }
+    return true;
 }
 
 // An operand of [tokens][heads][head_dim] vectors, and whether the vectors of two that cover the same stretch of memory are

@@ -23,6 +23,33 @@ def append(L, kc, vc, q_out=A[9], **kw):
     return L.regenvc_paged_append(ctypes.byref(B.PagedAppendDesc(**d)), A[0], A[1], A[2], None, None, None, A[6], A[7], A[8], q_out, kc, vc, None)
 
 
+def caches(order, heads=2, slots=16, pages=10, d=64, near=0):
+    """Strides and the distance of V (elements) of one tensor with axes (p, 2, s, h) in the given order."""
+    size, stride, at = {"p": pages, "2": 2, "s": slots, "h": heads}, {}, d
+    for a in reversed(order):
+        stride[a] = at
+        at *= size[a]
+    return dict(k_page_stride=stride["p"], k_slot_stride=stride["s"], k_cache_head_stride=stride["h"], v_page_stride=stride["p"],
+                v_slot_stride=stride["s"], v_cache_head_stride=stride["h"]), stride["2"] - near
+
+
+@pytest.mark.parametrize("order", ["p2sh", "ps2h", "psh2", "ph2s", "phs2", "2psh", "hp2s", "h2ps", "s2ph", "sph2"])
+def test_values_eight_elements_into_the_keys_are_refused(L, order):
+    strides, apart = caches(order, near=8)
+    assert append(L, A[10], A[10] + 2 * apart, **strides) == B.ERR_ALIASING
+    assert append(L, A[10] + 2 * apart, A[10], **strides) == B.ERR_ALIASING
+
+
+def test_values_among_the_keys_are_refused(L):
+    # one slot on (the next slot's keys), one page on, one head on, and on the keys themselves
+    strides, _ = caches("psh2")
+    for far in (128, 256, 16 * 256, 0):
+        assert append(L, A[10], A[10] + 2 * far, **strides) == B.ERR_ALIASING
+    strides, _ = caches("ps2h")
+    other = dict(strides, v_slot_stride=192)                         # the same pages, another step from slot to slot
+    assert append(L, A[10], A[10] + 2 * 128, **other) == B.ERR_ALIASING
+
+
 def test_strides_of_axes_with_one_entry_are_not_looked_at(L):
     """Refused for what comes later (keys given as the cache), not for a stride that no address uses."""
     for kw in (dict(n_k_heads=1, k_cache_head_stride=1 << 33, v_cache_head_stride=3), dict(page_size=1, k_slot_stride=1 << 33, v_slot_stride=8),
