@@ -53,7 +53,7 @@ Span positions_span(const Desc* d, const HeadRowsParams& p) {
 
 // One operand of [tokens][heads][head_dim] vectors; clears *vec where its rows do not allow 16-byte accesses.
 int view_of(const void* ptr, long long token, long long head, int n_tokens, int heads, int head_dim, size_t size, HeadView* v, bool* vec) {
-    *v = HeadView{ptr, 0, 0, heads, Span{nullptr, 0}};
+    *v = HeadView{ptr, 0, 0, n_tokens, heads, Span{nullptr, 0}};
     if (!ptr) return REGENVC_OK;
     if (!head_strides(token, head, n_tokens, heads, head_dim, &v->token, &v->head)) return REGENVC_ERR_BAD_SHAPE;
     if (!aligned(ptr, size)) return REGENVC_ERR_MISALIGNED;

@@ -60,11 +60,12 @@ inline bool nested(Axis* axes, int n, long long* extent) {
 }
 
 // An operand of [tokens][heads][head_dim] vectors, and whether the vectors of two that cover the same stretch of memory are
-// different ones all the same: views of one fused tensor, a whole number of vectors apart inside one token's stride.
+// different ones all the same, as in views of one fused tensor: the pair of them is one more axis among tokens and heads, or the
+// one's heads lie behind the other's inside one token's stride.
 struct HeadView {
     const void* p;
     long long token, head;
-    int heads;
+    int tokens, heads;
     Span span;
 };
 inline Span heads_span(const void* p, long long tokens, int heads, long long token, long long head, int head_dim, size_t size) {
@@ -72,9 +73,13 @@ inline Span heads_span(const void* p, long long tokens, int heads, long long tok
 }
 inline bool views_apart(const HeadView& a, const HeadView& b, int head_dim, size_t size) {
     if (!meet(a.span, b.span)) return true;
-    if (a.token != b.token) return false;
+    if (a.tokens > 1 && a.token != b.token) return false;
     const HeadView &low = (const char*)a.p < (const char*)b.p ? a : b, &high = &low == &a ? b : a;
     const long long gap = (long long)((const char*)high.p - (const char*)low.p) / (long long)size;
+    const HeadView& more = low.heads > high.heads ? low : high;
+    Axis axes[3] = {{low.token, low.tokens}, {more.head, more.heads}, {gap, 2}};
+    long long extent = head_dim;
+    if ((low.head == high.head || low.heads == 1 || high.heads == 1) && nested(axes, 3, &extent)) return true;
     return gap >= (low.heads - 1) * low.head + head_dim && gap + (high.heads - 1) * high.head + head_dim <= low.token;
 }
 
