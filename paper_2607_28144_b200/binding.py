@@ -722,8 +722,8 @@ def _own_strides(t, name: str, n: int, heads: int, d: int):
         raise TypeError(f"{name} must have neighbouring elements of a head")
     if (n > 1 and token < d) or (heads > 1 and head < d):
         raise ValueError(f"{name} has vectors that overlap (an expanded tensor?)")
-    head = head if heads > 1 else d       # the stride of an axis with one entry is never used: name the packed one
-    return (token if n > 1 else heads * head), head
+    # the stride of an axis with one entry is never used: name the packed one
+    return (token if n > 1 else heads * d), (head if heads > 1 else d)
 
 
 def _rotation(positions, widths, n: int):

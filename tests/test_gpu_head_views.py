@@ -53,3 +53,27 @@ def test_appending_with_the_queries_in_place(order):
         results.append((out.contiguous(), *caches))
     assert all(torch.equal(a, b) for a, b in zip(*results)) and B.regenvc_device_status() == B.OK
     assert torch.equal(x[1], kept[1]) and torch.equal(x[2], kept[2])
+
+
+@pytest.mark.parametrize("heads,far", [(3, (1 << 30) + 64), (2, 1 << 31)])
+def test_one_token_of_heads_that_lie_far_apart(heads, far):
+    """A [heads, tokens, d] buffer of more than 2^31 elements, one token of it."""
+    d = 64
+    room = torch.empty((heads - 1) * far + d, dtype=BF, device=DEV)
+    x = room.as_strided((1, heads, d), (d, far, 1))
+    x.copy_(torch.randn(1, heads, d, generator=torch.Generator().manual_seed(1)).to(BF))
+    near, pos = x.contiguous(), torch.full((1, 1), 9, dtype=torch.int32, device=DEV)
+    want = B.regenvc_qk_norm_rope_forward(near, None, pos, [d])[0]
+
+    def close(a, b):     # (vectors more than 2 GB apart take the form without 16-byte accesses, which sums in another order)
+        return ((a.double() - b.double()).abs() <= 2.0 ** -7 * b.double().abs() + 1e-5).all()
+
+    assert close(B.regenvc_qk_norm_rope_forward(x, None, pos, [d])[0], want)
+    caches = [torch.zeros(1, 16, heads, d, dtype=BF, device=DEV) for _ in range(4)]
+    lists = (torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV),
+             torch.tensor([0, 1], dtype=torch.int32, device=DEV))
+    q = B.regenvc_paged_append(x, x, *caches[:2], *lists, q=x, positions=pos, widths=[d], norm=B.NORM_RMS)
+    p = B.regenvc_paged_append(near, near, *caches[2:], *lists, q=near, positions=pos, widths=[d], norm=B.NORM_RMS)
+    assert close(q, p) and close(caches[0], caches[2]) and torch.equal(caches[1], caches[3])
+    outs = [B.regenvc_paged_attn_forward(t, *caches[2:], *lists, lse=True) for t in (x, near)]
+    assert all(torch.equal(a, b) for a, b in zip(*outs)) and B.regenvc_device_status() == B.OK

@@ -1,7 +1,8 @@
-"""Refusals of queries and keys that share memory, without a GPU: every call is refused."""
+"""Queries and keys that share memory, and strides as the library takes them, without a GPU: every call is refused."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2607_28144_b200 import binding as B
 from paper_2607_28144_b200 import build
@@ -34,3 +35,12 @@ def test_vectors_that_meet_are_refused(L):
     assert in_place(L, 768, 192, 64, k_token=1536) == B.ERR_ALIASING     # another step from token to token
     assert in_place(L, 768, 192, 192, hq=4, hk=1) == B.ERR_ALIASING      # a key of q's second head
     assert in_place(L, 768, 192, 128 + 8, hq=4, hk=1) == B.ERR_ALIASING  # ... that runs into it
+
+
+def test_one_token_of_heads_that_lie_far_apart():
+    """[heads, tokens, d] buffers: the stride of a single token means nothing, whatever the heads' is."""
+    for n, heads, strides, want in ((1, 3, (64, 1 << 30, 1), (192, 1 << 30)), (1, 1, (7, 9, 1), (0, 0)), (2, 1, (640, 5, 1), (640, 64)),
+                                    (2, 3, (64, 1 << 30, 1), (64, 1 << 30))):
+        t = torch.empty_strided((n, heads, 64), strides, dtype=torch.bfloat16, device="meta")
+        assert B._own_strides(t, "q", n, heads, 64) == want
+        assert B._head_strides(t, "q", torch.bfloat16, n, heads, 64) == want
