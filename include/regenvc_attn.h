@@ -65,7 +65,8 @@ typedef enum {
     REGENVC_ERR_CUDA = 6,        /* a CUDA call failed: see regenvc_last_cuda_error() */
     REGENVC_ERR_TIMEOUT = 7,     /* a bounded device-side wait expired (sticky device status) */
     REGENVC_ERR_WORKSPACE = 8,   /* caller-supplied workspace too small or misaligned */
-    REGENVC_ERR_RANGE = 9,       /* an input exceeded the fp16 operand range (sticky device status) */
+    REGENVC_ERR_RANGE = 9,       /* an input exceeded the fp16 operand range, or the lists of a paged cache contradict the
+                                    call's sizes (sticky device status) */
     REGENVC_ERR_STATIC_LIMIT = 10, /* regenvc_cross_attn_forward_static(): the shape needs more than the built-in scratch */
     REGENVC_ERR_INTERNAL = 11     /* a kernel found an assumption about its launch broken and did no work (sticky device
                                      status): the dynamic shared memory of the persistent attention kernel did not

@@ -974,7 +974,7 @@ const char* regenvc_status_string(int status) {
         case REGENVC_ERR_CUDA: return "CUDA call failed";
         case REGENVC_ERR_TIMEOUT: return "device-side bounded wait expired";
         case REGENVC_ERR_WORKSPACE: return "workspace too small or misaligned";
-        case REGENVC_ERR_RANGE: return "input outside the fp16 operand range";
+        case REGENVC_ERR_RANGE: return "input outside the fp16 operand range, or lists of a paged cache (row starts, lengths, pages) that contradict the call's sizes";
         case REGENVC_ERR_STATIC_LIMIT: return "shape exceeds the built-in scratch of the allocation-free entry point";
         case REGENVC_ERR_INTERNAL: return "a kernel found its launch assumptions broken and did no work";
         default: return "unknown status";

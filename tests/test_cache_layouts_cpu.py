@@ -1,4 +1,4 @@
-"""Host-side checks of cache layouts and scales of the operators over cached windows.  Every call is refused."""
+"""Host-side checks of cache layouts and status texts of the operators over cached windows.  Every call is refused."""
 import ctypes
 
 import pytest
@@ -67,3 +67,8 @@ def test_the_binding_names_short_strides_for_axes_with_one_entry():
     assert B._cache(both[:, 1], "v_cache", torch.bfloat16) == (4096, 128, 128)
     one = torch.empty((1, 2, 1 << 20, 16, 128), dtype=torch.bfloat16, device="meta")
     assert B._cache(one[:, :, :, :8][:, 1], "v_cache", torch.bfloat16)[1:] == (2048, 128)
+
+
+def test_the_text_of_a_range_error_names_lists_and_operands():
+    text = B.status_string(B.ERR_RANGE)
+    assert "fp16" in text and "lists" in text
