@@ -313,7 +313,7 @@ int regenvc_qk_norm_rope_backward(const regenvc_qk_norm_rope_desc* desc, const v
  * the description (a page outside 0 .. n_pages - 1, more tokens than the table holds, fewer than the new ones in an append,
  * starts that descend or leave 0 .. n_tokens), nothing outside the tensors is touched, an append writes no slot behind a
  * sequence's length, regenvc_device_status() reports REGENVC_ERR_RANGE (until then later attention calls skip their work) and
- * the results of the call are unspecified.  1 <= n_sequences <= 4096.
+ * the results of the call are unspecified.  1 <= n_sequences <= 4096; a sequence has at most 2^30 tokens (reported too).
  *
  * regenvc_paged_append(): k (normalised per head where norm is REGENVC_NORM_RMS, rotated where n_axes > 0, as in
  *   regenvc_qk_norm_rope_forward()) and v (as it is) of the call's tokens into their slots, and, where given, q -> q_out in

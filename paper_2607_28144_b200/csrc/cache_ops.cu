@@ -340,7 +340,7 @@ int regenvc_paged_append(const regenvc_paged_append_desc* d, const void* q, cons
     p.n_sequences = d->n_sequences;
     p.page_size = d->page_size;
     p.n_pages = d->n_pages;
-    p.pages_per_sequence = d->pages_per_sequence;
+    p.most_tokens = (int)std::min((long long)d->pages_per_sequence * d->page_size, kMaxCachedTokens);
     ladder(d, &p);
     int sm_count = 0;
     rc = op_device(&sm_count, &p.status);

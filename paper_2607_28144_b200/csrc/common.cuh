@@ -19,6 +19,8 @@ constexpr int kStatusTimeout = 7;
 constexpr int kStatusRange = 9;
 constexpr int kStatusInternal = 11;
 
+constexpr long long kMaxCachedTokens = 1ll << 30;   // of a sequence in a paged cache: positions are ints with room for a tile more
+
 // cos/sin table of one (T, H, W, theta): float2 (cos, sin) entries,
 // [T][22] then [H][21] then [W][21].
 struct RopeGrid {

@@ -46,7 +46,7 @@ __device__ __forceinline__ void find_slots(const HeadRowsParams& p, Slots& s, in
                 // (starts that do not ascend may count a row to a sequence that does not have it)
                 const int first = p.row_starts[seq], end = p.row_starts[seq + 1];
                 const long long at = (long long)p.lengths[seq] - ((long long)end - n);
-                bool good = first <= n && n < end && end <= p.n_tokens && at >= 0 && at < (long long)p.pages_per_sequence * p.page_size;
+                bool good = first <= n && n < end && end <= p.n_tokens && at >= 0 && at < p.most_tokens;
                 if (good) {
                     const int slot = (int)(at / p.page_size), in_page = (int)(at - (long long)slot * p.page_size);
                     const int page = p.table[seq * p.table_stride + slot];
@@ -70,7 +70,7 @@ __device__ __forceinline__ void find_slots(const HeadRowsParams& p, Slots& s, in
 __device__ __forceinline__ void check_lists(const HeadRowsParams& p) {
     for (int s = blockDim.x - 1 - threadIdx.x; s < p.n_sequences; s += blockDim.x) {
         const int first = p.row_starts[s], end = p.row_starts[s + 1], keys = p.lengths[s];
-        if (first < 0 || end < first || end > p.n_tokens || keys < end - first || keys > (long long)p.pages_per_sequence * p.page_size)
+        if (first < 0 || end < first || end > p.n_tokens || keys < end - first || keys > p.most_tokens)
             atomicCAS(p.status, 0, kStatusRange);
     }
 }

@@ -30,9 +30,10 @@ struct HeadRowsParams {
     int paged;
     const int* row_starts;             // [n_sequences + 1]
     const int* lengths;                // [n_sequences] cached tokens, the new ones among them
-    const int* table;                  // [n_sequences][pages_per_sequence]
+    const int* table;                  // [n_sequences][pages of a sequence]
     long long table_stride, page_stride[2];
-    int n_sequences, page_size, n_pages, pages_per_sequence;
+    int n_sequences, page_size, n_pages;
+    int most_tokens;                   // that a sequence's row of the table can hold
     int* status;
     // gradients: in[] = x, grad[] = dy, out[] = dx
     const void* grad[2];

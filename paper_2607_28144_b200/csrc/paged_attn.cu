@@ -126,7 +126,7 @@ __device__ __noinline__ Seq load_seq(const PagedAttnParams& p, int s) {
     Seq q;
     q.row0 = min(max(p.row_starts[s], 0), p.n_tokens);
     q.tokens = min(max(p.row_starts[s + 1], q.row0), p.n_tokens) - q.row0;
-    q.keys = (int)min((long long)max(p.lengths[s], 0), min((long long)p.pages_per_sequence * p.page_size, 1ll << 30));
+    q.keys = (int)min((long long)max(p.lengths[s], 0), min((long long)p.pages_per_sequence * p.page_size, kMaxCachedTokens));
     return q;
 }
 // First and one past the last key that the token at position pos sees.
@@ -286,7 +286,7 @@ __device__ __noinline__ long long cost_of(const PagedAttnParams& p, const Seq& q
 
 __device__ __forceinline__ void check_seq(const PagedAttnParams& p, int s) {
     const bool good = p.row_starts[s] >= 0 && p.row_starts[s + 1] >= p.row_starts[s] && p.row_starts[s + 1] <= p.n_tokens &&
-                      p.lengths[s] >= 0 && p.lengths[s] <= (long long)p.pages_per_sequence * p.page_size;
+                      p.lengths[s] >= 0 && p.lengths[s] <= min((long long)p.pages_per_sequence * p.page_size, kMaxCachedTokens);
     if (!good) atomicCAS(p.status, 0, kStatusRange);
 }
 

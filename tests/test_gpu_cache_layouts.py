@@ -1,5 +1,5 @@
 """Caches as views of one tensor: a page's, a slot's or a head's key beside its value in any order of the axes, axes with one
-entry in tensors of more than 2^31 elements."""
+entry in tensors of more than 2^31 elements, and the longest sequences."""
 import itertools
 
 import pytest
@@ -88,3 +88,17 @@ def test_one_slot_in_a_cache_of_more_than_2_31_elements():
     B.regenvc_paged_append(k, v, both[:, 0], both[:, 1], *lists([[pages - 1, 5]], [2], [0, 2]))
     assert B.regenvc_device_status() == B.OK
     assert torch.equal(both[pages - 1, :, 0], torch.stack([k[0], v[0]])) and torch.equal(both[5, :, 0], torch.stack([k[1], v[1]]))
+
+
+def test_sequences_of_more_than_2_30_tokens_are_reported():
+    """A table may name a page again and again; positions are held as far as 2^30."""
+    slots = 1 << 20
+    kc, vc = (torch.zeros(2, slots, 1, 64, dtype=BF, device=DEV) for _ in range(2))
+    x = torch.ones(1, 1, 64, dtype=BF, device=DEV)
+    table = [[0] * 1024 + [1]]
+    B.regenvc_paged_append(x, x, kc, vc, *lists(table, [1 << 30], [0, 1]))
+    assert B.regenvc_device_status() == B.OK and (kc[0, -1] == 1).all() and kc.sum() == 64
+    B.regenvc_paged_append(x, x, kc, vc, *lists(table, [(1 << 30) + 1], [0, 1]))
+    assert B.regenvc_device_status() == B.ERR_RANGE and kc.sum() == 64
+    B.regenvc_paged_attn_forward(x, kc, vc, *lists(table, [(1 << 30) + 1], [0, 1]))
+    assert B.regenvc_device_status() == B.ERR_RANGE
