@@ -326,7 +326,7 @@ int regenvc_qk_norm_rope_backward(const regenvc_qk_norm_rope_desc* desc, const v
  *            latent frame make it causal by frames
  *   window : 0, or (with group >= 1) the number of groups seen, its own among them: t / b > p / b - window; pages of tokens
  *            that no new token sees need not exist any more
- *   scale  : > 0, or 0 for 1 / sqrt(head_dim)
+ *   scale  : > 0 (scale log2(e) in fp32's range), or 0 for 1 / sqrt(head_dim)
  *   lse    : fp32 [n_tokens][n_q_heads] or NULL: natural logarithm of the sum of the exponentials of a row's scores
  *   A row that sees nothing gives zeros (lse -inf).  What lies in unseen slots (behind a length, before the window of all
  *   of a call's rows, in unused pages) does not matter; values that any new token of their sequence sees must be finite.

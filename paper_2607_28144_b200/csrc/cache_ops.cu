@@ -363,7 +363,9 @@ int regenvc_paged_attn_forward(const regenvc_paged_attn_desc* d, const void* q, 
         d->window < 0 || (d->window > 0 && d->group == 0))
         return REGENVC_ERR_BAD_SHAPE;
     if ((d->head_dim != 64 && d->head_dim != 128) || (d->type != REGENVC_BF16 && d->type != REGENVC_F16)) return REGENVC_ERR_UNSUPPORTED;
-    if (!(d->scale >= 0.0f) || !std::isfinite(d->scale)) return REGENVC_ERR_UNSUPPORTED;
+    const double scale = d->scale > 0.0f ? (double)d->scale : 1.0 / std::sqrt((double)d->head_dim);
+    const float scale_log2 = (float)(scale * 1.4426950408889634);
+    if (!(d->scale >= 0.0f) || !std::isfinite(scale_log2)) return REGENVC_ERR_UNSUPPORTED;
     Span lists[3];
     long long table_stride = d->table_stride;
     int rc = lists_ok(d->n_sequences, d->page_size, d->n_pages, d->pages_per_sequence, &table_stride, row_starts, lengths, block_table, lists);
@@ -412,8 +414,7 @@ int regenvc_paged_attn_forward(const regenvc_paged_attn_desc* d, const void* q, 
     p.pages_per_sequence = d->pages_per_sequence;
     p.group = d->group;
     p.window = d->window;
-    const double scale = d->scale > 0.0f ? (double)d->scale : 1.0 / std::sqrt((double)d->head_dim);
-    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    p.scale_log2 = scale_log2;
     // A tile of 128 keys comes in boxes of as many rows as divide a page; one that lies within a page in one box.
     p.box_rows = 128;
     while (d->page_size % p.box_rows != 0) p.box_rows /= 2;

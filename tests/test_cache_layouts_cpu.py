@@ -1,4 +1,4 @@
-"""Host-side checks of cache layouts and status texts of the operators over cached windows.  Every call is refused."""
+"""Host-side checks of cache layouts, scales and status texts of the operators over cached windows.  Every call is refused."""
 import ctypes
 
 import pytest
@@ -67,6 +67,17 @@ def test_the_binding_names_short_strides_for_axes_with_one_entry():
     assert B._cache(both[:, 1], "v_cache", torch.bfloat16) == (4096, 128, 128)
     one = torch.empty((1, 2, 1 << 20, 16, 128), dtype=torch.bfloat16, device="meta")
     assert B._cache(one[:, :, :, :8][:, 1], "v_cache", torch.bfloat16)[1:] == (2048, 128)
+
+
+def attend(L, scale, lse=A[7], **kw):
+    d = B.PagedAttnDesc(n_tokens=5, n_q_heads=4, n_k_heads=2, head_dim=64, type=0, n_sequences=3, page_size=16, n_pages=10,
+                        pages_per_sequence=4, scale=scale, **kw)
+    return L.regenvc_paged_attn_forward(ctypes.byref(d), A[0], A[1], A[2], A[3], A[4], A[5], A[6], lse, A[8], 0, None)
+
+
+def test_a_scale_whose_power_of_two_passes_the_range_is_refused(L):
+    assert attend(L, 2.4e38) == B.ERR_UNSUPPORTED                     # times log2(e): past fp32
+    assert attend(L, 1e38) == attend(L, 1e-45) == B.ERR_WORKSPACE     # in range; refused for the workspace of 0 bytes
 
 
 def test_the_text_of_a_range_error_names_lists_and_operands():
