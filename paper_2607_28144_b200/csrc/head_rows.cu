@@ -99,7 +99,8 @@ __device__ __forceinline__ bool locate(const HeadRowsParams& p, const Slots& s, 
     return true;
 }
 
-template <typename T, bool HALVES, bool PAGED>
+// SOME: adjacent pairs of which the head's last do not turn.
+template <typename T, bool HALVES, bool PAGED, bool SOME>
 __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
     extern __shared__ float4 shared_raw[];
     __shared__ Slots slots;
@@ -177,7 +178,8 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_rows_kernel(const __grid
             store_raw8(x.to + hi_from_lo, x.hi);
             continue;
         }
-        if (at.turns) turn(v, load_angles(words, turning));
+        if (SOME) turn_some(v, load_angles(words, turning), p.n_pairs - 4 * u, p.head_dim / 4);
+        else if (at.turns) turn(v, load_angles(words, turning));
         float lo[8], hi[8];
         spread<HALVES>(v, lo, hi);
         store8(x.to, lo);
@@ -256,8 +258,9 @@ cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, cudaStream_t
     const int all = p.heads[0] + p.heads[1] + p.heads[2];
     const bool unit = in_units(p, vec, sizeof(T));
     const int width = unit ? lanes_of_head(p) : 32;
-    auto kernel = p.halves ? (p.paged ? head_rows_kernel<T, true, true> : head_rows_kernel<T, true, false>)
-                           : (p.paged ? head_rows_kernel<T, false, true> : head_rows_kernel<T, false, false>);
+    auto kernel = p.halves        ? (p.paged ? head_rows_kernel<T, true, true, false> : head_rows_kernel<T, true, false, false>)
+                  : turns_some(p) ? (p.paged ? head_rows_kernel<T, false, true, true> : head_rows_kernel<T, false, false, true>)
+                                  : (p.paged ? head_rows_kernel<T, false, true, false> : head_rows_kernel<T, false, false, false>);
     int per_sm = 1;
     p.tokens_per_cta = kMaxTokens;
     if (p.n_tokens > sm_count) {   // (a query takes longer than the kernel of a call of a few tokens)

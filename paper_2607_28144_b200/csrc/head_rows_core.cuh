@@ -18,7 +18,8 @@ constexpr int kHeadThreads = 256;
 
 enum { kPlain = 0, kAdjacentUnits = 1, kHalfUnits = 2 };
 
-// Units of eight pairs of a table: the rotated ones, and for adjacent pairs, to the end of the head, (1, 0).
+// Units of eight pairs of a table: the rotated ones, and for adjacent pairs, to the end of the head, (1, 0).  (Those pairs do
+// not turn, see turn(); the angles fill the words that whole units are read in.)
 template <int ORDER>
 __device__ __forceinline__ int table_units(const HeadRowsParams& p) {
     return ORDER == kAdjacentUnits ? p.head_dim / 16 : p.n_pairs / 8;
@@ -188,6 +189,21 @@ __device__ __forceinline__ void turn(Unit& v, const Angles& by) {
         v.b[i] = fma2(b, by.cos[i], mul2(a, by.sin[i]));
     }
 }
+// The same for adjacent pairs of which the head's last do not turn: they keep their values (a 1 - b 0 is not a number where b is
+// infinite).  pairs: of a head that turn, less those before the unit's first piece; second: pairs from there to its second piece.
+__device__ __forceinline__ void turn_some(Unit& v, const Angles& by, int pairs, int second) {
+    Unit y = v;
+    turn(y, by);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = pairs - (i < 2 ? 2 * i : second + 2 * (i - 2));   // of this two: none, one or both
+        float a0, a1, b0, b1, c0, c1, d0, d1;
+        unpack2(v.a[i], a0, a1), unpack2(v.b[i], b0, b1);
+        unpack2(y.a[i], c0, c1), unpack2(y.b[i], d0, d1);
+        v.a[i] = pack2(left > 0 ? c0 : a0, left > 1 ? c1 : a1);
+        v.b[i] = pack2(left > 0 ? d0 : b0, left > 1 ? d1 : b1);
+    }
+}
 __device__ __forceinline__ float sum2(uint64_t v) {
     float a, b;
     unpack2(v, a, b);
@@ -221,6 +237,8 @@ inline bool in_units(HeadRowsParams& p, bool vec, int size) {
     }
     return fits;
 }
+// Adjacent pairs of which some do not turn (half pairs have units of their own for what does not).
+inline bool turns_some(const HeadRowsParams& p) { return !p.halves && p.n_axes > 0 && 2 * p.n_pairs < p.head_dim; }
 inline int lanes_of_head(const HeadRowsParams& p) { return p.head_dim <= 64 ? 4 : (p.head_dim <= 128 ? 8 : 16); }
 
 // Tokens per thread block: a power of two, so that a token has a whole number of the block's groups and these walk over its

@@ -29,7 +29,7 @@ __device__ __forceinline__ Vector<T> locate(const HeadRowsParams& p, int token, 
             reinterpret_cast<T*>(p.out[w]) + n * p.out_token[w] + hh * p.out_head[w]};
 }
 
-template <typename T, bool HALVES>
+template <typename T, bool HALVES, bool SOME>   // SOME: adjacent pairs of which the head's last do not turn
 __global__ void __launch_bounds__(kHeadThreads, 2) head_rows_grad_kernel(const __grid_constant__ HeadRowsParams p, const int width) {
     extern __shared__ float4 shared_raw[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the join sets itself up and waits for this grid
@@ -84,7 +84,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_rows_grad_kernel(const _
             const Item x = next;
             if (round + 1 < rounds) fetch(next);
             Unit v = widen<HALVES>(x.xl, x.xh), g = widen<HALVES>(x.yl, x.yh);
-            if (at.turns && x.to) turn(g, load_angles(words, turning));
+            if (SOME && x.to) turn_some(g, load_angles(words, turning), p.n_pairs - 4 * u, p.head_dim / 4);
+            else if (at.turns && x.to) turn(g, load_angles(words, turning));
             Unit w = load_gains<HALVES>(gain_words + (active ? x.of * 4 * units : -u), units);
             uint64_t sq2 = 0, hx2 = 0;
 #pragma unroll
@@ -257,7 +258,9 @@ cudaError_t launch_typed(HeadRowsParams& p, bool vec, int sm_count, int* blocks,
     const int all = p.heads[0] + p.heads[1];
     const bool unit = in_units(p, vec, sizeof(T));
     const int width = unit ? lanes_of_head(p) : 32;
-    auto kernel = p.halves ? head_rows_grad_kernel<T, true> : head_rows_grad_kernel<T, false>;
+    auto kernel = p.halves        ? head_rows_grad_kernel<T, true, false>
+                  : turns_some(p) ? head_rows_grad_kernel<T, false, true>
+                                  : head_rows_grad_kernel<T, false, false>;
     const size_t per_token = (size_t)table_pitch(p) * sizeof(float2), gains = 2 * (size_t)p.head_dim * sizeof(float);
     int per_sm = 1;
     const cudaError_t e = unit ? cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kHeadThreads, kHeadTokens * per_token + gains)
