@@ -271,7 +271,8 @@ int regenvc_rope_axes(const regenvc_rope_axes_desc* desc, const void* q, const v
  *   q_weight, k_weight : fp32 [head_dim] or NULL (ones), shared by the heads
  *   positions, n_axes, widths, halves, whole_ladder, pos_float, rope_theta : as there; n_axes 0 (and positions NULL): no
  *          rotation
- * A row whose sum of squares passes fp32's range normalises to 0.
+ * A row whose sum of squares passes fp32's range normalises to 0, and its gradients are 0; an infinite element is not a number
+ * in its own place.  With eps 0 a row's mean square has to be a normal fp32 number.
  * The gradients take the operands again (no statistics are kept): dq_out, dk_out with the strides of q_out, k_out; dq and dk
  * may be them in place; dq_weight, dk_weight: fp32 [head_dim], NULL where not wanted, need q_weight, k_weight and `workspace`
  * (regenvc_qk_norm_rope_workspace_bytes(), 16-byte aligned, one for each of the calls that may overlap on the GPU; else

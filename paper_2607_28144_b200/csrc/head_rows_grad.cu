@@ -97,7 +97,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_rows_grad_kernel(const _
             }
             const float sq = head_sum(sum2(sq2), width), hx = head_sum(sum2(hx2), width);
             const float r = rsqrtf(sq * inv_d + p.eps);
-            const float m = hx * inv_d * r;                 // mean(g w n)
+            // mean(g w n); of a row past fp32's range n is 0, whatever the sum of g w x came to
+            const float m = r == 0.0f ? 0.0f : hx * inv_d * r;
             if (x.to) {
                 const uint64_t r2 = pack2(r, r), m2 = pack2(-m, -m);
 #pragma unroll
@@ -195,14 +196,15 @@ __global__ void __launch_bounds__(kHeadThreads) head_rows_grad_element_kernel(co
             }
             sq = warp_sum(sq) / (float)p.head_dim;
             hx = warp_sum(hx) / (float)p.head_dim;
-            const float r = rsqrtf(sq + p.eps), m = hx * r * r;
+            const float r = rsqrtf(sq + p.eps);
+            const float m = r == 0.0f ? 0.0f : hx * r * r;  // mean(g w n) r, as above
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
                 const int u = lane + 32 * k;
                 if (u >= units) continue;
                 const int first = unit_first(u, p);
                 from_f32(r * (ga[k] * (gain ? gain[first] : 1.0f) - xa[k] * m), at.dx[first]);
-                const float sa = ga[k] * xa[k] * r, sb = gb[k] * xb[k] * r;
+                const float sa = ga[k] * (xa[k] * r), sb = gb[k] * (xb[k] * r);
                 if (w) da[1][k] += sa, db[1][k] += sb;
                 else da[0][k] += sa, db[0][k] += sb;
                 if (u < p.n_pairs) {

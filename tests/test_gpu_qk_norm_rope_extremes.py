@@ -1,4 +1,4 @@
-"""Infinities in the norm and rotation of queries and keys: what they reach and what not."""
+"""Infinities and sums past fp32's range in the norm and rotation of queries and keys: what they reach and what not."""
 import math
 
 import pytest
@@ -96,3 +96,47 @@ def test_an_infinite_gradient_behind_the_rotation(d, widths):
         got = B.regenvc_qk_norm_rope_backward(dy, None, rows, None, pos, list(widths), q_weight=w)
         same(got["dq_weight"], want, 1e-4)
         assert torch.isfinite(got["dq"][:7]).all() and torch.isfinite(got["dq"][8:]).all() and torch.isfinite(got["dq"][7, 0]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("d", [64, 128, 250])
+def test_gradients_of_a_row_past_the_range_are_zeros(dtype, halves, d):
+    """Its sum of squares passes fp32's range, so it normalises to 0: so do its gradients, and other rows' are as without it."""
+    g = torch.Generator().manual_seed(d)
+    x, dy = (torch.randn(6, 2, d, generator=g).to(dtype).to(DEV) for _ in range(2))
+    w = (1 + 0.3 * torch.randn(d, generator=g)).to(DEV)
+    pos = torch.arange(6, dtype=torch.int32, device=DEV).view(1, -1)
+    how = dict(halves=halves, q_weight=w)
+    x[2, 1] = 0
+    dy[2, 1] = dy[2, 1].abs() + 1                                    # the sum of dy x passes the range too
+    base = B.regenvc_qk_norm_rope_backward(dy, None, x, None, pos, [d], **how)
+    zero_row = dict(q_weight=w, halves=halves)
+    for big in (2e19, 1e30, 3e38):
+        y = x.clone()
+        y[2, 1] = torch.where(torch.arange(d, device=DEV) % 2 == 0, big, 0.5 * big)
+        assert (B.regenvc_qk_norm_rope_forward(y, None, pos, [d], **zero_row)[0][2, 1] == 0).all()
+        got = B.regenvc_qk_norm_rope_backward(dy, None, y, None, pos, [d], **how)
+        assert (got["dq"][2, 1] == 0).all()
+        keep = torch.ones(6, 2, dtype=torch.bool, device=DEV)
+        keep[2, 1] = False
+        assert torch.equal(got["dq"][keep], base["dq"][keep])
+        assert torch.isfinite(got["dq_weight"]).all() and torch.equal(got["dq_weight"], base["dq_weight"])
+
+
+@pytest.mark.parametrize("d", [64, 128, 250])
+def test_gradients_of_an_infinite_element(d):
+    """As in the forward pass: not a number in its place, zeros beside it, and the other rows as ever."""
+    g = torch.Generator().manual_seed(d)
+    x, dy = (torch.randn(6, 2, d, generator=g).to(DEV) for _ in range(2))
+    w = torch.ones(d, device=DEV)
+    base = B.regenvc_qk_norm_rope_backward(dy, None, x, None, q_weight=w)
+    x[2, 1, 5] = math.inf
+    got = B.regenvc_qk_norm_rope_backward(dy, None, x, None, q_weight=w)
+    place = torch.zeros(6, 2, d, dtype=torch.bool, device=DEV)
+    place[2, 1, 5] = True
+    assert torch.equal(torch.isnan(got["dq"]), place) and torch.equal(torch.isnan(got["dq_weight"]), place[2, 1])
+    row = got["dq"][2, 1].nan_to_num()
+    assert (row == 0).all()
+    keep = ~place.any(-1)
+    assert torch.equal(got["dq"][keep], base["dq"][keep])
