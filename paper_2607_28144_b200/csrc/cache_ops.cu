@@ -419,11 +419,6 @@ int regenvc_paged_attn_forward(const regenvc_paged_attn_desc* d, const void* q, 
     p.box_rows = 128;
     while (d->page_size % p.box_rows != 0) p.box_rows /= 2;
     p.one_page_box = p.box_rows < 128 && d->page_size >= 128;
-    // Whole items in rounds where several tiles of rows share a head's keys and there can be more items than thread blocks;
-    // calls of few rows per sequence have nothing to share (a batch of 9 chunks and single tokens: 216 us with one round, 233
-    // without).
-    const long long rows = (long long)d->n_tokens * p.share;
-    p.rounds = rows >= 64ll * d->n_sequences && (rows / kPagedRows + d->n_sequences) * d->n_k_heads >= kPagedRoundsFrom;
     char* w = reinterpret_cast<char*>(workspace);
     p.part_o = reinterpret_cast<float4*>(w);
     w += (size_t)kPagedMaxGrid * 2 * kPagedRows * d->head_dim * sizeof(float);
@@ -433,6 +428,12 @@ int regenvc_paged_attn_forward(const regenvc_paged_attn_desc* d, const void* q, 
     int sm_count = 0;
     rc = op_device(&sm_count, &p.status);
     if (rc != REGENVC_OK) return rc;
+    // Whole items in rounds where several tiles of rows share a head's keys and there can be an item for every thread block; calls
+    // of few rows per sequence have nothing to share (a batch of 9 chunks and single tokens: 216 us with one round, 233 without).
+    // A sequence's last item may hold one row, so these are as many items as the rows can make (planning for rounds where there
+    // are too few for one takes longer: 132 items over 4096 keys 95 us, 101 when planned so).
+    const long long rows = (long long)d->n_tokens * p.share, most_items = (rows + (kPagedRows - 1ll) * d->n_sequences) / kPagedRows * d->n_k_heads;
+    p.rounds = rows >= 64ll * d->n_sequences && most_items >= paged_attn_grid(sm_count);
     PagedMaps maps;
     const CUtensorMapDataType type = d->type == REGENVC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     CUtensorMap* small[2] = {&maps.k, &maps.v};

@@ -1213,7 +1213,7 @@ cudaError_t configure_paged_attn() {
 
 cudaError_t launch_paged_attn(const PagedMaps& maps, const PagedAttnParams& p, int head_dim, bool f16, int sm_count,
                               int* launches, cudaStream_t stream) {
-    const int grid = sm_count < kPagedMaxGrid ? sm_count : kPagedMaxGrid;
+    const int grid = paged_attn_grid(sm_count);
     *launches = 0;
     if (head_dim == 128)
         return f16 ? launch_one<128, true>(maps, p, grid, launches, stream) : launch_one<128, false>(maps, p, grid, launches, stream);

@@ -7,7 +7,6 @@
 namespace regenvc {
 
 constexpr int kPagedMaxGrid = 160;           // thread blocks of the attention kernel
-constexpr int kPagedRoundsFrom = 132;         // items from which on there may be one for every thread block
 constexpr int kPagedMaxSequences = 4096;
 constexpr int kPagedRows = 256;              // rows of an item
 
@@ -39,6 +38,7 @@ struct PagedAttnParams {
     int* status;
 };
 
+inline int paged_attn_grid(int sm_count) { return sm_count < kPagedMaxGrid ? sm_count : kPagedMaxGrid; }
 size_t paged_attn_workspace_bytes(int head_dim);
 cudaError_t configure_paged_attn();
 struct PagedMaps {
