@@ -907,8 +907,10 @@ def regenvc_paged_attn_forward(q, k_cache, v_cache, block_table, lengths, row_st
                                scale=None, out=None, lse=None, workspace=None, stream=None):
     """Attention of each sequence's new tokens q [tokens, heads, head_dim] (rows ``row_starts``) over its cached tokens, the new
     ones (already appended) among them; returns (out, lse).  ``group`` 0: every row sees them all; 1: causal; b: causal by
-    groups of b tokens (a latent frame), ``window`` of them at most (0: all).  ``lse``: None, or True or an fp32 tensor
-    [tokens, heads] for the logarithms of the rows' sums.  ``workspace``: uint8, regenvc_paged_attn_workspace_bytes() long."""
+    groups of b tokens (a latent frame), ``window`` of them at most (0: all).  ``scale``: of the scores, None or 0 for
+    1 / sqrt(head_dim).  ``lse``: None, or True or an fp32 tensor [tokens, heads] for the logarithms of the rows' sums.
+    ``workspace``: uint8, regenvc_paged_attn_workspace_bytes() long; without one 43 MB (22 at 64 columns) are taken from torch's
+    allocator in every call."""
     if q.dim() != 3 or q.dtype not in TYPES:
         raise TypeError("q must be [tokens, heads, head_dim] in bf16 or fp16")
     n, hq, d = q.shape

@@ -10,8 +10,10 @@
 // took 330 instructions and 65 shared wavefronts a vector, and 32 us where this takes 26).  One vector is in flight per group
 // beside the one at hand, with four blocks on an SM: angles or gains held in registers over the walk spill (31 to 55 us), three
 // blocks 30 us, five 37.
-// Measured, 10920 tokens, 12 + 12 heads of 128, bf16: 25.9 us, 5.2 TB/s of what it has to move (27.0 with one kernel for rows
-// and caches); with the values into a cache of 1560-token pages 42.1 us, 4.8 TB/s; one token 3 us, 64 tokens appended 5 us (a chain of list, page and row behind a launch).
+// Measured, 10920 tokens, 12 + 12 heads of 128: bf16 26.0 us, 5.2 TB/s of what it has to move (27.0 with one kernel for rows and
+// caches); fp32 48.5 us, 5.5 TB/s; with the values into a cache of 1560-token pages 42.8 us, 4.7 TB/s, fp32 85 us, 4.7 TB/s
+// (without the norm 2 to 3 % less).  One token 2.7 us, 64 tokens appended 5 us (a chain of list, page and row behind a launch).
+// Four blocks on an SM were chosen on bf16; fp32 takes 64 registers too, of which the kernel for caches spills some 110 bytes.
 // Paged: token n of the call belongs to the sequence whose rows it lies in, found by counting the row starts at or before
 // it (a warp per token, all loads independent: a binary search is a chain of loads, which is what a call of a few tokens
 // would wait for); its slot is the sequence's length minus the rows behind it, its page comes from the table.

@@ -46,7 +46,7 @@ struct HeadRowsParams {
 };
 
 cudaError_t launch_head_rows(HeadRowsParams p, int type, bool vec, int sm_count, cudaStream_t stream);
-// Blocks of the gradients' grid are at most this many per SM of the largest device, which sizes their workspace.
+// The gradients' grid has at most this many blocks, which sizes their workspace.
 constexpr int kHeadGradMaxBlocks = 1184;
 inline size_t head_grad_workspace_bytes(int head_dim) { return (size_t)kHeadGradMaxBlocks * 2 * head_dim * sizeof(float); }
 cudaError_t launch_head_rows_grad(HeadRowsParams p, int type, bool vec, int sm_count, int* launches, cudaStream_t stream);

@@ -7,7 +7,8 @@
 // 128 registers hold two vectors of operands, their products and the sums of both gains, so two blocks fill an SM (three spill:
 // 59 us instead of 44); what a block keeps in flight is then one vector a group, which is what bounds it.  Loads and stores are
 // marked as touched once (50 instead of 51 us, fp32 60 instead of 62 before the walk over one token's heads).
-// Measured, 10920 tokens, 12 + 12 heads of 128: bf16 44.3 us, 4.5 TB/s; fp32, 4097 tokens, 40 + 8 heads, 62 us, 4.9 TB/s.
+// Measured, 10920 tokens, 12 + 12 heads of 128: bf16 44.3 us, 4.5 TB/s; fp32, 4097 tokens, 40 + 8 heads, 61.5 us, 4.9 TB/s (whose
+// build spills 48 to 76 bytes at 128 registers).
 // The sums of dw have a fixed order: a thread adds up what its own vectors give, a block joins its threads, a second kernel
 // joins the blocks, each over the same vectors in every call of a shape; no atomics.
 #include "head_rows_core.cuh"

@@ -14,10 +14,11 @@
 // tokens): both streams have the same rows and take every other tile of keys, and their results are joined in tensor memory
 // at the end.  Either way one stream's products run under the other's exponentials.
 //
-// Bound: single tokens by HBM (64 streams with 16-token pages, 2.77 GB: 463 us, 6.0 TB/s of 6.44 measured).  Chunks by the
-// round a stream's tile takes through softmax and products, which one buffer of scores does not hide: 128 exponentials a row
-// (1100 cycles alone, 2000 beside the other stream's), the products (1024 and some 400 of hand-over), loads and hand-over (500)
-// (a window of 10920 tokens over 31200, 40 heads: 4.65 ms, 1.05 PFLOP/s; without exponentials 4.2 ms, without products 4.0).
+// Bound: single tokens by HBM (64 streams with 16-token pages, 2.77 GB: 463 us, 6.0 TB/s of 6.44 measured; half the bytes at 64
+// columns take 371 us, which is not HBM's and was not looked into).  Chunks by the round a stream's tile takes through softmax
+// and products, which one buffer of scores does not hide: 128 exponentials a row (1100 cycles alone, 2000 beside the other
+// stream's), the products (1024 and some 400 of hand-over), loads and hand-over (500) (a window of 10920 tokens over 31200, 40
+// heads: 4.65 ms, 1.05 PFLOP/s; without exponentials 4.2 ms, without products 4.0).
 //
 // Tensor memory: tiles of scores from column 0 on, two of them beside O0 and O1 of 128 columns, three beside 64 columns; the
 // probabilities (16-bit pairs) lie over the scores.  With three, a stream's next scores are formed under its exponentials.
@@ -51,6 +52,8 @@ namespace regenvc {
 namespace {
 
 constexpr int kPgSoftmax = 256, kPgThreads = kPgSoftmax + 128;
+// 168 registers a thread fill the SM's; the others hand most of theirs to the softmax warps.  ptxas spills 72 bytes of a build and
+// does not say in which role.
 constexpr int kPgLaunchRegs = 168, kPgControlRegs = 64;
 constexpr int kPgSoftmaxRegs = ((kPgLaunchRegs * kPgThreads - kPgControlRegs * 128) / kPgSoftmax) / 8 * 8;
 static_assert(kPgSoftmaxRegs * kPgSoftmax + kPgControlRegs * 128 <= kPgLaunchRegs * kPgThreads, "register budget");
