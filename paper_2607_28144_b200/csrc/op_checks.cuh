@@ -45,7 +45,7 @@ inline bool head_strides(long long token_in, long long head_in, long long tokens
 }
 
 // Axes of which each one's stride clears all that lies on those with shorter strides, from `extent` elements on: no two of
-// their places share memory.  Sorts them; `extent` becomes that of all together.
+// their places share memory, and their bytes are counted in 64 bits.  Sorts them; `extent` becomes that of all together.
 struct Axis {
     long long stride, count;
 };
@@ -53,7 +53,7 @@ inline bool nested(Axis* axes, int n, long long* extent) {
     std::sort(axes, axes + n, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
     for (int i = 0; i < n; ++i) {
         if (axes[i].count == 1) continue;
-        if (axes[i].stride < *extent) return false;
+        if (axes[i].stride < *extent || axes[i].count - 1 > (1ll << 58) / axes[i].stride) return false;
         *extent += (axes[i].count - 1) * axes[i].stride;
     }
     return true;

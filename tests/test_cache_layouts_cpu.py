@@ -59,6 +59,12 @@ def test_strides_of_axes_with_one_entry_are_not_looked_at(L):
         assert append(L, A[1], A[11], **kw) == B.ERR_BAD_SHAPE, kw
 
 
+def test_caches_whose_bytes_pass_64_bits_are_refused(L):
+    assert append(L, A[1], A[11], n_pages=1 << 30, k_page_stride=1 << 38) == B.ERR_BAD_SHAPE
+    assert append(L, A[11], A[1], n_pages=1 << 30, v_page_stride=1 << 36) == B.ERR_BAD_SHAPE
+    assert append(L, A[1], A[11], n_pages=1 << 20, k_page_stride=1 << 38) == B.ERR_ALIASING      # 2^59 bytes: counted
+
+
 def test_the_binding_names_short_strides_for_axes_with_one_entry():
     """Views of one tensor of 2^32 elements: (page, slot, head) strides that the library takes."""
     both = torch.empty((1 << 20, 2, 16, 1, 128), dtype=torch.bfloat16, device="meta")
